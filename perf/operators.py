@@ -1,0 +1,453 @@
+"""Measured work of the cleartext training operators: the gated feed-forward block and the AdamW step.
+
+A program that prepares weights for encrypted inference trains a head in the clear: it holds activations, weights, gradient
+buffers, optimiser states and workspaces on the GPU and calls a block's forward pass, its backward pass and one optimiser
+step over all tensors.  The same forward pass answers cleartext requests, down to single rows.  `run` makes these calls where
+`own` is true; where it is false it computes them by elementary torch operations in 32 bits, rounded once at the end.
+
+Activations in front of a layer are standard normal, weights N(0, 1/fan_in), so that the arguments of the activation are of
+order one, where the polynomials that replace it under encryption hold.  Gradients span magnitudes from tensor to tensor, as
+they do between layers.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+# the cubics c0 + c1 g + c2 g^2 + c3 g^3 of the encrypted schedules
+CUBICS = {
+    "linear": (0.0, 1.0, 0.0, 0.0),
+    "square": (0.0, 0.0, 1.0, 0.0),
+    "poly2": (0.0, 0.500000000000008, 0.000469841857369822, 0.0),
+    "poly3": (0.5, 0.25, 0.0, -0.02),
+}
+LR, BETA1, BETA2, EPS, DECAY, STEP = 1e-3, 0.9, 0.999, 1e-8, 0.01, 7
+BLOCK = 256  # elements of a state that share one unit
+
+
+def listed():
+    return [
+        # one request in the clear through a head of transformer proportions: latency, the weights are read once
+        {"name": "ff_1x1024", "op": "ff", "rows": 1, "d_in": 1024, "d_hidden": 4096, "d_out": 1024, "type": "bf16", "act": "silu"},
+        # a handful of requests at sizes that are multiples of nothing
+        {"name": "ff_7x999", "op": "ff", "rows": 7, "d_in": 999, "d_hidden": 2731, "d_out": 501, "type": "f16", "act": "gelu"},
+        # the features of the 2^16 network's images (3136 -> 256 -> 2) through its head, in full precision: the reference that decrypted
+        # answers are compared with
+        {"name": "ff_1024x3136", "op": "ff", "rows": 1024, "d_in": 3136, "d_hidden": 256, "d_out": 2, "type": "f32", "act": "poly3"},
+        # the fully connected width of Table 1 (4096), a batch of images
+        {"name": "ff_4096x4096", "op": "ff", "rows": 4096, "d_in": 4096, "d_hidden": 4096, "d_out": 4096, "type": "bf16", "act": "poly2"},
+        # training step of a small head (3136 -> 256 -> 2) on a batch of 64
+        {"name": "train_64x3136", "op": "train", "rows": 64, "d_in": 3136, "d_hidden": 256, "d_out": 2, "type": "f32", "act": "square", "grads": "f32"},
+        # ... of odd sizes, gradients of 16-bit weights in 32 bits
+        {"name": "train_333x517", "op": "train", "rows": 333, "d_in": 517, "d_hidden": 1021, "d_out": 129, "type": "bf16", "act": "poly3", "grads": "f32"},
+        # ... of an ordinary block
+        {"name": "train_2048x1024", "op": "train", "rows": 2048, "d_in": 1024, "d_hidden": 4096, "d_out": 1024, "type": "bf16", "act": "square",
+         "grads": "bf16"},
+        # ... of the largest, many rows
+        {"name": "train_16384x2048", "op": "train", "rows": 16384, "d_in": 2048, "d_hidden": 8192, "d_out": 2048, "type": "bf16", "act": "silu",
+         "grads": "bf16"},
+        # optimiser step over a small head's three tensors
+        {"name": "adamw_3x32", "op": "adamw", "tensors": 3, "least": 512, "most": 802816, "bits": 32, "type": "f32", "grads": "f32", "copy": False},
+        # ... over many tensors from single biases to matrices, states in 8 bits, 16-bit copy for the next forward pass
+        {"name": "adamw_160x8", "op": "adamw", "tensors": 160, "least": 1, "most": 4194304, "bits": 8, "type": "f32", "grads": "bf16", "copy": True},
+        # ... over a few large matrices
+        {"name": "adamw_12x32", "op": "adamw", "tensors": 12, "least": 16777216, "most": 37748736, "bits": 32, "type": "f32", "grads": "bf16", "copy": True},
+        {"name": "adamw_9x8", "op": "adamw", "tensors": 9, "least": 16777216, "most": 37748736, "bits": 8, "type": "bf16", "grads": "bf16", "copy": False},
+    ]
+
+
+def _size(rng, least, most):
+    """spread over the logarithm; half of the sizes multiples of 64, a quarter of 8, a quarter of anything"""
+    n = int(round(math.exp(rng.uniform(math.log(least), math.log(most)))))
+    step = rng.choice((64, 64, 8, 1))
+    return max(least, min(most, n if n < step else n // step * step))
+
+
+def draw(rng):
+    op = rng.choice(("ff", "train", "adamw"))
+    kind = rng.choice(("bf16", "bf16", "f16", "f32"))
+    if op == "adamw":
+        least = _size(rng, 1, 65536)
+        most = _size(rng, least, 16777216)
+        tensors = _size(rng, 1, 160)
+        while tensors > 1 and tensors * (most + least) / 2 > 2.4e8:
+            tensors //= 2
+        bits, kind = rng.choice((8, 32)), rng.choice(("f32", "f32", kind))
+        return {"op": op, "tensors": tensors, "least": least, "most": most, "bits": bits, "type": kind, "grads": rng.choice((kind, "bf16")),
+                "copy": kind == "f32" and rng.random() < 0.5}
+    while True:
+        # single rows and a handful are drawn as often as batches
+        rows, d_in, d_hidden = _size(rng, 1, rng.choice((16, 16384))), _size(rng, 64, 8192), _size(rng, 64, 8192)
+        d_out = rng.choice((d_in, _size(rng, 2, 8192)))
+        cost = rows * d_hidden * (2.0 * d_in + d_out) * (8 if kind == "f32" else 1)
+        if cost <= 16384 * 2048.0 * 8192 * 3 / 2:
+            break
+    act = rng.choice(("linear", "square", "poly2", "poly3", "relu", "silu", "gelu"))
+    case = {"op": op, "rows": rows, "d_in": d_in, "d_hidden": d_hidden, "d_out": d_out, "type": kind, "act": act}
+    return dict(case, grads=rng.choice((kind, "f32"))) if op == "train" else case
+
+
+def _numels(case):
+    r = random.Random(case["tensors"])
+    lo, hi = math.log(case["least"]), math.log(case["most"])
+    return [max(case["least"], min(case["most"], int(round(math.exp(r.uniform(lo, hi)))))) for _ in range(case["tensors"])]
+
+
+def _normal(g, shape, scale, dtype):
+    return torch.randn(shape, generator=g, device=DEV).mul_(scale).to(dtype)
+
+
+# --------------------------------------------------------------------------- inputs
+def _ff_inputs(case, seed):
+    g = torch.Generator(DEV).manual_seed(seed)
+    M, K, H, O = case["rows"], case["d_in"], case["d_hidden"], case["d_out"]
+    t = TYPES[case["type"]]
+    s = {"x": _normal(g, (M, K), 1.0, t), "wg": _normal(g, (H, K), K**-0.5, t), "wu": _normal(g, (H, K), K**-0.5, t), "wd": _normal(g, (O, H), H**-0.5, t)}
+    if case["op"] == "train":
+        s["dy"] = _normal(g, (M, O), 1.0, t)
+    return s
+
+
+def _views(flat, numels, align=BLOCK):
+    """the tensors that lie one behind the other in a program's buffer, each from a multiple of `align` on"""
+    out, at = [], 0
+    for n in numels:
+        out.append(flat[at : at + n])
+        at += -(-n // align) * align
+    return out
+
+
+def _flat(numels, dtype, align=BLOCK):
+    return torch.zeros(sum(-(-n // align) * align for n in numels), dtype=dtype, device=DEV)
+
+
+def _adamw_inputs(case, seed):
+    """parameters, gradients and the states that earlier steps left: m a mean of gradients, v a mean of their squares; each kind in
+    one buffer ("flat") and as tensors in it"""
+    g = torch.Generator(DEV).manual_seed(seed)
+    numels = _numels(case)
+    state = torch.float32 if case["bits"] == 32 else torch.uint8
+    kinds = {"p": TYPES[case["type"]], "g": TYPES[case["grads"]], "m": state, "v": state}
+    if case["copy"]:
+        kinds["copy"] = torch.bfloat16
+    flat = {k: _flat(numels, t) for k, t in kinds.items()}
+    s = {k: _views(f, numels) for k, f in flat.items()}
+    blocks = [-(-n // BLOCK) for n in numels]
+    if case["bits"] == 8:
+        for k in ("mu", "ru"):
+            flat[k] = _flat(blocks, torch.float32, 1)
+            s[k] = _views(flat[k], blocks, 1)
+    for i, n in enumerate(numels):
+        scale = 10.0 ** (-4 + i % 4)
+        s["p"][i].copy_(_normal(g, n, 0.05, torch.float32))
+        s["g"][i].copy_(_normal(g, n, scale, torch.float32))
+        m = _normal(g, n, 0.2 * scale, torch.float32)
+        v = _normal(g, n, 1.0, torch.float32).square_().add_(0.1).mul_(0.1 * scale * scale)
+        if case["bits"] == 8:
+            m, mu = _code(m, _dither(seed + 1, i, n, 0), 3)
+            v, ru = _code(v.sqrt_(), _dither(seed + 1, i, n, 1), 4)
+            s["mu"][i].copy_(mu)
+            s["ru"][i].copy_(ru)
+        s["m"][i].copy_(m)
+        s["v"][i].copy_(v)
+        if case["copy"]:
+            s["copy"][i].copy_(s["p"][i])
+    if case["bits"] == 8:  # where the states are read back as values
+        flat["m_value"], flat["v_value"] = _flat(numels, torch.float32), _flat(numels, torch.float32)
+        s["m_value"], s["v_value"] = _views(flat["m_value"], numels), _views(flat["v_value"], numels)
+    s["flat"], s["seed"] = flat, seed
+    return s
+
+
+def _adamw_out(s):
+    """the buffers that a step has updated; 8-bit states as the values they stand for"""
+    f = s["flat"]
+    out = {"p": f["p"], "m": f.get("m_value", f["m"]), "v": f.get("v_value", f["v"])}
+    if "copy" in f:
+        out["copy"] = f["copy"]
+    return out
+
+
+def prepare(case, seed):
+    s = _adamw_inputs(case, seed) if case["op"] == "adamw" else _ff_inputs(case, seed)
+    s["case"] = case
+    if not own:
+        return s
+    from paper_1911_11377_amd import ckksmi, training
+
+    s["ctx"] = ctx = ckksmi.Context(12, 3, 40, 1, 41, 1, device=0)
+    if case["op"] == "adamw":
+        s["opt"] = training.AdamW(ctx, s["p"], s["g"], s["m"], s["v"], m_units=s.get("mu"), r_units=s.get("ru"), copies=s.get("copy"))
+        return s
+    act = CUBICS.get(case["act"], case["act"])
+    s["ff"] = ff = training.GatedFF(ctx, case["d_in"], case["d_hidden"], case["d_out"], TYPES[case["type"]], act, grad_dtype=TYPES[case.get("grads", case["type"])])
+    train = case["op"] == "train"
+    s["y"] = torch.empty(case["rows"], case["d_out"], dtype=s["x"].dtype, device=DEV)
+    s["ws"] = torch.empty(max(16, ff.workspace_bytes(case["rows"], backward=train)), dtype=torch.uint8, device=DEV)
+    if train:
+        s["saved"] = torch.empty(max(16, ff.saved_bytes(case["rows"])), dtype=torch.uint8, device=DEV)
+        s["dx"] = torch.empty_like(s["x"])
+        s["dw"] = [torch.empty(s[k].shape, dtype=TYPES[case["grads"]], device=DEV) for k in ("wg", "wu", "wd")]
+    return s
+
+
+# --------------------------------------------------------------------------- one pass
+def run(s):
+    case = s["case"]
+    if case["op"] == "adamw":
+        return _adamw_own(s) if own else _adamw_plain(s)
+    if not own:
+        return _ff_plain(s)
+    if case["op"] == "ff":
+        s["ff"].forward(s["x"], s["wg"], s["wu"], s["wd"], s["y"], s["ws"])
+        return {"y": s["y"]}
+    s["ff"].forward(s["x"], s["wg"], s["wu"], s["wd"], s["y"], s["ws"], saved=s["saved"])
+    s["ff"].backward(s["x"], s["wg"], s["wu"], s["wd"], s["saved"], s["dy"], s["dx"], *s["dw"], s["ws"])
+    return {"y": s["y"], "dx": s["dx"], "dwg": s["dw"][0], "dwu": s["dw"][1], "dwd": s["dw"][2]}
+
+
+def _adamw_own(s):
+    s["opt"].step(LR, (BETA1, BETA2), EPS, DECAY, STEP, seed=s["seed"])
+    if s["case"]["bits"] == 8:
+        s["opt"].read_states(s["m_value"], s["v_value"])
+    return _adamw_out(s)
+
+
+# --------------------------------------------------------------------------- plain forms
+def _act(g, name):
+    """act(g) and act'(g)"""
+    if name in CUBICS:
+        c0, c1, c2, c3 = CUBICS[name]
+        return ((c3 * g + c2) * g + c1) * g + c0, (3.0 * c3 * g + 2.0 * c2) * g + c1
+    if name == "relu":
+        on = (g > 0).to(g.dtype)
+        return g * on, on
+    if name == "silu":
+        q = 1.0 / (1.0 + torch.exp(-g))
+        return g * q, q * (1.0 + g * (1.0 - q))
+    q = 0.5 * (1.0 + torch.erf(g * 0.5**0.5))
+    return g * q, q + g * torch.exp(-0.5 * g * g) * (2.0 * math.pi) ** -0.5
+
+
+def _ff_plain(s):
+    case, t = s["case"], s["x"].dtype
+    x, wg, wu, wd = (s[k].float() for k in ("x", "wg", "wu", "wd"))
+    g, u = x @ wg.t(), x @ wu.t()
+    a, da = _act(g, case["act"])
+    h = a * u
+    out = {"y": (h @ wd.t()).to(t)}
+    if case["op"] == "ff":
+        return out
+    dy, tg = s["dy"].float(), TYPES[case["grads"]]
+    dh = dy @ wd
+    dg, du = dh * u * da, dh * a
+    out["dx"] = (dg @ wg + du @ wu).to(t)
+    out["dwg"], out["dwu"], out["dwd"] = (dg.t() @ x).to(tg), (du.t() @ x).to(tg), (dy.t() @ h).to(tg)
+    return out
+
+
+def _mix(h):
+    """32-bit words in int64 tensors: two rounds of shift, xor and product"""
+    h = h ^ (h >> 16)
+    h = (h * 0x6A09E667) & 0xFFFFFFFF
+    h = h ^ (h >> 15)
+    h = (h * 0xBB67AE85) & 0xFFFFFFFF
+    return h ^ (h >> 16)
+
+
+def _dither(seed, tensor, n, which):
+    """16 random bits for every element: words of (seed, tensor, block, element); the upper half rounds m, the lower sqrt(v)"""
+    key = torch.tensor([seed & 0xFFFFFFFF], dtype=torch.int64, device=DEV)
+    key = _mix((_mix(key) + ((seed >> 32) & 0xFFFFFFFF)) & 0xFFFFFFFF)
+    key = _mix((key + tensor) & 0xFFFFFFFF)
+    b = torch.arange(-(-n // BLOCK), dtype=torch.int64, device=DEV)
+    b = _mix((_mix((key + (b & 0xFFFFFFFF)) & 0xFFFFFFFF) + (b >> 32)) & 0xFFFFFFFF)
+    j = torch.arange(BLOCK, dtype=torch.int64, device=DEV) * 0x9E3779B9
+    h = _mix((b[:, None] + j) & 0xFFFFFFFF).reshape(-1)[:n]
+    return h >> 16 if which == 0 else h & 0xFFFF
+
+
+def _blocks(x):
+    n = x.numel()
+    out = torch.zeros(-(-n // BLOCK) * BLOCK, dtype=x.dtype, device=x.device)
+    out[:n] = x
+    return out.reshape(-1, BLOCK)
+
+
+def _code(x, dither, fraction):
+    """8-bit codes of x with `fraction` bits behind the leading one and 4 bits of exponent (below the smallest one evenly
+    spaced), with a sign for fraction 3; rounded at random to one of the two neighbours; one unit per block, chosen so that the
+    block's largest magnitude is the largest code"""
+    n, one = x.numel(), 1 << fraction
+    largest = float((2 * one - 1) << 14)
+    x = _blocks(x)
+    units = x.abs().amax(1) * (1.0 / largest)
+    bad = ~torch.isfinite(units)
+    units = torch.where(units < 1e-30, torch.zeros_like(units), units)
+    inv = torch.where(units > 0, torch.ones_like(units) / units, torch.zeros_like(units))
+    z = x.abs() * inv[:, None]
+    small = z < one
+    w = torch.where(small, z + one, z)
+    shift = 23 - fraction
+    word = w.view(torch.int32).to(torch.int64) + (_blocks(dither) << (shift - 16))
+    code = (word >> shift) - torch.where(small, (127 + fraction) << fraction, ((127 + fraction) << fraction) - one)
+    if fraction == 4:
+        code = torch.where(z > 0, code.clamp(min=1), code)
+    code = code.clamp(max=16 * one - 1)
+    if fraction == 3:
+        code = code + 128 * (x < 0).to(torch.int64)
+    code = torch.where(bad[:, None], torch.zeros_like(code), code)
+    return code.reshape(-1)[:n].to(torch.uint8), torch.where(bad, torch.full_like(units, math.nan), units)
+
+
+def _value(code, units, fraction):
+    one = 1 << fraction
+    c = code.to(torch.int64)
+    sign = 1.0
+    if fraction == 3:
+        sign = 1.0 - 2.0 * (c >> 7).float()
+        c = c & 127
+    e = (c >> fraction) - 1
+    # c < one: c itself; else (one + low bits) * 2^e, a whole number
+    whole = torch.where(e < 0, c, (one + (c & (one - 1))) << e.clamp(min=0)).float() * sign
+    n = whole.numel()
+    return (_blocks(whole) * units[:, None]).reshape(-1)[:n]
+
+
+def _f32(v):
+    return float(torch.tensor(v, dtype=torch.float64).to(torch.float32))
+
+
+def _adamw_plain(s):
+    case = s["case"]
+    decay, size, root = _f32(1.0 - LR * DECAY), _f32(LR / (1.0 - BETA1**STEP)), _f32(1.0 / math.sqrt(1.0 - BETA2**STEP))
+    for i, p in enumerate(s["p"]):
+        g = s["g"][i].float()
+        if case["bits"] == 8:
+            m, r = _value(s["m"][i], s["mu"][i], 3), _value(s["v"][i], s["ru"][i], 4)
+            v = r * r
+        else:
+            m, v = s["m"][i], s["v"][i]
+        m = m * _f32(BETA1) + g * _f32(1.0 - BETA1)
+        v = v * _f32(BETA2) + g * g * _f32(1.0 - BETA2)
+        r = torch.sqrt(v)
+        q = p.float() * decay - m / (r * root + _f32(EPS)) * size
+        p.copy_(q)
+        if case["copy"]:
+            s["copy"][i].copy_(q)
+        if case["bits"] == 8:
+            n = p.numel()
+            for x, k, u, value, which, fraction in ((m, "m", "mu", "m_value", 0, 3), (r, "v", "ru", "v_value", 1, 4)):
+                code, units = _code(x, _dither(s["seed"], i, n, which), fraction)
+                s[k][i].copy_(code)
+                s[u][i].copy_(units)
+                x = _value(code, units, fraction)
+                s[value][i].copy_(x if which == 0 else x * x)
+        else:
+            s["m"][i].copy_(m)
+            s["v"][i].copy_(v)
+    return _adamw_out(s)
+
+
+# --------------------------------------------------------------------------- 64 bits
+def exact(case, seed):
+    return _adamw_exact(case, seed) if case["op"] == "adamw" else _ff_exact(case, seed)
+
+
+def _ff_exact(case, seed):
+    s = {k: v.double() for k, v in _ff_inputs(case, seed).items()}
+    g = torch.matmul(s["x"], s["wg"].transpose(0, 1))
+    u = torch.matmul(s["x"], s["wu"].transpose(0, 1))
+    name = case["act"]
+    if name in CUBICS:
+        c = CUBICS[name]
+        a, da = sum(c[k] * g**k for k in range(4)), sum(k * c[k] * g ** (k - 1) for k in range(1, 4))
+    elif name == "relu":
+        a, da = torch.clamp(g, min=0.0), torch.where(g > 0, 1.0, 0.0).to(g.dtype)
+    elif name == "silu":
+        q = torch.sigmoid(g)
+        a, da = g * q, q + g * q * (1 - q)
+    else:
+        q = torch.special.ndtr(g)
+        a, da = g * q, q + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    h = a * u
+    out = {"y": torch.matmul(h, s["wd"].transpose(0, 1))}
+    if case["op"] == "train":
+        dh = torch.matmul(s["dy"], s["wd"])
+        dg, du = dh * u * da, dh * a
+        out["dx"] = torch.matmul(dg, s["wg"]) + torch.matmul(du, s["wu"])
+        out["dwg"] = torch.matmul(dg.transpose(0, 1), s["x"])
+        out["dwu"] = torch.matmul(du.transpose(0, 1), s["x"])
+        out["dwd"] = torch.matmul(s["dy"].transpose(0, 1), h)
+    return out
+
+
+def _exact_value(code, units, fraction):
+    c = code.double()
+    sign = torch.ones_like(c)
+    if fraction == 3:
+        sign = torch.where(c >= 128, -1.0, 1.0).to(c.dtype)
+        c = torch.where(c >= 128, c - 128, c)
+    one = 2.0**fraction
+    e = torch.floor(c / one)
+    value = torch.where(e == 0, c, (one + c - e * one) * torch.exp2(e - 1))
+    return sign * value * units.double().repeat_interleave(BLOCK)[: c.numel()]
+
+
+def _exact_round(x, dither, fraction):
+    """what the rounded state stands for: the position of |x| among the codes, plus 16 random bits of one place, cut"""
+    n, one = x.numel(), 2.0**fraction
+    top = (2 * one - 1) * 2.0**14
+    unit = (_blocks(x.abs()).max(1).values / top).repeat_interleave(BLOCK)[:n]
+    z = torch.where(unit > 0, x.abs() / torch.where(unit > 0, unit, 1.0), 0.0)
+    e = torch.clamp(torch.floor(torch.log2(torch.clamp(z, min=one / 2))) - fraction, min=0.0)
+    e = torch.where(z < one, -1.0, e)
+    place = torch.exp2(torch.clamp(e, min=0.0))
+    low = torch.floor(z / place + dither.double() / 65536.0)
+    value = torch.clamp(low * place, max=top)
+    if fraction == 4:
+        value = torch.where((x > 0) & (value < 1), torch.ones_like(value), value)
+    return torch.sign(x) * value * unit
+
+
+def _adamw_exact(case, seed):
+    s, numels = _adamw_inputs(case, seed), _numels(case)
+    out = {k: _flat(numels, torch.float64) for k in ("p", "m", "v") + (("copy",) if case["copy"] else ())}
+    at = {k: _views(f, numels) for k, f in out.items()}
+    for i, n in enumerate(numels):
+        g, p = s["g"][i].double(), s["p"][i].double()
+        if case["bits"] == 8:
+            m, v = _exact_value(s["m"][i], s["mu"][i], 3), _exact_value(s["v"][i], s["ru"][i], 4) ** 2
+        else:
+            m, v = s["m"][i].double(), s["v"][i].double()
+        m = BETA1 * m + (1 - BETA1) * g
+        v = BETA2 * v + (1 - BETA2) * g * g
+        p = p - LR * DECAY * p - LR * (m / (1 - BETA1**STEP)) / (torch.sqrt(v / (1 - BETA2**STEP)) + EPS)
+        if case["bits"] == 8:
+            m = _exact_round(m, _dither(seed, i, n, 0), 3)
+            v = _exact_round(torch.sqrt(v), _dither(seed, i, n, 1), 4) ** 2
+        at["p"][i].copy_(p)
+        at["m"][i].copy_(m)
+        at["v"][i].copy_(v)
+        if case["copy"]:
+            at["copy"][i].copy_(p)
+    return out
+
+
+# --------------------------------------------------------------------------- what a pass cannot do without
+def work(case):
+    size = {"f32": 4, "bf16": 2, "f16": 2}
+    if case["op"] == "adamw":
+        n = sum(_numels(case))
+        states = 16 if case["bits"] == 32 else 4 + 8 + 4 * 4 / BLOCK  # 8 bits: read and written, and read back as 32-bit values
+        return {"bytes": n * (2 * size[case["type"]] + size[case["grads"]] + states + (2 if case["copy"] else 0)), "flops": 16.0 * n}
+    M, K, H, O, e = case["rows"], case["d_in"], case["d_hidden"], case["d_out"], size[case["type"]]
+    weights = 2 * H * K + H * O
+    b, f = e * (M * K + weights + M * O), 2.0 * M * weights
+    if case["op"] == "train":
+        b, f = b + e * (M * O + M * K) + size[case["grads"]] * weights, 3 * f
+    return {"bytes": b, "flops": f}
