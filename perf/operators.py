@@ -138,7 +138,7 @@ def _adamw_inputs(case, seed):
     s = {k: _views(f, numels) for k, f in flat.items()}
     blocks = [-(-n // BLOCK) for n in numels]
     if case["bits"] == 8:
-        for k in ("mu", "ru"):
+        for k in ("mu", "vu"):
             flat[k] = _flat(blocks, torch.float32, 1)
             s[k] = _views(flat[k], blocks, 1)
     for i, n in enumerate(numels):
@@ -149,9 +149,9 @@ def _adamw_inputs(case, seed):
         v = _normal(g, n, 1.0, torch.float32).square_().add_(0.1).mul_(0.1 * scale * scale)
         if case["bits"] == 8:
             m, mu = _code(m, _dither(seed + 1, i, n, 0), 3)
-            v, ru = _code(v.sqrt_(), _dither(seed + 1, i, n, 1), 4)
+            v, vu = _code(v, _dither(seed + 1, i, n, 1), 4)
             s["mu"][i].copy_(mu)
-            s["ru"][i].copy_(ru)
+            s["vu"][i].copy_(vu)
         s["m"][i].copy_(m)
         s["v"][i].copy_(v)
         if case["copy"]:
@@ -181,7 +181,7 @@ def prepare(case, seed):
 
     s["ctx"] = ctx = ckksmi.Context(12, 3, 40, 1, 41, 1, device=0)
     if case["op"] == "adamw":
-        s["opt"] = training.AdamW(ctx, s["p"], s["g"], s["m"], s["v"], m_units=s.get("mu"), r_units=s.get("ru"), copies=s.get("copy"))
+        s["opt"] = training.AdamW(ctx, s["p"], s["g"], s["m"], s["v"], m_units=s.get("mu"), v_units=s.get("vu"), copies=s.get("copy"))
         return s
     act = CUBICS.get(case["act"], case["act"])
     s["ff"] = ff = training.GatedFF(ctx, case["d_in"], case["d_hidden"], case["d_out"], TYPES[case["type"]], act, grad_dtype=TYPES[case.get("grads", case["type"])])
@@ -260,7 +260,7 @@ def _mix(h):
 
 
 def _dither(seed, tensor, n, which):
-    """16 random bits for every element: words of (seed, tensor, block, element); the upper half rounds m, the lower sqrt(v)"""
+    """16 random bits for every element: words of (seed, tensor, block, element); the upper half rounds m, the lower v"""
     key = torch.tensor([seed & 0xFFFFFFFF], dtype=torch.int64, device=DEV)
     key = _mix((_mix(key) + ((seed >> 32) & 0xFFFFFFFF)) & 0xFFFFFFFF)
     key = _mix((key + tensor) & 0xFFFFFFFF)
@@ -287,7 +287,7 @@ def _code(x, dither, fraction):
     x = _blocks(x)
     units = x.abs().amax(1) * (1.0 / largest)
     bad = ~torch.isfinite(units)
-    units = torch.where(units < 1e-30, torch.zeros_like(units), units)
+    units = torch.where(units < 1e-36, torch.zeros_like(units), units)
     inv = torch.where(units > 0, torch.ones_like(units) / units, torch.zeros_like(units))
     z = x.abs() * inv[:, None]
     small = z < one
@@ -328,25 +328,22 @@ def _adamw_plain(s):
     for i, p in enumerate(s["p"]):
         g = s["g"][i].float()
         if case["bits"] == 8:
-            m, r = _value(s["m"][i], s["mu"][i], 3), _value(s["v"][i], s["ru"][i], 4)
-            v = r * r
+            m, v = _value(s["m"][i], s["mu"][i], 3), _value(s["v"][i], s["vu"][i], 4)
         else:
             m, v = s["m"][i], s["v"][i]
         m = m * _f32(BETA1) + g * _f32(1.0 - BETA1)
         v = v * _f32(BETA2) + g * g * _f32(1.0 - BETA2)
-        r = torch.sqrt(v)
-        q = p.float() * decay - m / (r * root + _f32(EPS)) * size
+        q = p.float() * decay - m / (torch.sqrt(v) * root + _f32(EPS)) * size
         p.copy_(q)
         if case["copy"]:
             s["copy"][i].copy_(q)
         if case["bits"] == 8:
             n = p.numel()
-            for x, k, u, value, which, fraction in ((m, "m", "mu", "m_value", 0, 3), (r, "v", "ru", "v_value", 1, 4)):
+            for x, k, u, which, fraction in ((m, "m", "mu", 0, 3), (v, "v", "vu", 1, 4)):
                 code, units = _code(x, _dither(s["seed"], i, n, which), fraction)
                 s[k][i].copy_(code)
                 s[u][i].copy_(units)
-                x = _value(code, units, fraction)
-                s[value][i].copy_(x if which == 0 else x * x)
+                s[k + "_value"][i].copy_(_value(code, units, fraction))
         else:
             s["m"][i].copy_(m)
             s["v"][i].copy_(v)
@@ -421,7 +418,7 @@ def _adamw_exact(case, seed):
     for i, n in enumerate(numels):
         g, p = s["g"][i].double(), s["p"][i].double()
         if case["bits"] == 8:
-            m, v = _exact_value(s["m"][i], s["mu"][i], 3), _exact_value(s["v"][i], s["ru"][i], 4) ** 2
+            m, v = _exact_value(s["m"][i], s["mu"][i], 3), _exact_value(s["v"][i], s["vu"][i], 4)
         else:
             m, v = s["m"][i].double(), s["v"][i].double()
         m = BETA1 * m + (1 - BETA1) * g
@@ -429,7 +426,7 @@ def _adamw_exact(case, seed):
         p = p - LR * DECAY * p - LR * (m / (1 - BETA1**STEP)) / (torch.sqrt(v / (1 - BETA2**STEP)) + EPS)
         if case["bits"] == 8:
             m = _exact_round(m, _dither(seed, i, n, 0), 3)
-            v = _exact_round(torch.sqrt(v), _dither(seed, i, n, 1), 4) ** 2
+            v = _exact_round(v, _dither(seed, i, n, 1), 4)
         at["p"][i].copy_(p)
         at["m"][i].copy_(m)
         at["v"][i].copy_(v)
