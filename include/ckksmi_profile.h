@@ -57,7 +57,12 @@ extern "C" {
 #define CKKSMI_K_NTT_LDS_GAL 34   /* whole inverse transform of a rotation's polynomial, read through the automorphism */
 #define CKKSMI_K_TAIL_SOURCES 35  /* sources of ModDown followed by rescale: inverse transforms of k + 1 limbs a row (units: limbs) */
 #define CKKSMI_K_MACWSUM_MFMA 36  /* weight sums of the matrix-core multiply-accumulate (units: channels x limbs) */
-#define CKKSMI_K_COUNT 37
+#define CKKSMI_K_GEMM 37          /* matrix products of the gated feed-forward block (units: operations) */
+#define CKKSMI_K_GEMM_JOIN 38     /* parts of a split k axis added up (units: operations of the products) */
+#define CKKSMI_K_GEMM_COPY 39     /* operands copied to aligned rows (units: workgroups) */
+#define CKKSMI_K_ADAMW 40         /* optimiser step (units: elements, to whole workgroups) */
+#define CKKSMI_K_ADAMW_READ 41    /* 8-bit states read back (the same) */
+#define CKKSMI_K_COUNT 42
 int ckksmi_profile_enable(ckksmi_ctx *ctx, int on);
 int ckksmi_profile_read(ckksmi_ctx *ctx, int kernel_class, double *total_ms, long long *launches, double *units);
 /* name of the kernel that class runs as in this context (the transforms have size-specific kernels; a fused kernel's variants for

@@ -1,4 +1,4 @@
-"""Thin Python binding of the C ABI in include/ckksmi.h.
+"""Thin Python binding of the C ABI in include/ckksmi.h (and the entry points of include/ckksmi_train.h, used by training.py).
 
 Argument marshalling only: every step of the hot path runs in the HIP library.
 Host-side functions take and return numpy arrays.  Device-side functions take
@@ -32,6 +32,26 @@ class Params(C.Structure):
         ("special_bits", C.c_int), ("alpha", C.c_int),
         ("moduli_override", u64p), ("psi_override", u64p), ("device", C.c_int),
     ]
+
+
+F32, BF16, F16 = 0, 1, 2
+ACT_POLY, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+STATE_BLOCK = 256
+
+
+class GatedFFShape(C.Structure):  # ckksmi_gated_ff
+    _fields_ = [("dtype", C.c_int), ("grad_dtype", C.c_int), ("act", C.c_int), ("c", C.c_float * 4), ("rows", C.c_int64), ("d_in", C.c_int64),
+                ("d_hidden", C.c_int64), ("d_out", C.c_int64), ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("ld_dy", C.c_int64), ("ld_dx", C.c_int64)]
+
+
+class AdamWTensor(C.Structure):  # ckksmi_adamw_tensor
+    _fields_ = [("p", VP), ("grad", VP), ("m", VP), ("v", VP), ("m_unit", VP), ("v_unit", VP), ("copy", VP), ("n", C.c_int64)]
+
+
+class AdamWParams(C.Structure):  # ckksmi_adamw
+    _fields_ = [("p_dtype", C.c_int), ("grad_dtype", C.c_int), ("copy_dtype", C.c_int), ("state_bits", C.c_int), ("lr", C.c_double), ("beta1", C.c_double),
+                ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double), ("grad_scale", C.c_double), ("step", C.c_int64),
+                ("seed", C.c_uint64), ("skip", VP)]
 
 
 class CkksmiError(RuntimeError):
@@ -87,13 +107,20 @@ SIGNATURES = {
     "ckksmi_fc_mac": [VP, VP, VP, C.c_int, C.c_int, VP, C.c_int, VP, C.c_size_t, VP],
     "ckksmi_sum_pool2d": [VP, VP, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, VP, C.c_int, VP],
     "ckksmi_workspace_bytes": [VP, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)],
+    "ckksmi_gated_ff_workspace_bytes": [VP, C.POINTER(GatedFFShape), C.c_int, C.POINTER(C.c_size_t)],
+    "ckksmi_gated_ff_saved_bytes": [VP, C.POINTER(GatedFFShape), C.POINTER(C.c_size_t)],
+    "ckksmi_gated_ff_forward": [VP, C.POINTER(GatedFFShape)] + [VP] * 7 + [C.c_size_t, VP],
+    "ckksmi_gated_ff_backward": [VP, C.POINTER(GatedFFShape)] + [VP] * 10 + [C.c_int, VP, C.c_size_t, VP],
+    "ckksmi_adamw_step": [VP, C.POINTER(AdamWParams), C.POINTER(AdamWTensor), C.c_int, VP],
+    "ckksmi_adamw_read_states": [VP, C.POINTER(AdamWTensor), C.c_int, C.POINTER(VP), C.POINTER(VP), VP],
     "ckksmi_profile_enable": [VP, C.c_int],
     "ckksmi_profile_read": [VP, C.c_int, f64p, C.POINTER(C.c_longlong), f64p],
     "ckksmi_kernel_class_name": [VP, C.c_int],
     "ckksmi_tune": [VP, C.c_int, C.c_int],
 }
 _RESTYPES = {"ckksmi_ctx_destroy": None, "ckksmi_strerror": C.c_char_p, "ckksmi_kernel_class_name": C.c_char_p}
-K_COUNT = 37
+TRAINING = ("ckksmi_gated_ff_", "ckksmi_adamw_")  # entry points of csrc/train_device.hip
+K_COUNT = 42
 
 _LIBS = {}
 
@@ -107,6 +134,8 @@ def load(path=None):
         raise RuntimeError("%s not found: build it first (python -c 'import __graft_entry__ as g; g.build()')" % path)
     L = C.CDLL(path)
     for name, args in SIGNATURES.items():
+        if path != DEFAULT_LIB and name.startswith(TRAINING) and not hasattr(L, name):
+            continue  # a build of the ciphertext operations alone; calling one of these raises
         f = getattr(L, name)
         f.argtypes = args
         f.restype = _RESTYPES.get(name, C.c_int)

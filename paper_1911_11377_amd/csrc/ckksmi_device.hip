@@ -1,10 +1,5 @@
 // Device side of the C ABI: constant-table upload, argument validation and the
 // kernel launch sequences of every ciphertext operation.
-#ifndef CKKSMI_EMULATE
-#include <hip/hip_runtime.h>
-#define CKKSMI_LAUNCH(kern, grid, block, stream, ...) hipLaunchKernelGGL(kern, grid, block, 0, stream, __VA_ARGS__)
-#endif
-
 #include <algorithm>
 #include <cstdio>
 #include <cstdlib>
@@ -12,6 +7,7 @@
 #include <mutex>
 
 #include "ckksmi_internal.h"
+#include "device_call.h"
 #include "kernels.h"
 #include "ntt_v2.h"
 #include "ks_fused.h"
@@ -21,22 +17,6 @@
 #include "encode_device.h"
 #include "mac_mfma.h"
 #include "mac_rns.h"
-
-// Launch `kern`; when profiling is on, bracket it with two events on the same stream and
-// remember them under kernel class `kid` together with `units` of algorithmic work.
-#define KL(c, kid, units, kern, grid, block, st, ...)                                   \
-    do {                                                                                \
-        ProfRec *pr_ = (c)->prof_on ? prof_begin((c), (kid), (double)(units), (st)) : nullptr; \
-        CKKSMI_LAUNCH(kern, grid, block, st, __VA_ARGS__);                              \
-        if (pr_) (void)hipEventRecord((hipEvent_t)pr_->stop, (st));                     \
-    } while (0)
-
-// ... one of two instances of a kernel template
-#define KL2(c, kid, units, first, kern1, kern2, grid, block, st, ...)              \
-    do {                                                                            \
-        if (first) KL(c, kid, units, kern1, grid, block, st, __VA_ARGS__);          \
-        else KL(c, kid, units, kern2, grid, block, st, __VA_ARGS__);                \
-    } while (0)
 
 // Scratch memory of ckksmi_rescale_static, the one entry point that takes no workspace: a file-scope device array, one copy
 // per GPU, held until the process ends.  Host code never uses the array's name as an address: every device's copy is
@@ -60,29 +40,6 @@ bool lookup_static_scratch(int device) {
     return true;
 }
 
-ProfRec *prof_begin(ckksmi_ctx *c, int kid, double units, hipStream_t st) {
-    hipEvent_t a, b;
-    if (hipEventCreate(&a) != hipSuccess) return nullptr;
-    if (hipEventCreate(&b) != hipSuccess) { (void)hipEventDestroy(a); return nullptr; }
-    (void)hipEventRecord(a, st);
-    c->prof.push_back(ProfRec{kid, units, (void *)a, (void *)b});
-    return &c->prof.back();
-}
-
-struct Guard {  // records the first HIP error of a call
-    ckksmi_ctx *c;
-    bool ok = true;
-    explicit Guard(ckksmi_ctx *ctx) : c(ctx) {}
-    void check(hipError_t e) {
-        if (e != hipSuccess && ok) { ok = false; c->last_hip_error = (int)e; }
-    }
-    int rc() {
-        check(hipGetLastError());
-        if (c->no_kernel.exchange(false)) return CKKSMI_EUNSUPPORTED;
-        return ok ? CKKSMI_OK : CKKSMI_EDEVICE;
-    }
-};
-
 template <class Tp>
 Tp *upload(ckksmi_ctx *c, const Tp *host, size_t count, bool &ok) {
     void *p = nullptr;
@@ -94,9 +51,6 @@ Tp *upload(ckksmi_ctx *c, const Tp *host, size_t count, bool &ok) {
 }
 
 inline int la_for(int logN) { return logN <= 12 ? 0 : std::min(8, logN - 8); }
-
-inline bool dev_ok(const ckksmi_ctx *c) { return c && c->device >= 0; }
-inline hipStream_t S(void *s) { return (hipStream_t)s; }
 
 LimbMap table_map(const int *index, int n_limbs, size_t src_stride, size_t dst_stride) {
     LimbMap M;
@@ -1948,7 +1902,7 @@ extern "C" const char *ckksmi_kernel_class_name(const ckksmi_ctx *c, int kernel_
                                                 "rows_final_kernel", "modup_cols_kernel", "conv_mac_mfma_kernel", "mac_prepare_mfma_kernel", "ntt_wg_kernel", "tensor_rows_kernel",
                                                 "axpy_limb_kernel", "modup_cols_kernel", "inner_product_hoisted_tile_kernel", "automorphism_bcast_kernel",
                                                 "encoding kernels", "encryption kernels", "modup_cols_kernel", "conv_mac_mfma_resident_kernel", "conv_mac_mfma_strip_kernel", "conv_final_kernel", "inner_wg_kernel",
-                                                "tensor_wg_kernel", "ntt_wg_inv_gal_kernel", "tail_sources_kernel", "mac_wsum_kernel"};
+                                                "tensor_wg_kernel", "ntt_wg_inv_gal_kernel", "tail_sources_kernel", "mac_wsum_kernel", "gemm_kernel", "gemm_join_kernel", "pad_rows_kernel", "adamw_kernel", "adamw_read_kernel"};
     if (kernel_class < 0 || kernel_class >= CKKSMI_K_COUNT) return "";
     if (c && kernel_class == CKKSMI_K_INNER_HOISTED && !hoisted_tile_ok(c, c->beta_top)) return "inner_product_hoisted_kernel";
     if (c && c->logN >= 12 && c->logN <= 16) {

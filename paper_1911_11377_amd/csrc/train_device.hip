@@ -1,0 +1,447 @@
+// Device side of include/ckksmi_train.h: argument checks and launch sequences.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "device_call.h"
+#include "train_adamw.h"
+#include "train_gemm.h"
+
+namespace {
+
+constexpr int64_t kMaxDim = 1 << 20, kMaxRows = 0x7fffffff - 256;
+constexpr int64_t kMaxNumel = (int64_t)1 << 40;
+
+inline size_t round_up(size_t v, size_t to) { return (v + to - 1) / to * to; }
+inline bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+inline bool dtype_ok(int d) { return d == CKKSMI_F32 || d == CKKSMI_BF16 || d == CKKSMI_F16; }
+
+int check_ff(const ckksmi_gated_ff *f) {
+    if (!f || !dtype_ok(f->dtype) || (f->grad_dtype != f->dtype && f->grad_dtype != CKKSMI_F32) || f->act < CKKSMI_ACT_POLY || f->act > CKKSMI_ACT_GELU) return CKKSMI_EINVAL;
+    if (f->rows < 0 || f->rows > kMaxRows) return CKKSMI_EINVAL;
+    const int64_t d[3] = {f->d_in, f->d_hidden, f->d_out};
+    for (int64_t v : d)
+        if (v < 1 || v > kMaxDim) return CKKSMI_EINVAL;
+    const int64_t ld[4] = {f->ld_x, f->ld_y, f->ld_dy, f->ld_dx}, least[4] = {f->d_in, f->d_out, f->d_out, f->d_in};
+    for (int i = 0; i < 4; i++)
+        if (ld[i] != 0 && (ld[i] < least[i] || ld[i] > kMaxDim)) return CKKSMI_EINVAL;
+    return CKKSMI_OK;
+}
+
+// [a, a + na) and [b, b + nb) share a byte
+inline bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+    if (!a || !b || !na || !nb) return false;
+    const char *x = (const char *)a, *y = (const char *)b;
+    return x < y + nb && y < x + na;
+}
+
+// A workspace handed out piece by piece; with base == nullptr it only counts
+struct Carve {
+    char *base;
+    size_t size, used = 0;
+    Carve(void *p, size_t n) : base((char *)p), size(n) {}
+    char *take(size_t bytes) {
+        char *p = base ? base + used : nullptr;
+        used += round_up(bytes, 256);
+        return p;
+    }
+    bool fits() const { return used <= size; }
+};
+
+// one operand of a product: rows of `cols` elements, `ld` bytes apart
+struct Matrix {
+    const char *p;
+    size_t ld;
+};
+
+struct FF {  // a call's sizes
+    size_t es, ges, M, K, H, O, ldh;
+    explicit FF(const ckksmi_gated_ff &f)
+        : es(element_bytes(f.dtype)), ges(element_bytes(f.grad_dtype)), M((size_t)f.rows), K((size_t)f.d_in), H((size_t)f.d_hidden), O((size_t)f.d_out), ldh(round_up(H, 8)) {}
+    size_t hidden_bytes() const { return round_up(M * ldh * es, 256); }
+};
+inline size_t ld_bytes(int64_t ld, size_t cols, size_t es) { return (ld ? (size_t)ld : cols) * es; }
+
+Activation activation_of(const ckksmi_gated_ff &f) {
+    Activation a;
+    a.kind = f.act;
+    memcpy(a.c, f.c, sizeof(a.c));
+    return a;
+}
+
+// What a product's launch looks like: tile shape (an index of kTiles) and parts of the k axis
+struct Shape { int tile, splits; };
+struct TileShape { int bm, bn; };
+constexpr TileShape kTiles[3] = {{256, 256}, {128, 128}, {32, 128}};
+constexpr int kMaxSplits = 32;
+
+int tiles_of(const GemmProblem &p, const TileShape &t, bool gate, GemmProblem *out) {
+    const int cols = gate ? t.bn / 2 : t.bn;
+    const int tm = (p.M + t.bm - 1) / t.bm, tn = (p.N + cols - 1) / cols;
+    if (out) { out->tiles_m = tm; out->tiles_n = tn; }
+    return tm * tn;
+}
+
+Shape choose(const GemmProblem *p, int n, bool gate, size_t es) {
+    int most = 0;
+    for (int i = 0; i < n; i++) most = std::max(most, p[i].M);
+    Shape s;
+    s.tile = most <= 32 ? 2 : 1;
+    int tiles[2] = {0, 0};
+    for (int i = 0; i < n; i++) {
+        tiles[0] += tiles_of(p[i], kTiles[0], gate, nullptr);
+        tiles[1] += tiles_of(p[i], kTiles[s.tile], gate, nullptr);
+    }
+    if (es == 2 && tiles[0] >= 192) {
+        s.tile = 0;
+        s.splits = 1;
+        return s;
+    }
+    const int steps = (int)(((size_t)p[0].K * es + TG_STEP_BYTES - 1) / TG_STEP_BYTES) * p[0].nsrc;
+    s.splits = std::max(1, std::min(std::min(512 / std::max(1, tiles[1]), steps / 4), kMaxSplits));
+    return s;
+}
+
+size_t part_bytes(const GemmProblem &p, int splits, bool gate) {
+    return splits > 1 ? (size_t)splits * (gate ? 2 : 1) * p.M * round_up(p.N, 8) * sizeof(float) : 0;
+}
+
+// Up to TG_PROBLEMS products of one kind in a launch; `w` gives the memory for a split k axis
+template <class T, bool A_ROWS, bool B_ROWS, int EPI>
+void launch_gemm(ckksmi_ctx *c, GemmProblem *p, int n, Carve w, hipStream_t st) {
+    constexpr bool gate = EPI == EPI_GATE;
+    const Shape s = choose(p, n, gate, sizeof(T));
+    GemmArgs G;
+    memset(&G, 0, sizeof(G));
+    int total = 0, join = 0;
+    double flops = 0;
+    for (int i = 0; i < n; i++) {
+        G.first[i] = total;
+        total += tiles_of(p[i], kTiles[s.tile], gate, &p[i]);
+        p[i].ld_part = round_up(p[i].N, 8);
+        if (s.splits > 1) p[i].part = (float *)w.take(part_bytes(p[i], s.splits, gate));
+        G.p[i] = p[i];
+        join = std::max(join, (int)(((size_t)p[i].M * p[i].ld_part / 8 + 255) / 256));
+        flops += 2.0 * p[i].M * p[i].N * p[i].K * (gate ? 2 : p[i].nsrc);
+    }
+    G.first[n] = total;
+    G.n_problems = n;
+    G.splits = s.splits;
+    const dim3 grid(total, s.splits);
+    if constexpr (sizeof(T) == 2)
+        if (s.tile == 0) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 256, 256, 128, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(512), st, G);
+    if (s.tile == 1) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 128, 128, 64, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(256), st, G);
+    if (s.tile == 2) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 32, 128, 16, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(256), st, G);
+    if (s.splits > 1) KL(c, CKKSMI_K_GEMM_JOIN, flops, (gemm_join_kernel<T, EPI>), dim3(join, n), dim3(256), st, G);
+}
+
+GemmProblem product(Matrix a, Matrix b, size_t M, size_t N, size_t K) {
+    GemmProblem p;
+    memset(&p, 0, sizeof(p));
+    p.a[0] = a.p; p.b[0] = b.p; p.lda = a.ld; p.ldb = b.ld;
+    p.M = (int)M; p.N = (int)N; p.K = (int)K; p.nsrc = 1;
+    return p;
+}
+
+void store_to(GemmProblem &p, void *out, size_t ld_elements, int out_dtype, bool accumulate) {
+    const size_t es = element_bytes(out_dtype);
+    p.epi.o0 = out; p.epi.ldo = ld_elements; p.epi.N = p.N; p.epi.f32_out = out_dtype == CKKSMI_F32; p.epi.accumulate = accumulate;
+    p.epi.whole = p.N % 8 == 0 && aligned(out, 16) && ld_elements * es % 16 == 0;
+}
+
+// Operands whose rows begin on 16 bytes and hold whole 16-byte chunks are used where they lie, others through a padded copy
+template <class T> struct Operands {
+    CopyArgs C;
+    unsigned blocks = 0;
+    Operands() { memset(&C, 0, sizeof(C)); }
+    Matrix use(const void *src, size_t ld, size_t rows, size_t cols, Carve &w) {
+        constexpr size_t es = sizeof(T);
+        const size_t ld_dst = round_up(cols * es, 16);
+        char *dst = w.take(rows * ld_dst);  // counted whether needed or not: the workspace's size does not depend on addresses
+        if (aligned(src, 16) && ld % 16 == 0 && cols * es % 16 == 0) return Matrix{(const char *)src, ld};
+        CopyArgs::One &o = C.c[C.n++];
+        o.src = (const char *)src; o.dst = dst; o.ld_src = ld; o.ld_dst = ld_dst; o.cols = (int)cols; o.chunks = (int)(ld_dst / 16); o.rows = rows;
+        o.first = blocks;
+        blocks += (unsigned)((rows * o.chunks + 255) / 256);
+        return Matrix{dst, ld_dst};
+    }
+    void run(ckksmi_ctx *c, hipStream_t st) {
+        if (blocks) KL(c, CKKSMI_K_GEMM_COPY, blocks, pad_rows_kernel<T>, dim3(blocks), dim3(256), st, C);
+    }
+};
+
+// the products' shapes alone, for the workspace: as the passes below form them
+size_t split_bytes(const ckksmi_gated_ff &f, bool backward) {
+    const FF d(f);
+    const Matrix none{nullptr, 0};
+    auto one = [&](GemmProblem p, bool gate) { return part_bytes(p, choose(&p, 1, gate, d.es).splits, gate) + 256; };
+    size_t most = std::max(one(product(none, none, d.M, d.H, d.K), true), one(product(none, none, d.M, d.O, d.H), false));
+    if (!backward || d.M == 0) return most;
+    GemmProblem dx = product(none, none, d.M, d.K, d.H);
+    dx.nsrc = 2;
+    most = std::max(most, std::max(one(product(none, none, d.M, d.H, d.O), false), one(dx, false)));
+    GemmProblem dw[3] = {product(none, none, d.H, d.K, d.M), product(none, none, d.H, d.K, d.M), product(none, none, d.O, d.H, d.M)};
+    const int splits = choose(dw, 3, false, d.es).splits;
+    return std::max(most, part_bytes(dw[0], splits, false) * 2 + part_bytes(dw[2], splits, false) + 768);
+}
+
+size_t workspace_of(const ckksmi_gated_ff &f, bool backward) {
+    const FF d(f);
+    auto rows = [&](size_t r, size_t cols) { return round_up(r * round_up(cols * d.es, 16), 256); };
+    const size_t weights = 2 * rows(d.H, d.K) + rows(d.O, d.H);
+    const size_t forward = rows(d.M, d.K) + weights + d.hidden_bytes();
+    const size_t back = rows(d.M, d.K) + weights + rows(d.M, d.O) + 2 * d.hidden_bytes();
+    return (backward ? std::max(forward, back) : forward) + split_bytes(f, backward);
+}
+
+template <class T>
+int forward(ckksmi_ctx *c, const ckksmi_gated_ff &f, const void *x, const void *wg, const void *wu, const void *wd, void *y, void *saved, Carve w, hipStream_t st) {
+    const FF d(f);
+    Guard guard(c);
+    Operands<T> ops;
+    const Matrix mx = ops.use(x, ld_bytes(f.ld_x, d.K, d.es), d.M, d.K, w), mg = ops.use(wg, d.K * d.es, d.H, d.K, w), mu = ops.use(wu, d.K * d.es, d.H, d.K, w);
+    const Matrix md = ops.use(wd, d.H * d.es, d.O, d.H, w);
+    char *h = w.take(d.hidden_bytes());
+    char *const keep = (char *)saved;
+    if (keep) h = keep + 2 * d.hidden_bytes();
+    ops.run(c, st);
+
+    GemmProblem gate = product(mx, mg, d.M, d.H, d.K);
+    gate.b[1] = mu.p;
+    gate.epi.o0 = h; gate.epi.o1 = keep; gate.epi.o2 = keep ? keep + d.hidden_bytes() : nullptr;
+    gate.epi.ldo = d.ldh; gate.epi.N = (int)d.H; gate.epi.act = activation_of(f);
+    launch_gemm<T, false, false, EPI_GATE>(c, &gate, 1, w, st);
+
+    GemmProblem down = product(Matrix{h, d.ldh * d.es}, md, d.M, d.O, d.H);
+    store_to(down, y, f.ld_y ? f.ld_y : d.O, f.dtype, false);
+    launch_gemm<T, false, false, EPI_STORE>(c, &down, 1, w, st);
+    return guard.rc();
+}
+
+template <class T>
+int backward(ckksmi_ctx *c, const ckksmi_gated_ff &f, const void *x, const void *wg, const void *wu, const void *wd, const void *saved, const void *dy, void *dx,
+             void *dwg, void *dwu, void *dwd, bool accumulate, Carve w, hipStream_t st) {
+    const FF d(f);
+    Guard guard(c);
+    Operands<T> ops;
+    const Matrix mx = ops.use(x, ld_bytes(f.ld_x, d.K, d.es), d.M, d.K, w), mg = ops.use(wg, d.K * d.es, d.H, d.K, w), mu = ops.use(wu, d.K * d.es, d.H, d.K, w);
+    const Matrix md = ops.use(wd, d.H * d.es, d.O, d.H, w), mdy = ops.use(dy, ld_bytes(f.ld_dy, d.O, d.es), d.M, d.O, w);
+    char *dg = w.take(d.hidden_bytes()), *du = w.take(d.hidden_bytes());
+    const char *g = (const char *)saved, *u = g + d.hidden_bytes(), *h = u + d.hidden_bytes();
+    const size_t ldh = d.ldh * d.es;
+    ops.run(c, st);
+
+    GemmProblem dh = product(mdy, md, d.M, d.H, d.O);
+    dh.epi.o0 = dg; dh.epi.o1 = du; dh.epi.g = g; dh.epi.u = u;
+    dh.epi.ldo = d.ldh; dh.epi.N = (int)d.H; dh.epi.act = activation_of(f);
+    launch_gemm<T, false, true, EPI_DHID>(c, &dh, 1, w, st);
+
+    if (dx) {
+        GemmProblem p = product(Matrix{dg, ldh}, mg, d.M, d.K, d.H);
+        p.a[1] = du; p.b[1] = mu.p; p.nsrc = 2;
+        store_to(p, dx, f.ld_dx ? f.ld_dx : d.K, f.dtype, false);
+        launch_gemm<T, false, true, EPI_STORE>(c, &p, 1, w, st);
+    }
+    GemmProblem dw[3] = {product(Matrix{dg, ldh}, mx, d.H, d.K, d.M), product(Matrix{du, ldh}, mx, d.H, d.K, d.M), product(mdy, Matrix{h, ldh}, d.O, d.H, d.M)};
+    store_to(dw[0], dwg, d.K, f.grad_dtype, accumulate);
+    store_to(dw[1], dwu, d.K, f.grad_dtype, accumulate);
+    store_to(dw[2], dwd, d.H, f.grad_dtype, accumulate);
+    launch_gemm<T, true, true, EPI_STORE>(c, dw, 3, w, st);
+    return guard.rc();
+}
+
+__global__ void __launch_bounds__(256) clear_kernel(char *p, size_t bytes) {
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < bytes; i += (size_t)gridDim.x * 256) p[i] = 0;
+}
+
+}  // namespace
+
+extern "C" int ckksmi_gated_ff_workspace_bytes(const ckksmi_ctx *c, const ckksmi_gated_ff *f, int backward, size_t *bytes) {
+    if (!c || !bytes) return CKKSMI_EINVAL;
+    const int rc = check_ff(f);
+    if (rc) return rc;
+    *bytes = workspace_of(*f, backward != 0);
+    return CKKSMI_OK;
+}
+
+extern "C" int ckksmi_gated_ff_saved_bytes(const ckksmi_ctx *c, const ckksmi_gated_ff *f, size_t *bytes) {
+    if (!c || !bytes) return CKKSMI_EINVAL;
+    const int rc = check_ff(f);
+    if (rc) return rc;
+    *bytes = 3 * FF(*f).hidden_bytes();
+    return CKKSMI_OK;
+}
+
+extern "C" int ckksmi_gated_ff_forward(ckksmi_ctx *c, const ckksmi_gated_ff *f, const void *x, const void *wg, const void *wu, const void *wd, void *y, void *saved,
+                                       void *ws, size_t ws_bytes, void *stream) {
+    if (!dev_ok(c)) return CKKSMI_EDEVICE;
+    const int rc = check_ff(f);
+    if (rc) return rc;
+    if (!wg || !wu || !wd) return CKKSMI_EINVAL;
+    if (f->rows == 0) return CKKSMI_OK;
+    const FF d(*f);
+    if (!x || !y || !ws || !aligned(ws, 16) || !aligned(saved, 16)) return CKKSMI_EINVAL;
+    for (const void *p : {x, wg, wu, wd, (const void *)y})
+        if (!aligned(p, d.es)) return CKKSMI_EINVAL;
+    const size_t ldx = ld_bytes(f->ld_x, d.K, d.es), ldy = ld_bytes(f->ld_y, d.O, d.es);
+    const size_t nx = (d.M - 1) * ldx + d.K * d.es, ny = (d.M - 1) * ldy + d.O * d.es, nw = d.H * d.K * d.es, nd = d.O * d.H * d.es, ns = saved ? 3 * d.hidden_bytes() : 0;
+    const void *in[4] = {x, wg, wu, wd};
+    const size_t n_in[4] = {nx, nw, nw, nd};
+    const size_t need = workspace_of(*f, false);
+    for (int i = 0; i < 4; i++)
+        if (overlap(y, ny, in[i], n_in[i]) || overlap(saved, ns, in[i], n_in[i]) || overlap(ws, need, in[i], n_in[i])) return CKKSMI_EINVAL;
+    if (overlap(y, ny, saved, ns) || overlap(ws, need, y, ny) || overlap(ws, need, saved, ns)) return CKKSMI_EINVAL;
+    if (ws_bytes < need) return CKKSMI_EWORKSPACE;
+    const Carve w(ws, ws_bytes);
+    switch (f->dtype) {
+        case CKKSMI_F32: return forward<float>(c, *f, x, wg, wu, wd, y, saved, w, S(stream));
+        case CKKSMI_BF16: return forward<__bf16>(c, *f, x, wg, wu, wd, y, saved, w, S(stream));
+        default: return forward<_Float16>(c, *f, x, wg, wu, wd, y, saved, w, S(stream));
+    }
+}
+
+extern "C" int ckksmi_gated_ff_backward(ckksmi_ctx *c, const ckksmi_gated_ff *f, const void *x, const void *wg, const void *wu, const void *wd, const void *saved,
+                                        const void *dy, void *dx, void *dwg, void *dwu, void *dwd, int accumulate, void *ws, size_t ws_bytes, void *stream) {
+    if (!dev_ok(c)) return CKKSMI_EDEVICE;
+    const int rc = check_ff(f);
+    if (rc) return rc;
+    const FF d(*f);
+    if (!wg || !wu || !wd || !dwg || !dwu || !dwd) return CKKSMI_EINVAL;
+    for (const void *p : {(const void *)dwg, (const void *)dwu, (const void *)dwd})
+        if (!aligned(p, d.ges)) return CKKSMI_EINVAL;
+    const size_t gw = d.H * d.K * d.ges, gd = d.O * d.H * d.ges;
+    if (overlap(dwg, gw, dwu, gw) || overlap(dwg, gw, dwd, gd) || overlap(dwu, gw, dwd, gd)) return CKKSMI_EINVAL;
+    if (f->rows == 0) {  // sums of nothing
+        if (accumulate) return CKKSMI_OK;
+        Guard guard(c);
+        KL(c, CKKSMI_K_GEMM_COPY, 1, clear_kernel, dim3(1024), dim3(256), S(stream), (char *)dwg, gw);
+        KL(c, CKKSMI_K_GEMM_COPY, 1, clear_kernel, dim3(1024), dim3(256), S(stream), (char *)dwu, gw);
+        KL(c, CKKSMI_K_GEMM_COPY, 1, clear_kernel, dim3(1024), dim3(256), S(stream), (char *)dwd, gd);
+        return guard.rc();
+    }
+    if (!x || !dy || !saved || !ws || !aligned(ws, 16) || !aligned(saved, 16)) return CKKSMI_EINVAL;
+    for (const void *p : {x, wg, wu, wd, dy, (const void *)dx})
+        if (!aligned(p, d.es)) return CKKSMI_EINVAL;
+    const size_t nw = d.H * d.K * d.es, nd = d.O * d.H * d.es;
+    auto span = [&](int64_t ld, size_t cols) { return (d.M - 1) * ld_bytes(ld, cols, d.es) + cols * d.es; };
+    const size_t need = workspace_of(*f, true);
+    const void *in[6] = {x, wg, wu, wd, saved, dy};
+    const size_t n_in[6] = {span(f->ld_x, d.K), nw, nw, nd, 3 * d.hidden_bytes(), span(f->ld_dy, d.O)};
+    const void *out[4] = {dx, dwg, dwu, dwd};
+    const size_t n_out[4] = {dx ? span(f->ld_dx, d.K) : 0, gw, gw, gd};
+    for (int o = 0; o < 4; o++) {
+        for (int i = 0; i < 6; i++)
+            if (overlap(out[o], n_out[o], in[i], n_in[i])) return CKKSMI_EINVAL;
+        if (overlap(out[o], n_out[o], ws, need) || (o && overlap(out[0], n_out[0], out[o], n_out[o]))) return CKKSMI_EINVAL;
+    }
+    for (int i = 0; i < 6; i++)
+        if (overlap(ws, need, in[i], n_in[i])) return CKKSMI_EINVAL;
+    if (ws_bytes < need) return CKKSMI_EWORKSPACE;
+    const Carve w(ws, ws_bytes);
+    switch (f->dtype) {
+        case CKKSMI_F32: return backward<float>(c, *f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
+        case CKKSMI_BF16: return backward<__bf16>(c, *f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
+        default: return backward<_Float16>(c, *f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
+    }
+}
+
+// ------------------------------------------------------------------ AdamW
+static int check_tensor(const ckksmi_adamw_tensor &t, size_t p_align, size_t g_align, size_t copy_align, bool bytes) {
+    if (t.n < 0 || t.n >= kMaxNumel) return CKKSMI_EINVAL;
+    if (t.n == 0) return CKKSMI_OK;
+    if (!t.p || !t.grad || !t.m || !t.v || !aligned(t.p, p_align) || !aligned(t.grad, g_align) || !aligned(t.copy, copy_align)) return CKKSMI_EINVAL;
+    if (bytes) return t.m_unit && t.v_unit && aligned(t.m_unit, 4) && aligned(t.v_unit, 4) ? CKKSMI_OK : CKKSMI_EINVAL;
+    return aligned(t.m, 4) && aligned(t.v, 4) ? CKKSMI_OK : CKKSMI_EINVAL;
+}
+
+template <class P, int BITS>
+static void launch_adamw(ckksmi_ctx *c, const AdamwArgs &A, int grad_dtype, unsigned blocks, hipStream_t st) {
+    const double units = (double)blocks * TA_CHUNK;
+    switch (grad_dtype) {
+        case CKKSMI_F32: KL(c, CKKSMI_K_ADAMW, units, (adamw_kernel<P, float, BITS>), dim3(blocks), dim3(256), st, A); break;
+        case CKKSMI_BF16: KL(c, CKKSMI_K_ADAMW, units, (adamw_kernel<P, __bf16, BITS>), dim3(blocks), dim3(256), st, A); break;
+        default: KL(c, CKKSMI_K_ADAMW, units, (adamw_kernel<P, _Float16, BITS>), dim3(blocks), dim3(256), st, A); break;
+    }
+}
+
+extern "C" int ckksmi_adamw_step(ckksmi_ctx *c, const ckksmi_adamw *o, const ckksmi_adamw_tensor *t, int n_tensors, void *stream) {
+    if (!dev_ok(c)) return CKKSMI_EDEVICE;
+    if (!o || n_tensors < 0 || (!t && n_tensors) || !dtype_ok(o->p_dtype) || !dtype_ok(o->grad_dtype) || (o->state_bits != 8 && o->state_bits != 32)) return CKKSMI_EINVAL;
+    if (o->step < 1 || !(o->beta1 >= 0 && o->beta1 < 1) || !(o->beta2 >= 0 && o->beta2 < 1) || !(o->eps >= 0) || !std::isfinite(o->eps) || !std::isfinite(o->lr) ||
+        !std::isfinite(o->weight_decay) || !std::isfinite(o->grad_scale) || !aligned(o->skip, 4))
+        return CKKSMI_EINVAL;
+    bool copies = false;
+    for (int i = 0; i < n_tensors; i++) copies = copies || (t[i].n > 0 && t[i].copy);
+    if (copies && o->copy_dtype != CKKSMI_BF16 && o->copy_dtype != CKKSMI_F16) return CKKSMI_EINVAL;
+    const bool bytes = o->state_bits == 8;
+    for (int i = 0; i < n_tensors; i++) {
+        const int rc = check_tensor(t[i], element_bytes(o->p_dtype), element_bytes(o->grad_dtype), 2, bytes);
+        if (rc) return rc;
+    }
+    AdamwArgs A;
+    memset(&A, 0, sizeof(A));
+    A.copy_f16 = o->copy_dtype == CKKSMI_F16;
+    A.key = adamw_mix(adamw_mix((unsigned)o->seed) + (unsigned)(o->seed >> 32));
+    A.beta1 = (float)o->beta1; A.rest1 = (float)(1.0 - o->beta1);
+    A.beta2 = (float)o->beta2; A.rest2 = (float)(1.0 - o->beta2);
+    A.decay = (float)(1.0 - o->lr * o->weight_decay);
+    A.size = (float)(o->lr / (1.0 - std::pow(o->beta1, (double)o->step)));
+    A.root = (float)(1.0 / std::sqrt(1.0 - std::pow(o->beta2, (double)o->step)));
+    A.eps = (float)o->eps; A.grad_scale = (float)o->grad_scale; A.skip = o->skip;
+    Guard guard(c);
+    for (int i = 0; i < n_tensors;) {
+        // as many tensors as the table holds and a grid may have workgroups (one tensor's always fit: 2^40 elements are 2^28)
+        size_t blocks = 0;
+        A.tensor0 = i;
+        A.n = 0;
+        while (i < n_tensors && A.n < TA_TENSORS) {
+            const size_t more = (size_t)(t[i].n + TA_CHUNK - 1) / TA_CHUNK;
+            if (A.n && blocks + more > 0x7fffffffu) break;
+            A.t[A.n] = t[i];
+            A.first[A.n++] = (unsigned)blocks;
+            blocks += more;
+            i++;
+        }
+        A.first[A.n] = (unsigned)blocks;
+        if (blocks == 0) continue;
+        switch (o->p_dtype * 64 + o->state_bits) {
+            case CKKSMI_F32 * 64 + 32: launch_adamw<float, 32>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
+            case CKKSMI_F32 * 64 + 8: launch_adamw<float, 8>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
+            case CKKSMI_BF16 * 64 + 32: launch_adamw<__bf16, 32>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
+            case CKKSMI_BF16 * 64 + 8: launch_adamw<__bf16, 8>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
+            case CKKSMI_F16 * 64 + 32: launch_adamw<_Float16, 32>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
+            default: launch_adamw<_Float16, 8>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
+        }
+    }
+    return guard.rc();
+}
+
+extern "C" int ckksmi_adamw_read_states(ckksmi_ctx *c, const ckksmi_adamw_tensor *t, int n_tensors, float *const *m_out, float *const *v_out, void *stream) {
+    if (!dev_ok(c)) return CKKSMI_EDEVICE;
+    if (n_tensors < 0 || (!t && n_tensors) || (!m_out && !v_out)) return CKKSMI_EINVAL;
+    for (int i = 0; i < n_tensors; i++) {
+        if (t[i].n < 0 || t[i].n >= kMaxNumel) return CKKSMI_EINVAL;
+        if (t[i].n == 0) continue;
+        if (m_out && (!m_out[i] || !t[i].m || !t[i].m_unit || !aligned(m_out[i], 4) || !aligned(t[i].m_unit, 4))) return CKKSMI_EINVAL;
+        if (v_out && (!v_out[i] || !t[i].v || !t[i].v_unit || !aligned(v_out[i], 4) || !aligned(t[i].v_unit, 4))) return CKKSMI_EINVAL;
+    }
+    ReadStatesArgs A;
+    memset(&A, 0, sizeof(A));
+    Guard guard(c);
+    for (int i = 0; i < n_tensors;) {
+        size_t blocks = 0;
+        A.n = 0;
+        while (i < n_tensors && A.n < TA_TENSORS) {
+            const size_t more = (size_t)(t[i].n + TA_CHUNK - 1) / TA_CHUNK;
+            if (A.n && blocks + more > 0x7fffffffu) break;
+            ReadStatesArgs::One &o = A.t[A.n];
+            o.m = (const unsigned char *)t[i].m; o.v = (const unsigned char *)t[i].v; o.m_unit = t[i].m_unit; o.v_unit = t[i].v_unit;
+            o.m_out = m_out ? m_out[i] : nullptr; o.v_out = v_out ? v_out[i] : nullptr; o.n = t[i].n;
+            A.first[A.n++] = (unsigned)blocks;
+            blocks += more;
+            i++;
+        }
+        if (blocks) KL(c, CKKSMI_K_ADAMW_READ, (double)blocks * TA_CHUNK, adamw_read_kernel, dim3((unsigned)blocks), dim3(256), S(stream), A);
+    }
+    return guard.rc();
+}

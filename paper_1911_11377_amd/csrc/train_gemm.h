@@ -1,0 +1,369 @@
+// Matrix products of the gated feed-forward block on the matrix cores.
+//
+//     C[m][n] = sum over k of A(m, k) * B(n, k)
+//
+// for the block's operand orders.  An operand "along k" has its k indices side by side in memory (x, weights of the forward
+// pass); one "along rows" has its rows side by side (weights of the backward pass, both operands of the weights' gradients).
+//
+// Tiles.  A workgroup computes BM x BN results, 128 bytes of k (64 or 32 indices) a step.  Both operands' tiles go from
+// memory to LDS without registers in between (16 bytes a lane), two stages: while one is multiplied the next is on its way.
+// Lanes whose row, column or k index lies beyond the operand are pointed past the end of the load's descriptor and bring
+// zeros, so no tile needs a case of its own.
+//
+// Lane layout: v_mfma_f32_16x16x32 (16 bits) or four v_mfma_f32_16x16x4 (32 bits) take 16 bytes of each operand a lane:
+// row l % 16, k chunk l / 16.  B is the first operand, so lane l holds the results of A's row l % 16 and of B's rows
+// 4*(l/16) .. +3.  The B rows of two fragments are taken so that a lane's results of both are 8 neighbouring columns.
+//   along k    : LDS row r holds its eight 16-byte chunks at (chunk ^ swizzle(r)); a fragment is one ds_read_b128.
+//   along rows : LDS row k holds the tile's rows; 16-bit fragments are two ds_read_b64_tr_b16 (a group of 16 lanes reads
+//                4 k x 16 rows and gets them transposed), 32-bit ones four ds_read_b32.
+#pragma once
+#include "train_types.h"
+
+#define TG_STEP_BYTES 128   // bytes of k a step
+#define TG_OUTSIDE 0x80000000u  // a lane offset beyond every descriptor's end
+
+enum { EPI_GATE = 0, EPI_STORE = 1, EPI_DHID = 2 };
+
+// What happens to 8 neighbouring results of a row
+struct EpiArgs {
+    void *o0, *o1, *o2;    // GATE: h, g, u (g, u may be null); STORE: the result; DHID: dg, du
+    const void *g, *u;     // DHID
+    size_t ldo;            // elements, all of them
+    int N;                 // columns
+    int f32_out;           // STORE: the result is f32 whatever the operands
+    int accumulate;        // STORE
+    int whole;             // 8 columns may be stored at once: 16-byte aligned rows of at least the next multiple of 8
+    Activation act;
+};
+
+struct GemmProblem {
+    const char *a[2], *b[2];  // sources: STORE may add two products (A0 B0 + A1 B1); GATE has two B's on one A
+    size_t lda, ldb;          // bytes from one row (along k) or one k index (along rows) to the next
+    int M, N, K;
+    int nsrc;
+    int tiles_m, tiles_n;
+    float *part;              // k axis in parts: [splits][values][M][ld_part]
+    size_t ld_part;
+    EpiArgs epi;
+};
+
+#define TG_PROBLEMS 3
+struct GemmArgs {
+    GemmProblem p[TG_PROBLEMS];
+    int first[TG_PROBLEMS + 1];  // tiles of the problems before
+    int n_problems;
+    int splits;                  // parts of the k axis, joined by gemm_join_kernel
+};
+
+template <class T, int EPI>
+__device__ __forceinline__ void epilogue8(const EpiArgs &E, size_t m, int n, const float (&v0)[8], const float (&v1)[8]) {
+    const size_t at = m * E.ldo + n;
+    if constexpr (EPI == EPI_GATE) {
+        float h[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) h[e] = act_value(E.act, v0[e]) * v1[e];
+        store_oct((T *)E.o0 + at, h);
+        if (E.o1) {
+            store_oct((T *)E.o1 + at, v0);
+            store_oct((T *)E.o2 + at, v1);
+        }
+    } else if constexpr (EPI == EPI_DHID) {
+        float g[8], u[8], dg[8], du[8];
+        load_oct((const T *)E.g + at, g);
+        load_oct((const T *)E.u + at, u);
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            float a, da;
+            act_both(E.act, g[e], a, da);
+            dg[e] = v0[e] * u[e] * da;
+            du[e] = v0[e] * a;
+        }
+        store_oct((T *)E.o0 + at, dg);
+        store_oct((T *)E.o1 + at, du);
+    } else {
+        float r[8];
+        if (E.f32_out || sizeof(T) == 4) {
+            float *o = (float *)E.o0 + at;
+            if (E.whole) {
+                if (E.accumulate) load_oct(o, r);
+#pragma unroll
+                for (int e = 0; e < 8; e++) r[e] = E.accumulate ? r[e] + v0[e] : v0[e];
+                store_oct(o, r);
+            } else {
+                for (int e = 0; e < 8; e++)
+                    if (n + e < E.N) o[e] = E.accumulate ? o[e] + v0[e] : v0[e];
+            }
+        } else {
+            T *o = (T *)E.o0 + at;
+            if (E.whole) {
+                if (E.accumulate) load_oct(o, r);
+#pragma unroll
+                for (int e = 0; e < 8; e++) r[e] = E.accumulate ? r[e] + v0[e] : v0[e];
+                store_oct(o, r);
+            } else {
+                for (int e = 0; e < 8; e++)
+                    if (n + e < E.N) o[e] = (T)(E.accumulate ? (float)o[e] + v0[e] : v0[e]);
+            }
+        }
+    }
+}
+
+// ---- operand tiles
+// swizzle of an LDS row's 16-byte chunks, so that the lanes of a fragment read spread over the banks.  Fragment rows:
+// A takes 16 neighbouring rows; B takes rows 8*(i/4) + i%4 (+ 4 for the second fragment of a pair), i = lane % 16
+template <bool IS_B> __device__ __forceinline__ int swizzle_k(int row) {
+    return IS_B ? ((row >> 1) & 1) | ((row >> 3) & 3) << 1 : (row >> 1) & 7;
+}
+template <bool IS_B, int ES, int R> __device__ __forceinline__ int swizzle_rows(int k) {
+    constexpr int chunks = R * ES / 16;  // of an LDS row: the swizzle stays among them
+    const int q = (k >> 2) & 3;
+    if constexpr (ES == 2) return (IS_B ? (k & 3) << 2 : ((k & 3) | ((k >> 3) & 1) << 2) << 1) & (chunks - 1);
+    return (IS_B ? (q & 1) | (q >> 1) << 3 : q << 2) & (chunks - 1);
+}
+
+// Loads of one operand's tiles of R rows: what a lane needs to know, found once
+template <class T, int R, bool ALONG_ROWS, bool IS_B, int WAVES, bool TWO>
+struct TileLoad {
+    static constexpr int ES = sizeof(T), EPC = 16 / ES, KSTEP = TG_STEP_BYTES / ES;
+    static constexpr int BYTES = R * TG_STEP_BYTES;
+    static constexpr int NI = BYTES / 1024 / WAVES;  // load instructions of a wave
+    static_assert(NI * WAVES * 1024 == BYTES, "whole instructions");
+    unsigned off[NI];  // byte offset of the lane's 16 bytes from the tile's first
+    int kc[NI];        // their (first) k index within the step
+
+    __device__ __forceinline__ void init(int wave, int lane, size_t ld, int rows_left) {
+#pragma unroll
+        for (int it = 0; it < NI; it++) {
+            const int s = it * WAVES + wave;
+            if constexpr (!ALONG_ROWS) {
+                const int row = s * 8 + (lane >> 3), c = (lane & 7) ^ swizzle_k<IS_B>(row);
+                const int mem_row = TWO && row >= R / 2 ? row - R / 2 : row;
+                off[it] = mem_row < rows_left ? (unsigned)(mem_row * ld + c * 16) : TG_OUTSIDE;
+                kc[it] = c * EPC;
+            } else {
+                constexpr int LPR = R * ES / 16, KPI = 64 / LPR;
+                const int k = s * KPI + lane / LPR, c = (lane % LPR) ^ swizzle_rows<IS_B, ES, R>(k);
+                off[it] = c * EPC < rows_left ? (unsigned)(k * ld + c * 16) : TG_OUTSIDE;
+                kc[it] = k;
+            }
+        }
+    }
+    // the tile whose k indices begin at k0 of K; base: the operand at the tile's first row (TWO: both operands')
+    __device__ __forceinline__ void issue(char *lds, int wave, const char *base0, const char *base1, size_t ld, int k0, int K) const {
+        const size_t skip = ALONG_ROWS ? (size_t)k0 * ld : (size_t)k0 * ES;
+        const __amdgpu_buffer_rsrc_t r0 = __builtin_amdgcn_make_buffer_rsrc((void *)(base0 + skip), 0, 0x7ffffff0, 0x00027000);
+        const __amdgpu_buffer_rsrc_t r1 = __builtin_amdgcn_make_buffer_rsrc((void *)((TWO ? base1 : base0) + skip), 0, 0x7ffffff0, 0x00027000);
+        const bool tail = k0 + KSTEP > K;
+#pragma unroll
+        for (int it = 0; it < NI; it++) {
+            unsigned o = off[it];
+            if (tail && k0 + kc[it] >= K) o = TG_OUTSIDE;
+            char *d = lds + (it * WAVES + wave) * 1024;
+            if (TWO && it >= NI / 2)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r1, (__attribute__((address_space(3))) void *)d, 16, o, 0, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r0, (__attribute__((address_space(3))) void *)d, 16, o, 0, 0, 0);
+        }
+    }
+    // 16 bytes of a lane: sub-step kk (0: the first half of the step's k indices, 1: the second) of the fragment whose first row is `row0`;
+    // IS_B: of the pair's fragment `half`
+    static __device__ __forceinline__ u32x4 fragment(const char *lds, int row0, int half, int kk, int lane) {
+        const int i = lane & 15, q = lane >> 4;
+        u32x4 f;
+        if constexpr (!ALONG_ROWS) {
+            const int row = IS_B ? row0 + 8 * (i >> 2) + 4 * half + (i & 3) : row0 + i;
+            f = *(const u32x4 *)(lds + row * TG_STEP_BYTES + (((4 * kk + q) ^ swizzle_k<IS_B>(row)) << 4));
+        } else if constexpr (ES == 2) {
+            // the lane's address: k index i / 4 of the group's four, rows 4*(i % 4) .. +3 of the fragment's sixteen
+            const int a = i & 3, row = IS_B ? row0 + 8 * a + 4 * half : row0 + 4 * a;
+            s16x4 h[2];
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const int k = 32 * kk + 8 * q + 4 * j + (i >> 2);
+                const char *p = lds + k * (R * ES) + (((row >> 3) ^ swizzle_rows<IS_B, ES, R>(k)) << 4) + (row & 4) * 2;
+                h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
+            }
+            __builtin_memcpy(&f, h, 16);
+        } else {
+            const int row = IS_B ? row0 + 8 * (i >> 2) + 4 * half + (i & 3) : row0 + i;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int k = 16 * kk + 4 * q + j;
+                f[j] = *(const unsigned *)(lds + k * (R * ES) + (((row >> 2) ^ swizzle_rows<IS_B, ES, R>(k)) << 4) + (row & 3) * 4);
+            }
+        }
+        return f;
+    }
+};
+
+template <class T> __device__ __forceinline__ f32x4 mma(const u32x4 &first, const u32x4 &second, f32x4 c) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(first[j]), __uint_as_float(second[j]), c, 0, 0, 0);
+        return c;
+    } else if constexpr (__is_same(T, __bf16)) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, first), __builtin_bit_cast(bf16x8, second), c, 0, 0, 0);
+    } else {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, first), __builtin_bit_cast(f16x8, second), c, 0, 0, 0);
+    }
+}
+
+// Tiles in the order in which their operands are shared: workgroups reach the 8 XCDs in turn, so each XCD takes a run of
+// neighbouring tiles, and runs go down 8 tile rows before they move to the next tile column
+__device__ __forceinline__ int xcd_order(int wg, int total) {
+    const int per = total / 8, rest = total % 8, x = wg % 8, i = wg / 8;
+    return x * per + (x < rest ? x : rest) + i;
+}
+
+template <class T, int BM, int BN, int WM, int WN, bool A_ROWS, bool B_ROWS, int EPI>
+__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN)) gemm_kernel(GemmArgs G) {
+    constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32;
+    constexpr bool GATE = EPI == EPI_GATE;
+    typedef TileLoad<T, BM, A_ROWS, false, WAVES, false> LA;
+    typedef TileLoad<T, BN, B_ROWS, true, WAVES, GATE> LB;
+    __shared__ __attribute__((aligned(1024))) char stage0[LA::BYTES + LB::BYTES];
+    __shared__ __attribute__((aligned(1024))) char stage1[LA::BYTES + LB::BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN);
+
+    int tile = xcd_order(blockIdx.x, gridDim.x), pi = 0;
+    while (pi + 1 < G.n_problems && tile >= G.first[pi + 1]) pi++;
+    tile -= G.first[pi];
+    const GemmProblem &P = G.p[pi];
+    constexpr int GROUP = 8;
+    const int band = tile / (GROUP * P.tiles_n), in_band = tile % (GROUP * P.tiles_n);
+    const int band_rows = min(GROUP, P.tiles_m - band * GROUP);
+    const int tm = band * GROUP + in_band % band_rows, tn = in_band / band_rows;
+    constexpr int COLS = GATE ? BN / 2 : BN;  // results' columns of a tile
+    const int m0 = tm * BM, n0 = tn * COLS;
+
+    LA la;
+    LB lb;
+    la.init(wave, lane, P.lda, P.M - m0);
+    lb.init(wave, lane, P.ldb, P.N - n0);
+    const size_t a_skip = A_ROWS ? (size_t)m0 * sizeof(T) : (size_t)m0 * P.lda;
+    const size_t b_skip = B_ROWS ? (size_t)n0 * sizeof(T) : (size_t)n0 * P.ldb;
+
+    const int per_src = (P.K + LA::KSTEP - 1) / LA::KSTEP, steps = per_src * P.nsrc;
+    const int s0 = (int)((long long)steps * blockIdx.y / G.splits), s1 = (int)((long long)steps * (blockIdx.y + 1) / G.splits);
+
+    auto issue = [&](char *st, int s) {
+        const bool second = s >= per_src;
+        const int k0 = (second ? s - per_src : s) * LA::KSTEP;
+        la.issue(st, wave, (second ? P.a[1] : P.a[0]) + a_skip, nullptr, P.lda, k0, P.K);
+        lb.issue(st + LA::BYTES, wave, (second ? P.b[1] : P.b[0]) + b_skip, GATE ? P.b[1] + b_skip : nullptr, P.ldb, k0, P.K);
+    };
+    f32x4 acc[FM][2 * PAIRS];
+#pragma unroll
+    for (int i = 0; i < FM; i++)
+#pragma unroll
+        for (int j = 0; j < 2 * PAIRS; j++) acc[i][j] = f32x4{0, 0, 0, 0};
+    auto multiply = [&](const char *st) {
+#pragma unroll
+        for (int kk = 0; kk < 2; kk++) {
+            u32x4 b[2 * PAIRS];
+#pragma unroll
+            for (int p = 0; p < PAIRS; p++) {
+                // GATE: pair 0 is of the gate's weights, pair 1 of the other's
+                const int row0 = GATE ? p * (BN / 2) + wn * 32 : wn * WN + 32 * p;
+                b[2 * p] = LB::fragment(st + LA::BYTES, row0, 0, kk, lane);
+                b[2 * p + 1] = LB::fragment(st + LA::BYTES, row0, 1, kk, lane);
+            }
+#pragma unroll
+            for (int i = 0; i < FM; i++) {
+                const u32x4 a = LA::fragment(st, wm + 16 * i, 0, kk, lane);
+#pragma unroll
+                for (int j = 0; j < 2 * PAIRS; j++) acc[i][j] = mma<T>(b[j], a, acc[i][j]);
+            }
+        }
+    };
+    static_assert(!GATE || WN == 64, "a wave holds 32 columns of both products");
+
+    if (s0 < s1) issue(stage0, s0);
+    for (int s = s0; s < s1; s += 2) {
+        __syncthreads();  // stage0 has arrived, stage1 is no longer read
+        if (s + 1 < s1) issue(stage1, s + 1);
+        multiply(stage0);
+        if (s + 1 < s1) {
+            __syncthreads();
+            if (s + 2 < s1) issue(stage0, s + 2);
+            multiply(stage1);
+        }
+    }
+
+    const int i = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int f = 0; f < FM; f++) {
+        const int m = m0 + wm + 16 * f + i;
+        if (m >= P.M) continue;
+        auto eight = [&](int p, float (&v)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] = acc[f][2 * p + e / 4][e % 4];
+        };
+        float v0[8], v1[8];
+        if constexpr (GATE) {
+            const int n = n0 + wn * 32 + 8 * q;
+            if (n >= P.N) continue;
+            eight(0, v0);
+            eight(1, v1);
+            if (G.splits > 1) {
+                float *o = P.part + ((size_t)blockIdx.y * 2 * P.M + m) * P.ld_part + n;
+                store_oct(o, v0);
+                store_oct(o + (size_t)P.M * P.ld_part, v1);
+            } else
+                epilogue8<T, EPI>(P.epi, m, n, v0, v1);
+        } else {
+#pragma unroll
+            for (int p = 0; p < PAIRS; p++) {
+                const int n = n0 + wn * WN + 32 * p + 8 * q;
+                if (n >= P.N) continue;
+                eight(p, v0);
+                if (G.splits > 1) store_oct(P.part + ((size_t)blockIdx.y * P.M + m) * P.ld_part + n, v0);
+                else epilogue8<T, EPI>(P.epi, m, n, v0, v0);
+            }
+        }
+    }
+}
+
+// Sum of the parts of a split k axis, always in the same order, and the epilogue
+template <class T, int EPI>
+__global__ void __launch_bounds__(256) gemm_join_kernel(GemmArgs G) {
+    constexpr int VALUES = EPI == EPI_GATE ? 2 : 1;
+    const GemmProblem &P = G.p[blockIdx.y];
+    const size_t octs = P.ld_part / 8, id = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= octs * P.M) return;
+    const size_t m = id / octs;
+    const int n = (int)(id % octs) * 8;
+    float v[2][8] = {};
+    for (int s = 0; s < G.splits; s++)
+#pragma unroll
+        for (int w = 0; w < VALUES; w++) {
+            float x[8];
+            load_oct(P.part + (((size_t)s * VALUES + w) * P.M + m) * P.ld_part + n, x);
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[w][e] = s ? v[w][e] + x[e] : x[e];
+        }
+    epilogue8<T, EPI>(P.epi, m, n, v[0], v[1]);
+}
+
+// Copies with rows padded to whole 16-byte chunks (zeros behind the last column), for operands whose rows do not begin on them
+#define TG_COPIES 6
+struct CopyArgs {
+    struct One { const char *src; char *dst; size_t ld_src, ld_dst; int cols, chunks; size_t rows; unsigned first; } c[TG_COPIES];
+    int n;
+};
+template <class T> __global__ void __launch_bounds__(256) pad_rows_kernel(CopyArgs A) {
+    int i = 0;
+    while (i + 1 < A.n && blockIdx.x >= A.c[i + 1].first) i++;
+    const CopyArgs::One &C = A.c[i];
+    constexpr int EPC = 16 / sizeof(T);
+    const size_t id = (size_t)(blockIdx.x - C.first) * 256 + threadIdx.x;
+    if (id >= C.rows * C.chunks) return;
+    const size_t r = id / C.chunks;
+    const int c = (int)(id % C.chunks) * EPC;
+    const T *s = (const T *)(C.src + r * C.ld_src) + c;
+    T v[EPC];
+#pragma unroll
+    for (int e = 0; e < EPC; e++) v[e] = c + e < C.cols ? s[e] : (T)0.0f;
+    *(u32x4 *)(C.dst + r * C.ld_dst + (size_t)c * sizeof(T)) = *(const u32x4 *)v;
+}

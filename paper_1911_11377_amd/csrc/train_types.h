@@ -1,0 +1,80 @@
+// Element types, activations and small helpers of the cleartext training kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/ckksmi_train.h"
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+template <int DT> struct ElementOf;
+template <> struct ElementOf<CKKSMI_F32> { typedef float type; };
+template <> struct ElementOf<CKKSMI_BF16> { typedef __bf16 type; };
+template <> struct ElementOf<CKKSMI_F16> { typedef _Float16 type; };
+template <int DT> using element = typename ElementOf<DT>::type;
+
+inline size_t element_bytes(int dtype) { return dtype == CKKSMI_F32 ? 4 : 2; }
+
+// 8 consecutive elements, 16-byte aligned
+template <class T> struct Oct { T v[8]; };
+template <class T> __device__ __forceinline__ void load_oct(const T *p, float (&x)[8]) {
+    Oct<T> o;
+    u32x4 *w = (u32x4 *)&o;
+    const u32x4 *s = (const u32x4 *)p;
+    w[0] = s[0];
+    if constexpr (sizeof(T) == 4) w[1] = s[1];
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = (float)o.v[e];
+}
+template <class T> __device__ __forceinline__ void store_oct(T *p, const float (&x)[8]) {
+    Oct<T> o;
+#pragma unroll
+    for (int e = 0; e < 8; e++) o.v[e] = (T)x[e];
+    const u32x4 *w = (const u32x4 *)&o;
+    u32x4 *d = (u32x4 *)p;
+    d[0] = w[0];
+    if constexpr (sizeof(T) == 4) d[1] = w[1];
+}
+
+struct Activation { int kind; float c[4]; };
+
+// act(g) in 32 bits
+__device__ __forceinline__ float act_value(const Activation &A, float g) {
+    switch (A.kind) {
+        case CKKSMI_ACT_POLY: return ((A.c[3] * g + A.c[2]) * g + A.c[1]) * g + A.c[0];
+        case CKKSMI_ACT_RELU: return g > 0.0f ? g : g * 0.0f;  // a NaN stays one
+        case CKKSMI_ACT_SILU: return g / (1.0f + expf(-g));
+        default: return g * (0.5f * (1.0f + erff(g * 0.70710678f)));
+    }
+}
+// act(g) and its derivative
+__device__ __forceinline__ void act_both(const Activation &A, float g, float &a, float &da) {
+    switch (A.kind) {
+        case CKKSMI_ACT_POLY:
+            a = ((A.c[3] * g + A.c[2]) * g + A.c[1]) * g + A.c[0];
+            da = (3.0f * A.c[3] * g + 2.0f * A.c[2]) * g + A.c[1];
+            return;
+        case CKKSMI_ACT_RELU:
+            a = g > 0.0f ? g : g * 0.0f;
+            da = g > 0.0f ? 1.0f : 0.0f;
+            return;
+        case CKKSMI_ACT_SILU: {
+            const float q = 1.0f / (1.0f + expf(-g));
+            a = g * q;
+            da = q * (1.0f + g * (1.0f - q));
+            return;
+        }
+        default: {
+            const float q = 0.5f * (1.0f + erff(g * 0.70710678f));
+            a = g * q;
+            da = q + g * expf(-0.5f * g * g) * 0.39894228f;
+            return;
+        }
+    }
+}
