@@ -34,7 +34,7 @@ extern "C" {
 /* Gated feed-forward block on `rows` rows:
  *     g = x Wg^T,  u = x Wu^T,  h = act(g) * u,  y = h Wd^T
  * x: [rows][d_in], Wg, Wu: [d_hidden][d_in], Wd: [d_out][d_hidden], y: [rows][d_out].  Elements are of `dtype`; sums,
- * activations and their derivatives are formed in 32 bits, and g, u, h are rounded to `dtype` where they are stored.
+ * activations and their derivatives are formed in 32 bits, and h is rounded to `dtype` before the last product.
  * Weights are dense; rows of x, y, dy, dx may lie further apart: ld_* elements, 0 = dense.  0 <= rows < 2^31, every
  * dimension and ld 1 .. 2^20. */
 typedef struct {
@@ -46,8 +46,8 @@ typedef struct {
     int64_t ld_x, ld_y, ld_dy, ld_dx;
 } ckksmi_gated_ff;
 
-/* bytes of workspace of the forward (backward = 0) or of either pass (backward = 1); of the activations that a forward
- * pass saves for the backward pass (g, u and h, in an order of their own) */
+/* bytes of workspace of the forward (backward = 0) or of either pass (backward = 1); of what a forward pass saves for the
+ * backward pass: act(g), u act'(g) and h, 8 bytes per row and hidden unit for 16-bit types (with f32 gradients 12 for f16, 14 for bf16), 12 for f32 */
 int ckksmi_gated_ff_workspace_bytes(const ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, int backward, size_t *bytes);
 int ckksmi_gated_ff_saved_bytes(const ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, size_t *bytes);
 /* saved: NULL (nothing is kept: answering requests) or a buffer for the backward pass.  y must not overlap an input. */
@@ -56,8 +56,9 @@ int ckksmi_gated_ff_forward(ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, const vo
 /* Gradients from dy [rows][d_out]: with dh = dy Wd,  dg = dh * u * act'(g),  du = dh * act(g),
  *     dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x,  dWd = dy^T h.
  * saved: what the forward pass on the same x and weights left.  dx may be NULL (a first layer needs none).  accumulate != 0: the weights'
- * gradients are added to what the buffers hold.  dg and du are rounded to `dtype` between the products.  Outputs must not
- * overlap inputs.  The sums' order depends on the sizes alone: equal calls give equal bits. */
+ * gradients are added to what the buffers hold.  dg and du are rounded to `dtype` between the products; where the gradients are
+ * f32 and `dtype` is not, they and h enter the weights' gradients as sums of two (f16) or three (bf16) values of `dtype`, at as
+ * many times these products' cost, and the gradients are as good as f32 operands' would be.  Outputs must not overlap inputs.  The sums' order depends on the sizes alone: equal calls give equal bits. */
 int ckksmi_gated_ff_backward(ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, const void *x, const void *w_gate, const void *w_up, const void *w_down,
                              const void *saved, const void *dy, void *dx, void *dw_gate, void *dw_up, void *dw_down, int accumulate,
                              void *ws, size_t ws_bytes, void *stream);

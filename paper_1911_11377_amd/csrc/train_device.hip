@@ -59,6 +59,19 @@ struct FF {  // a call's sizes
     explicit FF(const ckksmi_gated_ff &f)
         : es(element_bytes(f.dtype)), ges(element_bytes(f.grad_dtype)), M((size_t)f.rows), K((size_t)f.d_in), H((size_t)f.d_hidden), O((size_t)f.d_out), ldh(round_up(H, 8)) {}
     size_t hidden_bytes() const { return round_up(M * ldh * es, 256); }
+    bool fine() const { return es == 2 && ges == 4; }  // f32 gradients of 16-bit operands
+    // 16-bit values whose sum h, dg and du enter the weights' gradients as: 24 bits of bf16, 22 of f16
+    int parts(int dtype) const { return !fine() ? 1 : dtype == CKKSMI_BF16 ? 3 : 2; }
+    // what a forward pass saves: act(g), u act'(g) (4 bytes, or 2 + 1), h in its parts
+    size_t kept_bytes() const { return fine() ? round_up(M * ldh * 4, 256) : hidden_bytes(); }
+    size_t low_bytes() const { return es == 2 && !fine() ? round_up(M * ldh, 256) : 0; }
+    size_t saved_bytes(int dtype) const { return 2 * kept_bytes() + 2 * low_bytes() + parts(dtype) * hidden_bytes(); }
+    Kept kept(const void *saved) const {
+        char *p = (char *)saved;
+        uint8_t *low = (uint8_t *)p + 2 * kept_bytes();
+        return low_bytes() ? Kept{p, p + kept_bytes(), low, low + low_bytes()} : Kept{p, p + kept_bytes(), nullptr, nullptr};
+    }
+    char *saved_h(const void *saved) const { return (char *)saved + 2 * kept_bytes() + 2 * low_bytes(); }
 };
 inline size_t ld_bytes(int64_t ld, size_t cols, size_t es) { return (ld ? (size_t)ld : cols) * es; }
 
@@ -181,6 +194,7 @@ size_t split_bytes(const ckksmi_gated_ff &f, bool backward) {
     dx.nsrc = 2;
     most = std::max(most, std::max(one(product(none, none, d.M, d.H, d.O), false), one(dx, false)));
     GemmProblem dw[3] = {product(none, none, d.H, d.K, d.M), product(none, none, d.H, d.K, d.M), product(none, none, d.O, d.H, d.M)};
+    for (GemmProblem &p : dw) p.nsrc = d.parts(f.dtype);
     const int splits = choose(dw, 3, false, d.es).splits;
     return std::max(most, part_bytes(dw[0], splits, false) * 2 + part_bytes(dw[2], splits, false) + 768);
 }
@@ -190,7 +204,7 @@ size_t workspace_of(const ckksmi_gated_ff &f, bool backward) {
     auto rows = [&](size_t r, size_t cols) { return round_up(r * round_up(cols * d.es, 16), 256); };
     const size_t weights = 2 * rows(d.H, d.K) + rows(d.O, d.H);
     const size_t forward = rows(d.M, d.K) + weights + d.hidden_bytes();
-    const size_t back = rows(d.M, d.K) + weights + rows(d.M, d.O) + 2 * d.hidden_bytes();
+    const size_t back = rows(d.M, d.K) + weights + rows(d.M, d.O) + 2 * d.parts(f.dtype) * d.hidden_bytes();
     return (backward ? std::max(forward, back) : forward) + split_bytes(f, backward);
 }
 
@@ -203,12 +217,15 @@ int forward(ckksmi_ctx *c, const ckksmi_gated_ff &f, const void *x, const void *
     const Matrix md = ops.use(wd, d.H * d.es, d.O, d.H, w);
     char *h = w.take(d.hidden_bytes());
     char *const keep = (char *)saved;
-    if (keep) h = keep + 2 * d.hidden_bytes();
+    if (keep) h = d.saved_h(keep);
     ops.run(c, st);
 
     GemmProblem gate = product(mx, mg, d.M, d.H, d.K);
     gate.b[1] = mu.p;
-    gate.epi.o0 = h; gate.epi.o1 = keep; gate.epi.o2 = keep ? keep + d.hidden_bytes() : nullptr;
+    gate.epi.o0 = h;
+    if (keep) gate.epi.kept = d.kept(keep);
+    gate.epi.parts = keep ? d.parts(f.dtype) : 1;
+    gate.epi.part_bytes = d.hidden_bytes();
     gate.epi.ldo = d.ldh; gate.epi.N = (int)d.H; gate.epi.act = activation_of(f);
     launch_gemm<T, false, false, EPI_GATE>(c, &gate, 1, w, st);
 
@@ -226,14 +243,15 @@ int backward(ckksmi_ctx *c, const ckksmi_gated_ff &f, const void *x, const void 
     Operands<T> ops;
     const Matrix mx = ops.use(x, ld_bytes(f.ld_x, d.K, d.es), d.M, d.K, w), mg = ops.use(wg, d.K * d.es, d.H, d.K, w), mu = ops.use(wu, d.K * d.es, d.H, d.K, w);
     const Matrix md = ops.use(wd, d.H * d.es, d.O, d.H, w), mdy = ops.use(dy, ld_bytes(f.ld_dy, d.O, d.es), d.M, d.O, w);
-    char *dg = w.take(d.hidden_bytes()), *du = w.take(d.hidden_bytes());
-    const char *g = (const char *)saved, *u = g + d.hidden_bytes(), *h = u + d.hidden_bytes();
+    const int parts = d.parts(f.dtype);
+    char *dg = w.take(parts * d.hidden_bytes()), *du = w.take(parts * d.hidden_bytes());
+    const char *h = d.saved_h(saved);
     const size_t ldh = d.ldh * d.es;
     ops.run(c, st);
 
     GemmProblem dh = product(mdy, md, d.M, d.H, d.O);
-    dh.epi.o0 = dg; dh.epi.o1 = du; dh.epi.g = g; dh.epi.u = u;
-    dh.epi.ldo = d.ldh; dh.epi.N = (int)d.H; dh.epi.act = activation_of(f);
+    dh.epi.o0 = dg; dh.epi.o1 = du; dh.epi.parts = parts; dh.epi.part_bytes = d.hidden_bytes(); dh.epi.kept = d.kept(saved);
+    dh.epi.ldo = d.ldh; dh.epi.N = (int)d.H;
     launch_gemm<T, false, true, EPI_DHID>(c, &dh, 1, w, st);
 
     if (dx) {
@@ -243,6 +261,12 @@ int backward(ckksmi_ctx *c, const ckksmi_gated_ff &f, const void *x, const void 
         launch_gemm<T, false, true, EPI_STORE>(c, &p, 1, w, st);
     }
     GemmProblem dw[3] = {product(Matrix{dg, ldh}, mx, d.H, d.K, d.M), product(Matrix{du, ldh}, mx, d.H, d.K, d.M), product(mdy, Matrix{h, ldh}, d.O, d.H, d.M)};
+    for (GemmProblem &p : dw) p.nsrc = parts;
+    for (int i = 1; i < parts; i++) {
+        const size_t at = i * d.hidden_bytes();
+        dw[0].a[i] = dg + at; dw[1].a[i] = du + at; dw[2].a[i] = mdy.p;
+        dw[0].b[i] = mx.p; dw[1].b[i] = mx.p; dw[2].b[i] = h + at;
+    }
     store_to(dw[0], dwg, d.K, f.grad_dtype, accumulate);
     store_to(dw[1], dwu, d.K, f.grad_dtype, accumulate);
     store_to(dw[2], dwd, d.H, f.grad_dtype, accumulate);
@@ -268,7 +292,7 @@ extern "C" int ckksmi_gated_ff_saved_bytes(const ckksmi_ctx *c, const ckksmi_gat
     if (!c || !bytes) return CKKSMI_EINVAL;
     const int rc = check_ff(f);
     if (rc) return rc;
-    *bytes = 3 * FF(*f).hidden_bytes();
+    *bytes = FF(*f).saved_bytes(f->dtype);
     return CKKSMI_OK;
 }
 
@@ -284,7 +308,7 @@ extern "C" int ckksmi_gated_ff_forward(ckksmi_ctx *c, const ckksmi_gated_ff *f, 
     for (const void *p : {x, wg, wu, wd, (const void *)y})
         if (!aligned(p, d.es)) return CKKSMI_EINVAL;
     const size_t ldx = ld_bytes(f->ld_x, d.K, d.es), ldy = ld_bytes(f->ld_y, d.O, d.es);
-    const size_t nx = (d.M - 1) * ldx + d.K * d.es, ny = (d.M - 1) * ldy + d.O * d.es, nw = d.H * d.K * d.es, nd = d.O * d.H * d.es, ns = saved ? 3 * d.hidden_bytes() : 0;
+    const size_t nx = (d.M - 1) * ldx + d.K * d.es, ny = (d.M - 1) * ldy + d.O * d.es, nw = d.H * d.K * d.es, nd = d.O * d.H * d.es, ns = saved ? d.saved_bytes(f->dtype) : 0;
     const void *in[4] = {x, wg, wu, wd};
     const size_t n_in[4] = {nx, nw, nw, nd};
     const size_t need = workspace_of(*f, false);
@@ -326,7 +350,7 @@ extern "C" int ckksmi_gated_ff_backward(ckksmi_ctx *c, const ckksmi_gated_ff *f,
     auto span = [&](int64_t ld, size_t cols) { return (d.M - 1) * ld_bytes(ld, cols, d.es) + cols * d.es; };
     const size_t need = workspace_of(*f, true);
     const void *in[6] = {x, wg, wu, wd, saved, dy};
-    const size_t n_in[6] = {span(f->ld_x, d.K), nw, nw, nd, 3 * d.hidden_bytes(), span(f->ld_dy, d.O)};
+    const size_t n_in[6] = {span(f->ld_x, d.K), nw, nw, nd, d.saved_bytes(f->dtype), span(f->ld_dy, d.O)};
     const void *out[4] = {dx, dwg, dwu, dwd};
     const size_t n_out[4] = {dx ? span(f->ld_dx, d.K) : 0, gw, gw, gd};
     for (int o = 0; o < 4; o++) {

@@ -24,10 +24,20 @@
 
 enum { EPI_GATE = 0, EPI_STORE = 1, EPI_DHID = 2 };
 
+// What the forward pass saves and the backward pass reads: act(g) and u act'(g), in 32 bits where the weights' gradients are f32.
+// 16-bit gradients need them in 24 bits only: their roundings to 16 bits are then dg's, du's and h's own and no others
+// (kept in 16 bits, act(g) and u act'(g) would add as much again)
+struct Kept {
+    char *a, *da;            // upper 16 bits, or the values
+    uint8_t *a_low, *da_low; // 8 bits below; null: 32 bits are kept
+};
+
 // What happens to 8 neighbouring results of a row
 struct EpiArgs {
-    void *o0, *o1, *o2;    // GATE: h, g, u (g, u may be null); STORE: the result; DHID: dg, du
-    const void *g, *u;     // DHID
+    void *o0, *o1;         // GATE: h; STORE: the result; DHID: dg, du
+    int parts;             // GATE, DHID: 16-bit values that o0 and o1 are written as the sum of
+    size_t part_bytes;     // from one of them to the next
+    Kept kept;             // GATE: to be written (a null: nothing is kept); DHID: to be read
     size_t ldo;            // elements, all of them
     int N;                 // columns
     int f32_out;           // STORE: the result is f32 whatever the operands
@@ -36,8 +46,9 @@ struct EpiArgs {
     Activation act;
 };
 
+#define TG_SOURCES 3
 struct GemmProblem {
-    const char *a[2], *b[2];  // sources: STORE may add two products (A0 B0 + A1 B1); GATE has two B's on one A
+    const char *a[TG_SOURCES], *b[TG_SOURCES];  // STORE adds nsrc products, A0 B0 + A1 B1 + ..; GATE has two B's on one A
     size_t lda, ldb;          // bytes from one row (along k) or one k index (along rows) to the next
     int M, N, K;
     int nsrc;
@@ -55,31 +66,60 @@ struct GemmArgs {
     int splits;                  // parts of the k axis, joined by gemm_join_kernel
 };
 
+// x rounded to T; more parts: what that left, rounded likewise, and so on
+template <class T> __device__ __forceinline__ void store_parts(const EpiArgs &E, void *o, size_t at, const float (&x)[8]) {
+    store_oct((T *)o + at, x);
+    if constexpr (sizeof(T) == 2) {
+        float r[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) r[e] = x[e];
+        for (int p = 1; p < E.parts; p++) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) r[e] -= (float)(T)r[e];
+            store_oct((T *)((char *)o + p * E.part_bytes) + at, r);
+        }
+    }
+}
+template <class T> __device__ __forceinline__ void store_kept(char *p, uint8_t *low, size_t at, const float (&x)[8]) {
+    if (sizeof(T) == 4 || !low) store_oct((float *)p + at, x);
+    else store_oct24((uint16_t *)p + at, low + at, x);
+}
+template <class T> __device__ __forceinline__ void load_kept(const char *p, const uint8_t *low, size_t at, float (&x)[8]) {
+    if (sizeof(T) == 4 || !low) load_oct((const float *)p + at, x);
+    else load_oct24((const uint16_t *)p + at, low + at, x);
+}
+
 template <class T, int EPI>
 __device__ __forceinline__ void epilogue8(const EpiArgs &E, size_t m, int n, const float (&v0)[8], const float (&v1)[8]) {
     const size_t at = m * E.ldo + n;
     if constexpr (EPI == EPI_GATE) {
         float h[8];
+        if (E.kept.a) {
+            float a[8], da[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) h[e] = act_value(E.act, v0[e]) * v1[e];
-        store_oct((T *)E.o0 + at, h);
-        if (E.o1) {
-            store_oct((T *)E.o1 + at, v0);
-            store_oct((T *)E.o2 + at, v1);
+            for (int e = 0; e < 8; e++) {
+                act_both(E.act, v0[e], a[e], da[e]);
+                da[e] *= v1[e];
+                h[e] = a[e] * v1[e];
+            }
+            store_kept<T>(E.kept.a, E.kept.a_low, at, a);
+            store_kept<T>(E.kept.da, E.kept.da_low, at, da);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++) h[e] = act_value(E.act, v0[e]) * v1[e];
         }
+        store_parts<T>(E, E.o0, at, h);
     } else if constexpr (EPI == EPI_DHID) {
-        float g[8], u[8], dg[8], du[8];
-        load_oct((const T *)E.g + at, g);
-        load_oct((const T *)E.u + at, u);
+        float a[8], da[8];
+        load_kept<T>(E.kept.a, E.kept.a_low, at, a);
+        load_kept<T>(E.kept.da, E.kept.da_low, at, da);
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            float a, da;
-            act_both(E.act, g[e], a, da);
-            dg[e] = v0[e] * u[e] * da;
-            du[e] = v0[e] * a;
+            da[e] *= v0[e];
+            a[e] *= v0[e];
         }
-        store_oct((T *)E.o0 + at, dg);
-        store_oct((T *)E.o1 + at, du);
+        store_parts<T>(E, E.o0, at, da);
+        store_parts<T>(E, E.o1, at, a);
     } else {
         float r[8];
         if (E.f32_out || sizeof(T) == 4) {
@@ -248,10 +288,16 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN)) gemm_kernel(GemmAr
     const int s0 = (int)((long long)steps * blockIdx.y / G.splits), s1 = (int)((long long)steps * (blockIdx.y + 1) / G.splits);
 
     auto issue = [&](char *st, int s) {
-        const bool second = s >= per_src;
-        const int k0 = (second ? s - per_src : s) * LA::KSTEP;
-        la.issue(st, wave, (second ? P.a[1] : P.a[0]) + a_skip, nullptr, P.lda, k0, P.K);
-        lb.issue(st + LA::BYTES, wave, (second ? P.b[1] : P.b[0]) + b_skip, GATE ? P.b[1] + b_skip : nullptr, P.ldb, k0, P.K);
+        const char *a = P.a[0], *b = P.b[0];
+        if constexpr (EPI == EPI_STORE)
+            for (int i = 1; i < P.nsrc && s >= per_src; i++) {
+                s -= per_src;
+                a = P.a[i];
+                b = P.b[i];
+            }
+        const int k0 = s * LA::KSTEP;
+        la.issue(st, wave, a + a_skip, nullptr, P.lda, k0, P.K);
+        lb.issue(st + LA::BYTES, wave, b + b_skip, GATE ? P.b[1] + b_skip : nullptr, P.ldb, k0, P.K);
     };
     f32x4 acc[FM][2 * PAIRS];
 #pragma unroll

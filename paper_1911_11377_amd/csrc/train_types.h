@@ -42,6 +42,30 @@ template <class T> __device__ __forceinline__ void store_oct(T *p, const float (
     if constexpr (sizeof(T) == 4) d[1] = w[1];
 }
 
+// 32-bit values kept in 24 bits: the upper 16 of their words in one plane, the next 8 (rounded to nearest even) in another
+__device__ __forceinline__ void store_oct24(uint16_t *hi, uint8_t *lo, const float (&x)[8]) {
+    u32x4 h;
+    unsigned l[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        unsigned w = __float_as_uint(x[e]);
+        w += 0x7fu + ((w >> 8) & 1u);
+        if (e % 2 == 0) h[e / 2] = w >> 16;
+        else h[e / 2] |= w & 0xffff0000u;
+        l[e / 4] |= ((w >> 8) & 0xffu) << (8 * (e % 4));
+    }
+    *(u32x4 *)hi = h;
+    *(uint2 *)lo = make_uint2(l[0], l[1]);
+}
+__device__ __forceinline__ void load_oct24(const uint16_t *hi, const uint8_t *lo, float (&x)[8]) {
+    const u32x4 h = *(const u32x4 *)hi;
+    const uint2 l2 = *(const uint2 *)lo;
+    const unsigned l[2] = {l2.x, l2.y};
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        x[e] = __uint_as_float((e % 2 ? h[e / 2] & 0xffff0000u : h[e / 2] << 16) | ((l[e / 4] >> (8 * (e % 4))) & 0xffu) << 8);
+}
+
 struct Activation { int kind; float c[4]; };
 
 // act(g) in 32 bits

@@ -49,6 +49,7 @@ class GatedFF:
                 raise ValueError("a cubic has four coefficients")
             s.act, s.c = ckksmi.ACT_POLY, (C.c_float * 4)(*cubic)
         self._s, self._r = s, C.byref(s)
+        self._saved_of = {}  # rows of the last call: bytes they save
 
     def _bytes(self, name, rows, *args):
         n = C.c_size_t(0)
@@ -81,8 +82,10 @@ class GatedFF:
                 self._matrix(w_down, self.d_out, self.d_hidden, dtype))
 
     def _saved(self, saved, rows):
-        if ckksmi._nbytes(saved) < 3 * rows * (self.d_hidden + 7) // 8 * 8 * (4 if self._s.dtype == ckksmi.F32 else 2) and ckksmi._nbytes(saved) < self.saved_bytes(rows):
-            raise ValueError("the buffer for saved activations is too small")
+        if self._saved_of.get(rows) is None:
+            self._saved_of = {rows: self.saved_bytes(rows)}
+        if ckksmi._nbytes(saved) < self._saved_of[rows]:
+            raise ValueError("the buffer for saved activations holds %d bytes of %d" % (ckksmi._nbytes(saved), self._saved_of[rows]))
         return ckksmi._ptr(saved)
 
     def forward(self, x, w_gate, w_up, w_down, y, ws, saved=None, stream=None):

@@ -35,8 +35,9 @@ def _rounded(v, dtype):
 def block(x, wg, wu, wd, act, dy=None, grad_dtype=None):
     """{name: (value, bound of |kernel - value|)} of the block's results.  The bound follows the kernel's order of steps to first
     order (times 1.25 for the rest): sums of n products in 32 bits lose at most (n + 8) 2^-24 of the sum of magnitudes in any
-    order, g, u, h, dg and du are rounded to the element type, results to theirs; an activation loses at most 32 x 2^-24 of the
-    magnitudes it is made of."""
+    order, h, dg and du are rounded to the element type (with f32 gradients of 16-bit operands to the sum of two f16 or three bf16
+    where they enter the weights' gradients), act(g) and u act'(g) to 17 bits between the passes (f32 gradients: 24), results to their type; an activation loses
+    at most 32 x 2^-24 of the magnitudes it is made of."""
     dtype = x.dtype
     grad_dtype = grad_dtype or dtype
     x, wg, wu, wd = (t.double() for t in (x, wg, wu, wd))
@@ -51,7 +52,14 @@ def block(x, wg, wu, wd, act, dy=None, grad_dtype=None):
         d1_near = torch.maximum(d1_near, (g.abs() <= eg).double())
     ea = d1_near * eg + 32 * U32 * mag
     h = a * u
-    eh = ea * u.abs() + a.abs() * eu + ea * eu + _rounded(h, dtype) + 4 * U32 * h.abs()
+    fine = dtype != torch.float32 and grad_dtype == torch.float32
+    parts = (3 if dtype == torch.bfloat16 else 2) if fine else 1
+
+    def paired(v):
+        return ROUND[dtype] ** parts * v.abs() + TINY[dtype]
+
+    eh0 = ea * u.abs() + a.abs() * eu + ea * eu + 4 * U32 * h.abs()
+    eh = eh0 + _rounded(h, dtype)
     y = h @ wd.t().contiguous()
     wda = wd.abs()
     ey = eh @ wda.t().contiguous() + (H + 8) * U32 * (h.abs() @ wda.t().contiguous())
@@ -59,18 +67,20 @@ def block(x, wg, wu, wd, act, dy=None, grad_dtype=None):
     if dy is None:
         return out
     dy = dy.double()
-    egs, eus = eg + _rounded(g, dtype), eu + _rounded(u, dtype)
     dh = dy @ wd
     edh = (O + 8) * U32 * (dy.abs() @ wda)
-    ed1 = d2.abs() * egs + 32 * U32 * (1 + mag)
+    ed1 = d2.abs() * eg + 32 * U32 * (1 + mag)
     if not isinstance(act, str):
-        ed1 = ed1 + 6 * abs(float(act[3])) * egs * egs
+        ed1 = ed1 + 6 * abs(float(act[3])) * eg * eg
     if act == "relu":
-        ed1 = ed1 + (g.abs() <= egs).double()
-    eas = d1.abs() * egs + ed1 * egs + 32 * U32 * mag
+        ed1 = ed1 + (g.abs() <= eg).double()
+    keep = 2.0**-17 if dtype != torch.float32 and not fine else U32
+    ea_kept = ea + keep * a.abs()
+    ep_kept = ed1 * u.abs() + d1.abs() * eu + ed1 * eu + (keep + 2 * U32) * (u * d1).abs()
     dg, du = dh * u * d1, dh * a
-    edg = edh * (u * d1).abs() + (dh * d1).abs() * eus + (dh * u).abs() * ed1 + dh.abs() * eus * ed1 + _rounded(dg, dtype) + 8 * U32 * dg.abs()
-    edu = edh * a.abs() + dh.abs() * eas + _rounded(du, dtype) + 8 * U32 * du.abs()
+    edg0 = edh * (u * d1).abs() + dh.abs() * ep_kept + 2 * U32 * dg.abs()
+    edu0 = edh * a.abs() + dh.abs() * ea_kept + 2 * U32 * du.abs()
+    edg, edu = edg0 + _rounded(dg, dtype), edu0 + _rounded(du, dtype)
     dx = dg @ wg + du @ wu
     edx = edg @ wg.abs() + edu @ wu.abs() + (2 * H + 8) * U32 * (dg.abs() @ wg.abs() + du.abs() @ wu.abs())
     out["dx"] = (dx, 1.25 * (edx + _rounded(dx, dtype)))
@@ -78,14 +88,14 @@ def block(x, wg, wu, wd, act, dy=None, grad_dtype=None):
     def weights(l, el, r, er):
         lt, elt = l.t().contiguous(), el.t().contiguous()
         v = lt @ r
-        e = elt @ r.abs() + (M + 8) * U32 * (lt.abs() @ r.abs())
+        e = elt @ r.abs() + (parts * M + 8) * U32 * (lt.abs() @ r.abs())
         if er is not None:
             e = e + lt.abs() @ er
         return v, 1.25 * (e + _rounded(v, grad_dtype))
 
-    out["dwg"] = weights(dg, edg, x, None)
-    out["dwu"] = weights(du, edu, x, None)
-    out["dwd"] = weights(dy, torch.zeros_like(dy), h, eh)
+    out["dwg"] = weights(dg, edg0 + paired(dg), x, None)
+    out["dwu"] = weights(du, edu0 + paired(du), x, None)
+    out["dwd"] = weights(dy, torch.zeros_like(dy), h, eh0 + paired(h))
     return out
 
 
