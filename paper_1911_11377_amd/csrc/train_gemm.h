@@ -161,6 +161,19 @@ template <bool IS_B, int ES, int R> __device__ __forceinline__ int swizzle_rows(
     return (IS_B ? (q & 1) | (q >> 1) << 3 : q << 2) & (chunks - 1);
 }
 
+// 16 bytes a lane from a descriptor's memory to LDS: lane l's to lds + 16 l.  In assembly, so that the compiler, which takes every
+// such load for a write to all of the LDS, does not wait for it before it reads the other stage: tile_barrier() waits
+__device__ __forceinline__ void load_to_lds(unsigned lds, unsigned offset, u32x4 descriptor) {
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(descriptor) : "memory");
+}
+__device__ __forceinline__ u32x4 descriptor(const char *p) {
+    const uint64_t a = (uint64_t)p;
+    return u32x4{(unsigned)a, (unsigned)(a >> 32) & 0xffffu, 0x7ffffff0u, 0x00027000u};
+}
+// Every wave's loads to LDS have arrived, and every wave has read what it read before
+__device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ unsigned lds_address(const char *p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
+
 // Loads of one operand's tiles of R rows: what a lane needs to know, found once
 template <class T, int R, bool ALONG_ROWS, bool IS_B, int WAVES, bool TWO>
 struct TileLoad {
@@ -188,21 +201,13 @@ struct TileLoad {
             }
         }
     }
-    // the tile whose k indices begin at k0 of K; base: the operand at the tile's first row (TWO: both operands')
-    __device__ __forceinline__ void issue(char *lds, int wave, const char *base0, const char *base1, size_t ld, int k0, int K) const {
-        const size_t skip = ALONG_ROWS ? (size_t)k0 * ld : (size_t)k0 * ES;
-        const __amdgpu_buffer_rsrc_t r0 = __builtin_amdgcn_make_buffer_rsrc((void *)(base0 + skip), 0, 0x7ffffff0, 0x00027000);
-        const __amdgpu_buffer_rsrc_t r1 = __builtin_amdgcn_make_buffer_rsrc((void *)((TWO ? base1 : base0) + skip), 0, 0x7ffffff0, 0x00027000);
-        const bool tail = k0 + KSTEP > K;
+    // the tile at p0 (TWO: its second half at p1), whose first k_left k indices exist
+    __device__ __forceinline__ void issue(unsigned lds, int wave, const char *p0, const char *p1, int k_left) const {
+        const u32x4 r0 = descriptor(p0), r1 = descriptor(TWO ? p1 : p0);
 #pragma unroll
         for (int it = 0; it < NI; it++) {
-            unsigned o = off[it];
-            if (tail && k0 + kc[it] >= K) o = TG_OUTSIDE;
-            char *d = lds + (it * WAVES + wave) * 1024;
-            if (TWO && it >= NI / 2)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r1, (__attribute__((address_space(3))) void *)d, 16, o, 0, 0, 0);
-            else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r0, (__attribute__((address_space(3))) void *)d, 16, o, 0, 0, 0);
+            const unsigned o = k_left >= KSTEP || kc[it] < k_left ? off[it] : TG_OUTSIDE;
+            load_to_lds(lds + (it * WAVES + wave) * 1024, o, TWO && it >= NI / 2 ? r1 : r0);
         }
     }
     // 16 bytes of a lane: sub-step kk (0: the first half of the step's k indices, 1: the second) of the fragment whose first row is `row0`;
@@ -281,23 +286,28 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN)) gemm_kernel(GemmAr
     LB lb;
     la.init(wave, lane, P.lda, P.M - m0);
     lb.init(wave, lane, P.ldb, P.N - n0);
-    const size_t a_skip = A_ROWS ? (size_t)m0 * sizeof(T) : (size_t)m0 * P.lda;
-    const size_t b_skip = B_ROWS ? (size_t)n0 * sizeof(T) : (size_t)n0 * P.ldb;
-
-    const int per_src = (P.K + LA::KSTEP - 1) / LA::KSTEP, steps = per_src * P.nsrc;
+    // k indices [step s0, step s1) of the sources' steps, one behind the other
+    const int K = P.K, per_src = (K + LA::KSTEP - 1) / LA::KSTEP, steps = per_src * P.nsrc;
     const int s0 = (int)((long long)steps * blockIdx.y / G.splits), s1 = (int)((long long)steps * (blockIdx.y + 1) / G.splits);
-
-    auto issue = [&](char *st, int s) {
-        const char *a = P.a[0], *b = P.b[0];
-        if constexpr (EPI == EPI_STORE)
-            for (int i = 1; i < P.nsrc && s >= per_src; i++) {
-                s -= per_src;
-                a = P.a[i];
-                b = P.b[i];
-            }
-        const int k0 = s * LA::KSTEP;
-        la.issue(st, wave, a + a_skip, nullptr, P.lda, k0, P.K);
-        lb.issue(st + LA::BYTES, wave, b + b_skip, GATE ? P.b[1] + b_skip : nullptr, P.ldb, k0, P.K);
+    int src = s0 / per_src, k_left = K - (s0 - src * per_src) * LA::KSTEP;
+    const size_t a_step = A_ROWS ? LA::KSTEP * P.lda : TG_STEP_BYTES, b_step = B_ROWS ? LA::KSTEP * P.ldb : TG_STEP_BYTES;
+    const size_t a_tile = A_ROWS ? (size_t)m0 * sizeof(T) : (size_t)m0 * P.lda, b_tile = B_ROWS ? (size_t)n0 * sizeof(T) : (size_t)n0 * P.ldb;
+    const char *pa = P.a[src] + a_tile + (s0 - src * per_src) * a_step, *pb = P.b[src] + b_tile + (s0 - src * per_src) * b_step;
+    const char *pb1 = GATE ? P.b[1] + b_tile + s0 * b_step : nullptr;
+    auto issue = [&](const char *st) {
+        const unsigned at = lds_address(st);
+        la.issue(at, wave, pa, nullptr, k_left);
+        lb.issue(at + LA::BYTES, wave, pb, pb1, k_left);
+        pa += a_step;
+        pb += b_step;
+        if constexpr (GATE) pb1 += b_step;
+        k_left -= LA::KSTEP;
+        if (EPI == EPI_STORE && k_left <= 0 && src + 1 < P.nsrc) {
+            src++;
+            pa = P.a[src] + a_tile;
+            pb = P.b[src] + b_tile;
+            k_left = K;
+        }
     };
     f32x4 acc[FM][2 * PAIRS];
 #pragma unroll
@@ -305,9 +315,9 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN)) gemm_kernel(GemmAr
 #pragma unroll
         for (int j = 0; j < 2 * PAIRS; j++) acc[i][j] = f32x4{0, 0, 0, 0};
     auto multiply = [&](const char *st) {
+        u32x4 b[2 * PAIRS];
 #pragma unroll
         for (int kk = 0; kk < 2; kk++) {
-            u32x4 b[2 * PAIRS];
 #pragma unroll
             for (int p = 0; p < PAIRS; p++) {
                 // GATE: pair 0 is of the gate's weights, pair 1 of the other's
@@ -325,14 +335,14 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN)) gemm_kernel(GemmAr
     };
     static_assert(!GATE || WN == 64, "a wave holds 32 columns of both products");
 
-    if (s0 < s1) issue(stage0, s0);
+    if (s0 < s1) issue(stage0);
     for (int s = s0; s < s1; s += 2) {
-        __syncthreads();  // stage0 has arrived, stage1 is no longer read
-        if (s + 1 < s1) issue(stage1, s + 1);
+        tile_barrier();
+        if (s + 1 < s1) issue(stage1);
         multiply(stage0);
         if (s + 1 < s1) {
-            __syncthreads();
-            if (s + 2 < s1) issue(stage0, s + 2);
+            tile_barrier();
+            if (s + 2 < s1) issue(stage0);
             multiply(stage1);
         }
     }
