@@ -110,11 +110,12 @@ template <class P, class G, int BITS> struct AdamwLoaded;
 template <class P, class G> struct AdamwLoaded<P, G, 32> { P p[4]; G g[4]; float m[4], v[4]; };
 template <class P, class G> struct AdamwLoaded<P, G, 8> { P p[4]; G g[4]; unsigned char m[4], v[4]; float mu, vu; };
 
-template <class P, class G, int BITS, bool WHOLE>
+// a wave's share of a chunk: BLOCKS blocks from `begin` on, 1024 elements apart
+template <class P, class G, int BITS, bool WHOLE, int BLOCKS>
 __device__ __forceinline__ void adamw_chunk(const AdamwArgs &A, const ckksmi_adamw_tensor &t, int64_t begin, unsigned tensor) {
     typedef typename std::conditional<BITS == 8, unsigned char, float>::type State;
     const int64_t n = t.n;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
     P *p = (P *)t.p;
     const G *grad = (const G *)t.grad;
     State *m = (State *)t.m, *v = (State *)t.v;
@@ -122,7 +123,7 @@ __device__ __forceinline__ void adamw_chunk(const AdamwArgs &A, const ckksmi_ada
     const unsigned key = adamw_mix(A.key + tensor);
 
     auto load = [&](int b, AdamwLoaded<P, G, BITS> &x) {
-        const int64_t first = begin + (b * 4 + wave) * 256, i = first + 4 * lane;
+        const int64_t first = begin + b * 1024, i = first + 4 * lane;
         if (!WHOLE && first >= n) return;
         load4<WHOLE>(p, i, n, p4, x.p);
         load4<WHOLE>(grad, i, n, g4, x.g);
@@ -134,7 +135,7 @@ __device__ __forceinline__ void adamw_chunk(const AdamwArgs &A, const ckksmi_ada
         }
     };
     auto update = [&](int b, AdamwLoaded<P, G, BITS> &x) {
-        const int64_t first = begin + (b * 4 + wave) * 256, i = first + 4 * lane;
+        const int64_t first = begin + b * 1024, i = first + 4 * lane;
         if (!WHOLE && first >= n) return;
         float q[4];
         if constexpr (BITS == 32) {
@@ -212,8 +213,8 @@ __device__ __forceinline__ void adamw_chunk(const AdamwArgs &A, const ckksmi_ada
     AdamwLoaded<P, G, BITS> x[2];
     load(0, x[0]);
 #pragma unroll
-    for (int b = 0; b < TA_CHUNK / 1024; b++) {
-        if (b + 1 < TA_CHUNK / 1024) load(b + 1, x[(b + 1) & 1]);
+    for (int b = 0; b < BLOCKS; b++) {
+        if (b + 1 < BLOCKS) load(b + 1, x[(b + 1) & 1]);
         update(b, x[b & 1]);
     }
 }
@@ -230,9 +231,16 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwArgs A) {
     const ckksmi_adamw_tensor &t = A.t[lo];
     const int64_t begin = (int64_t)(blockIdx.x - A.first[lo]) * TA_CHUNK;
     typedef typename std::conditional<BITS == 8, unsigned char, float>::type State;
-    const bool whole = begin + TA_CHUNK <= t.n && at4((P *)t.p) && at4((const G *)t.grad) && at4((State *)t.m) && at4((State *)t.v) && at4((const __bf16 *)t.copy);
-    if (whole) adamw_chunk<P, G, BITS, true>(A, t, begin, (unsigned)(A.tensor0 + lo));
-    else adamw_chunk<P, G, BITS, false>(A, t, begin, (unsigned)(A.tensor0 + lo));
+    const bool aligned = at4((P *)t.p) && at4((const G *)t.grad) && at4((State *)t.m) && at4((State *)t.v) && at4((const __bf16 *)t.copy);
+    const unsigned tensor = (unsigned)(A.tensor0 + lo);
+    int64_t first = begin + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 256;
+    if (aligned && begin + TA_CHUNK <= t.n) return adamw_chunk<P, G, BITS, true, TA_CHUNK / 1024>(A, t, first, tensor);
+    // a tensor's end: its whole blocks without conditions likewise
+#pragma unroll 1
+    for (int b = 0; b < TA_CHUNK / 1024; b++, first += 1024) {
+        if (aligned && first + 256 <= t.n) adamw_chunk<P, G, BITS, true, 1>(A, t, first, tensor);
+        else adamw_chunk<P, G, BITS, false, 1>(A, t, first, tensor);
+    }
 }
 
 struct ReadStatesArgs {
