@@ -62,7 +62,8 @@ extern "C" {
 #define CKKSMI_K_GEMM_COPY 39     /* operands copied to aligned rows (units: workgroups) */
 #define CKKSMI_K_ADAMW 40         /* optimiser step (units: elements, to whole workgroups) */
 #define CKKSMI_K_ADAMW_READ 41    /* 8-bit states read back (the same) */
-#define CKKSMI_K_COUNT 42
+#define CKKSMI_K_GEMM_ROWS 42     /* products of few rows with a weight matrix (units: operations) */
+#define CKKSMI_K_COUNT 43
 int ckksmi_profile_enable(ckksmi_ctx *ctx, int on);
 int ckksmi_profile_read(ckksmi_ctx *ctx, int kernel_class, double *total_ms, long long *launches, double *units);
 /* name of the kernel that class runs as in this context (the transforms have size-specific kernels; a fused kernel's variants for

@@ -120,7 +120,7 @@ SIGNATURES = {
 }
 _RESTYPES = {"ckksmi_ctx_destroy": None, "ckksmi_strerror": C.c_char_p, "ckksmi_kernel_class_name": C.c_char_p}
 TRAINING = ("ckksmi_gated_ff_", "ckksmi_adamw_")  # entry points of csrc/train_device.hip
-K_COUNT = 42
+K_COUNT = 43
 
 _LIBS = {}
 

@@ -6,6 +6,7 @@
 #include "device_call.h"
 #include "train_adamw.h"
 #include "train_gemm.h"
+#include "train_rows.h"
 
 namespace {
 
@@ -95,24 +96,20 @@ int tiles_of(const GemmProblem &p, const TileShape &t, bool gate, GemmProblem *o
     return tm * tn;
 }
 
+// The largest tile of which there are enough for most compute units; below that, tiles of 32 rows whose steps are shared by four groups of waves
+// (small products, bound by latency), or larger tiles with the k axis in parts where the operands' bytes count
 Shape choose(const GemmProblem *p, int n, bool gate, size_t es) {
-    int most = 0;
-    for (int i = 0; i < n; i++) most = std::max(most, p[i].M);
-    Shape s;
-    s.tile = most <= 32 ? 2 : 1;
-    int tiles[2] = {0, 0};
+    int tiles[3] = {0, 0, 0};
+    double flops = 0;
     for (int i = 0; i < n; i++) {
-        tiles[0] += tiles_of(p[i], kTiles[0], gate, nullptr);
-        tiles[1] += tiles_of(p[i], kTiles[s.tile], gate, nullptr);
-    }
-    if (es == 2 && tiles[0] >= 192) {
-        s.tile = 0;
-        s.splits = 1;
-        return s;
+        for (int t = 0; t < 3; t++) tiles[t] += tiles_of(p[i], kTiles[t], gate, nullptr);
+        flops += 2.0 * p[i].M * p[i].N * p[i].K * (gate ? 2 : p[i].nsrc);
     }
     const int steps = (int)(((size_t)p[0].K * es + TG_STEP_BYTES - 1) / TG_STEP_BYTES) * p[0].nsrc;
-    s.splits = std::max(1, std::min(std::min(512 / std::max(1, tiles[1]), steps / 4), kMaxSplits));
-    return s;
+    if (es == 2 && tiles[0] >= 192) return Shape{0, 1};
+    if (tiles[1] >= 192) return Shape{1, std::max(1, std::min(512 / tiles[1], steps / 8))};
+    if (flops > (es == 2 ? 4e9 : 1e9) && p[0].M > 64) return Shape{1, std::max(1, std::min(std::min(512 / std::max(1, tiles[1]), steps / 4), kMaxSplits))};
+    return Shape{2, std::max(1, std::min(std::min(256 / std::max(1, tiles[2]), steps / 16), kMaxSplits))};
 }
 
 size_t part_bytes(const GemmProblem &p, int splits, bool gate) {
@@ -142,9 +139,9 @@ void launch_gemm(ckksmi_ctx *c, GemmProblem *p, int n, Carve w, hipStream_t st) 
     G.splits = s.splits;
     const dim3 grid(total, s.splits);
     if constexpr (sizeof(T) == 2)
-        if (s.tile == 0) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 256, 256, 128, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(512), st, G);
-    if (s.tile == 1) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 128, 128, 64, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(256), st, G);
-    if (s.tile == 2) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 32, 128, 16, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(256), st, G);
+        if (s.tile == 0) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 256, 256, 128, 64, 1, A_ROWS, B_ROWS, EPI>), grid, dim3(512), st, G);
+    if (s.tile == 1) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 128, 128, 64, 64, 1, A_ROWS, B_ROWS, EPI>), grid, dim3(256), st, G);
+    if (s.tile == 2) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 32, 128, 16, 64, 4, A_ROWS, B_ROWS, EPI>), grid, dim3(1024), st, G);
     if (s.splits > 1) KL(c, CKKSMI_K_GEMM_JOIN, flops, (gemm_join_kernel<T, EPI>), dim3(join, n), dim3(256), st, G);
 }
 
@@ -208,25 +205,57 @@ size_t workspace_of(const ckksmi_gated_ff &f, bool backward) {
     return (backward ? std::max(forward, back) : forward) + split_bytes(f, backward);
 }
 
+// Few rows: products straight from the operands where they lie
+constexpr int kFewRows = 64;
+template <class T, int EPI>
+void launch_rows(ckksmi_ctx *c, const RowsArgs &R, hipStream_t st) {
+    const int blocks = (R.N + 15) / 16, tiles = (R.M + 15) / 16;
+    const double flops = 2.0 * R.M * R.N * R.K * (EPI == EPI_GATE ? 2 : 1);
+    // as many rows of x a workgroup as keep two workgroups a compute unit
+    const int mt = blocks * tiles <= 512 ? 1 : blocks * ((tiles + 1) / 2) <= 512 ? 2 : 4;
+    const dim3 grid(blocks, (tiles + mt - 1) / mt);
+    switch (mt) {
+        case 1: KL(c, CKKSMI_K_GEMM_ROWS, flops, (rows_kernel<T, EPI, 1, 16>), grid, dim3(1024), st, R); break;
+        case 2: KL(c, CKKSMI_K_GEMM_ROWS, flops, (rows_kernel<T, EPI, 2, 8>), grid, dim3(512), st, R); break;
+        default: KL(c, CKKSMI_K_GEMM_ROWS, flops, (rows_kernel<T, EPI, 4, 8>), grid, dim3(512), st, R); break;
+    }
+}
+
 template <class T>
 int forward(ckksmi_ctx *c, const ckksmi_gated_ff &f, const void *x, const void *wg, const void *wu, const void *wd, void *y, void *saved, Carve w, hipStream_t st) {
     const FF d(f);
     Guard guard(c);
+    char *const keep = (char *)saved;
+    EpiArgs to_hidden;
+    memset(&to_hidden, 0, sizeof(to_hidden));
+    if (keep) to_hidden.kept = d.kept(keep);
+    to_hidden.parts = keep ? d.parts(f.dtype) : 1;
+    to_hidden.part_bytes = d.hidden_bytes();
+    to_hidden.ldo = d.ldh; to_hidden.N = (int)d.H; to_hidden.act = activation_of(f);
+    if (d.M <= kFewRows) {
+        RowsArgs R;
+        memset(&R, 0, sizeof(R));
+        char *const h = keep ? d.saved_h(keep) : w.take(d.hidden_bytes());
+        R.x = (const char *)x; R.w[0] = (const char *)wg; R.w[1] = (const char *)wu; R.ldx = ld_bytes(f.ld_x, d.K, d.es); R.ldw = d.K * d.es;
+        R.M = (int)d.M; R.N = (int)d.H; R.K = (int)d.K; R.epi = to_hidden; R.epi.o0 = h;
+        launch_rows<T, EPI_GATE>(c, R, st);
+        GemmProblem down = product(Matrix{h, d.ldh * d.es}, Matrix{(const char *)wd, d.H * d.es}, d.M, d.O, d.H);
+        store_to(down, y, f.ld_y ? f.ld_y : d.O, f.dtype, false);
+        R.x = h; R.w[0] = down.b[0]; R.ldx = down.lda; R.ldw = down.ldb;
+        R.N = (int)d.O; R.K = (int)d.H; R.epi = down.epi;
+        launch_rows<T, EPI_STORE>(c, R, st);
+        return guard.rc();
+    }
     Operands<T> ops;
     const Matrix mx = ops.use(x, ld_bytes(f.ld_x, d.K, d.es), d.M, d.K, w), mg = ops.use(wg, d.K * d.es, d.H, d.K, w), mu = ops.use(wu, d.K * d.es, d.H, d.K, w);
     const Matrix md = ops.use(wd, d.H * d.es, d.O, d.H, w);
-    char *h = w.take(d.hidden_bytes());
-    char *const keep = (char *)saved;
-    if (keep) h = d.saved_h(keep);
+    char *const h = keep ? d.saved_h(keep) : w.take(d.hidden_bytes());
     ops.run(c, st);
 
     GemmProblem gate = product(mx, mg, d.M, d.H, d.K);
     gate.b[1] = mu.p;
+    gate.epi = to_hidden;
     gate.epi.o0 = h;
-    if (keep) gate.epi.kept = d.kept(keep);
-    gate.epi.parts = keep ? d.parts(f.dtype) : 1;
-    gate.epi.part_bytes = d.hidden_bytes();
-    gate.epi.ldo = d.ldh; gate.epi.N = (int)d.H; gate.epi.act = activation_of(f);
     launch_gemm<T, false, false, EPI_GATE>(c, &gate, 1, w, st);
 
     GemmProblem down = product(Matrix{h, d.ldh * d.es}, md, d.M, d.O, d.H);

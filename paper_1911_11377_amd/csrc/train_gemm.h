@@ -5,7 +5,7 @@
 // for the block's operand orders.  An operand "along k" has its k indices side by side in memory (x, weights of the forward
 // pass); one "along rows" has its rows side by side (weights of the backward pass, both operands of the weights' gradients).
 //
-// Tiles.  A workgroup computes BM x BN results, 128 bytes of k (64 or 32 indices) a step.  Both operands' tiles go from
+// Tiles.  A workgroup computes BM x BN results, 128 bytes of k (64 or 32 indices) a step (small tiles: four steps at once).  Both operands' tiles go from
 // memory to LDS without registers in between (16 bytes a lane), two stages: while one is multiplied the next is on its way.
 // Lanes whose row, column or k index lies beyond the operand are pointed past the end of the load's descriptor and bring
 // zeros, so no tile needs a case of its own.
@@ -260,15 +260,17 @@ __device__ __forceinline__ int xcd_order(int wg, int total) {
     return x * per + (x < rest ? x : rest) + i;
 }
 
-template <class T, int BM, int BN, int WM, int WN, bool A_ROWS, bool B_ROWS, int EPI>
-__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN)) gemm_kernel(GemmArgs G) {
+// KG: groups of waves that share the k axis of a tile step by step, each with LDS stages of its own; group 0 adds up
+template <class T, int BM, int BN, int WM, int WN, int KG, bool A_ROWS, bool B_ROWS, int EPI>
+__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_kernel(GemmArgs G) {
     constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32;
     constexpr bool GATE = EPI == EPI_GATE;
     typedef TileLoad<T, BM, A_ROWS, false, WAVES, false> LA;
     typedef TileLoad<T, BN, B_ROWS, true, WAVES, GATE> LB;
-    __shared__ __attribute__((aligned(1024))) char stage0[LA::BYTES + LB::BYTES];
-    __shared__ __attribute__((aligned(1024))) char stage1[LA::BYTES + LB::BYTES];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int STAGE = LA::BYTES + LB::BYTES;
+    __shared__ __attribute__((aligned(1024))) char stages[KG * 2 * STAGE];
+    const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave_of_all % WAVES, group = wave_of_all / WAVES;
+    char *const stage0 = stages + group * 2 * STAGE, *const stage1 = stage0 + STAGE;
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN);
 
     int tile = xcd_order(blockIdx.x, gridDim.x), pi = 0;
@@ -289,24 +291,31 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN)) gemm_kernel(GemmAr
     // k indices [step s0, step s1) of the sources' steps, one behind the other
     const int K = P.K, per_src = (K + LA::KSTEP - 1) / LA::KSTEP, steps = per_src * P.nsrc;
     const int s0 = (int)((long long)steps * blockIdx.y / G.splits), s1 = (int)((long long)steps * (blockIdx.y + 1) / G.splits);
-    int src = s0 / per_src, k_left = K - (s0 - src * per_src) * LA::KSTEP;
     const size_t a_step = A_ROWS ? LA::KSTEP * P.lda : TG_STEP_BYTES, b_step = B_ROWS ? LA::KSTEP * P.ldb : TG_STEP_BYTES;
     const size_t a_tile = A_ROWS ? (size_t)m0 * sizeof(T) : (size_t)m0 * P.lda, b_tile = B_ROWS ? (size_t)n0 * sizeof(T) : (size_t)n0 * P.ldb;
-    const char *pa = P.a[src] + a_tile + (s0 - src * per_src) * a_step, *pb = P.b[src] + b_tile + (s0 - src * per_src) * b_step;
-    const char *pb1 = GATE ? P.b[1] + b_tile + s0 * b_step : nullptr;
+    int src = 0, step = s0 + group;  // of the source
+    auto enter = [&]() {
+        while (step >= per_src && src + 1 < P.nsrc) {
+            step -= per_src;
+            src++;
+        }
+    };
+    enter();
+    const char *pa = P.a[src] + a_tile + step * a_step, *pb = P.b[src] + b_tile + step * b_step;
+    const char *pb1 = GATE ? P.b[1] + b_tile + step * b_step : nullptr;
     auto issue = [&](const char *st) {
         const unsigned at = lds_address(st);
+        const int k_left = K - step * LA::KSTEP;
         la.issue(at, wave, pa, nullptr, k_left);
         lb.issue(at + LA::BYTES, wave, pb, pb1, k_left);
-        pa += a_step;
-        pb += b_step;
-        if constexpr (GATE) pb1 += b_step;
-        k_left -= LA::KSTEP;
-        if (EPI == EPI_STORE && k_left <= 0 && src + 1 < P.nsrc) {
-            src++;
-            pa = P.a[src] + a_tile;
-            pb = P.b[src] + b_tile;
-            k_left = K;
+        pa += KG * a_step;
+        pb += KG * b_step;
+        if constexpr (GATE) pb1 += KG * b_step;
+        step += KG;
+        if (EPI == EPI_STORE && step >= per_src && src + 1 < P.nsrc) {
+            enter();
+            pa = P.a[src] + a_tile + step * a_step;
+            pb = P.b[src] + b_tile + step * b_step;
         }
     };
     f32x4 acc[FM][2 * PAIRS];
@@ -335,16 +344,35 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN)) gemm_kernel(GemmAr
     };
     static_assert(!GATE || WN == 64, "a wave holds 32 columns of both products");
 
-    if (s0 < s1) issue(stage0);
-    for (int s = s0; s < s1; s += 2) {
+    const int rounds = (s1 - s0 + KG - 1) / KG, own = (s1 - s0 - group + KG - 1) / KG;  // of the workgroup, of this group
+    if (own > 0) issue(stage0);
+    for (int r = 0; r < rounds; r += 2) {
         tile_barrier();
-        if (s + 1 < s1) issue(stage1);
-        multiply(stage0);
-        if (s + 1 < s1) {
+        if (r + 1 < own) issue(stage1);
+        if (KG == 1 || r < own) multiply(stage0);
+        if (r + 1 < rounds) {
             tile_barrier();
-            if (s + 2 < s1) issue(stage0);
-            multiply(stage1);
+            if (r + 2 < own) issue(stage0);
+            if (KG == 1 || r + 1 < own) multiply(stage1);
         }
+    }
+    if constexpr (KG > 1) {
+        static_assert((KG - 1) * BM * BN * 4 <= KG * 2 * STAGE, "the other groups' sums fit the stages");
+        f32x4 *sums = (f32x4 *)stages;
+        tile_barrier();
+#pragma unroll
+        for (int f = 0; f < FM; f++)
+#pragma unroll
+            for (int j = 0; j < 2 * PAIRS; j++)
+                if (group) sums[(((group - 1) * FM + f) * 2 * PAIRS + j) * WAVES * 64 + wave * 64 + lane] = acc[f][j];
+        tile_barrier();
+        if (group) return;
+#pragma unroll
+        for (int g = 0; g < KG - 1; g++)
+#pragma unroll
+            for (int f = 0; f < FM; f++)
+#pragma unroll
+                for (int j = 0; j < 2 * PAIRS; j++) acc[f][j] += sums[((g * FM + f) * 2 * PAIRS + j) * WAVES * 64 + wave * 64 + lane];
     }
 
     const int i = lane & 15, q = lane >> 4;

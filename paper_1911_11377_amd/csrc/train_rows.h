@@ -1,0 +1,95 @@
+// Products of few rows with a weight matrix, y = x W^T, for answering requests: the weights are read once, at whatever
+// alignment their rows have, and nothing is copied, staged or joined by another launch.
+//
+// A workgroup takes 16 weight rows (GATE: 16 of each matrix) and 16 * MT rows of x; its waves share the k axis in runs of 128
+// bytes a row.  Both operands come from memory as the fragments that the matrix cores take, 16 bytes a lane (row l % 16, chunk
+// l / 16); the waves' sums meet in LDS and are added in their order.
+// Bound by the weights' bytes and, at these sizes, by the latency of one trip to memory: hence many waves, each with all its
+// loads of a run in flight.
+#pragma once
+#include "train_gemm.h"
+
+struct RowsArgs {
+    const char *x, *w[2];
+    size_t ldx, ldw;  // bytes
+    int M, N, K;
+    EpiArgs epi;
+};
+
+// 16 bytes of a row from element k on; elements from K on are zeros
+template <class T> __device__ __forceinline__ u32x4 row_chunk(const char *row, int k, int K) {
+    constexpr int EPC = 16 / sizeof(T);
+    const T *p = (const T *)row + k;
+    u32x4 v = {0, 0, 0, 0};
+    if (k + EPC <= K) __builtin_memcpy(&v, p, 16);
+    else if (k < K) {
+        T e[EPC];
+#pragma unroll
+        for (int j = 0; j < EPC; j++) e[j] = k + j < K ? p[j] : (T)0.0f;
+        __builtin_memcpy(&v, e, 16);
+    }
+    return v;
+}
+
+template <class T, int EPI, int MT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) rows_kernel(RowsArgs R) {
+    constexpr int MATS = EPI == EPI_GATE ? 2 : 1, EPC = 16 / sizeof(T), RUN = 128 / sizeof(T);
+    __shared__ f32x4 sums[WAVES][MATS][MT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
+    // rows beyond the end repeat the last one: their results are not stored
+    const char *w[MATS], *x[MT];
+#pragma unroll
+    for (int a = 0; a < MATS; a++) w[a] = R.w[a] + (size_t)min(n0 + i, R.N - 1) * R.ldw;
+#pragma unroll
+    for (int t = 0; t < MT; t++) x[t] = R.x + (size_t)min(m0 + 16 * t + i, R.M - 1) * R.ldx;
+    f32x4 acc[MATS][MT];
+#pragma unroll
+    for (int a = 0; a < MATS; a++)
+#pragma unroll
+        for (int t = 0; t < MT; t++) acc[a][t] = f32x4{0, 0, 0, 0};
+#pragma unroll 2
+    for (int k0 = wave * RUN; k0 < R.K; k0 += WAVES * RUN) {
+        u32x4 fw[MATS][2], fx[MT][2];
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+            const int k = k0 + (4 * s + q) * EPC;
+#pragma unroll
+            for (int a = 0; a < MATS; a++) fw[a][s] = row_chunk<T>(w[a], k, R.K);
+#pragma unroll
+            for (int t = 0; t < MT; t++) fx[t][s] = row_chunk<T>(x[t], k, R.K);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; s++)
+#pragma unroll
+            for (int a = 0; a < MATS; a++)
+#pragma unroll
+                for (int t = 0; t < MT; t++) acc[a][t] = mma<T>(fw[a][s], fx[t][s], acc[a][t]);
+    }
+#pragma unroll
+    for (int a = 0; a < MATS; a++)
+#pragma unroll
+        for (int t = 0; t < MT; t++) sums[wave][a][t][lane] = acc[a][t];
+    __syncthreads();
+    // lane l's sums are row l % 16's columns 4*(l/16) .. +3: a thread takes 8 columns of a row
+    if (threadIdx.x >= 32 * MT) return;
+    const int t = threadIdx.x / 32, row = threadIdx.x % 16, half = threadIdx.x / 16 % 2, m = m0 + 16 * t + row, n = n0 + 8 * half;
+    if (m >= R.M || n >= R.N) return;
+    float v[2][8];
+#pragma unroll
+    for (int a = 0; a < MATS; a++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            f32x4 s = sums[0][a][t][(2 * half + e) * 16 + row];
+#pragma unroll
+            for (int k = 1; k < WAVES; k++) s += sums[k][a][t][(2 * half + e) * 16 + row];
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[a][4 * e + j] = s[j];
+        }
+    // columns beyond the end are kept as zeros in padded rows
+    if constexpr (EPI == EPI_GATE)
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            if (n + j >= R.N) v[0][j] = v[1][j] = 0.0f;
+    epilogue8<T, EPI>(R.epi, m, n, v[0], v[MATS - 1]);
+}
