@@ -105,7 +105,7 @@ Shape choose(const GemmProblem *p, int n, bool gate, size_t es) {
         for (int t = 0; t < 3; t++) tiles[t] += tiles_of(p[i], kTiles[t], gate, nullptr);
         flops += 2.0 * p[i].M * p[i].N * p[i].K * (gate ? 2 : p[i].nsrc);
     }
-    const int steps = (int)(((size_t)p[0].K * es + TG_STEP_BYTES - 1) / TG_STEP_BYTES) * p[0].nsrc;
+    const int steps = (int)(((size_t)p[0].K * es + 127) / 128) * p[0].nsrc;  // of 128 bytes
     if (es == 2 && tiles[0] >= 192) return Shape{0, 1};
     if (tiles[1] >= 192) return Shape{1, std::max(1, std::min(512 / tiles[1], steps / 8))};
     if (flops > (es == 2 ? 4e9 : 1e9) && p[0].M > 64) return Shape{1, std::max(1, std::min(std::min(512 / std::max(1, tiles[1]), steps / 4), kMaxSplits))};
@@ -139,9 +139,9 @@ void launch_gemm(ckksmi_ctx *c, GemmProblem *p, int n, Carve w, hipStream_t st) 
     G.splits = s.splits;
     const dim3 grid(total, s.splits);
     if constexpr (sizeof(T) == 2)
-        if (s.tile == 0) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 256, 256, 128, 64, 1, A_ROWS, B_ROWS, EPI>), grid, dim3(512), st, G);
-    if (s.tile == 1) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 128, 128, 64, 64, 1, A_ROWS, B_ROWS, EPI>), grid, dim3(256), st, G);
-    if (s.tile == 2) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 32, 128, 16, 64, 4, A_ROWS, B_ROWS, EPI>), grid, dim3(1024), st, G);
+        if (s.tile == 0) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 256, 256, 128, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(512), st, G);
+    if (s.tile == 1) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 128, 128, 64, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(256), st, G);
+    if (s.tile == 2) KL(c, CKKSMI_K_GEMM, flops, (gemm_small_kernel<T, 32, 128, 16, 64, 4, A_ROWS, B_ROWS, EPI>), grid, dim3(1024), st, G);
     if (s.splits > 1) KL(c, CKKSMI_K_GEMM_JOIN, flops, (gemm_join_kernel<T, EPI>), dim3(join, n), dim3(256), st, G);
 }
 

@@ -5,21 +5,19 @@
 // for the block's operand orders.  An operand "along k" has its k indices side by side in memory (x, weights of the forward
 // pass); one "along rows" has its rows side by side (weights of the backward pass, both operands of the weights' gradients).
 //
-// Tiles.  A workgroup computes BM x BN results, 128 bytes of k (64 or 32 indices) a step (small tiles: four steps at once).  Both operands' tiles go from
-// memory to LDS without registers in between (16 bytes a lane), two stages: while one is multiplied the next is on its way.
-// Lanes whose row, column or k index lies beyond the operand are pointed past the end of the load's descriptor and bring
-// zeros, so no tile needs a case of its own.
+// Tiles.  A workgroup computes BM x BN results.  Both operands' tiles go from memory to LDS without registers in between (16 bytes a
+// lane), some steps ahead of their use.  Lanes whose row, column or k index lies beyond the operand are pointed past the end
+// of the load's descriptor and bring zeros, so no tile needs a case of its own.
 //
 // Lane layout: v_mfma_f32_16x16x32 (16 bits) or four v_mfma_f32_16x16x4 (32 bits) take 16 bytes of each operand a lane:
 // row l % 16, k chunk l / 16.  B is the first operand, so lane l holds the results of A's row l % 16 and of B's rows
 // 4*(l/16) .. +3.  The B rows of two fragments are taken so that a lane's results of both are 8 neighbouring columns.
-//   along k    : LDS row r holds its eight 16-byte chunks at (chunk ^ swizzle(r)); a fragment is one ds_read_b128.
+//   along k    : LDS row r holds its 16-byte chunks at (chunk ^ swizzle(r)); a fragment is one ds_read_b128.
 //   along rows : LDS row k holds the tile's rows; 16-bit fragments are two ds_read_b64_tr_b16 (a group of 16 lanes reads
 //                4 k x 16 rows and gets them transposed), 32-bit ones four ds_read_b32.
 #pragma once
 #include "train_types.h"
 
-#define TG_STEP_BYTES 128   // bytes of k a step
 #define TG_OUTSIDE 0x80000000u  // a lane offset beyond every descriptor's end
 
 enum { EPI_GATE = 0, EPI_STORE = 1, EPI_DHID = 2 };
@@ -148,10 +146,11 @@ __device__ __forceinline__ void epilogue8(const EpiArgs &E, size_t m, int n, con
     }
 }
 
-// ---- operand tiles
+// ---- operand tiles, SB bytes of k deep (128 or 64)
 // swizzle of an LDS row's 16-byte chunks, so that the lanes of a fragment read spread over the banks.  Fragment rows:
 // A takes 16 neighbouring rows; B takes rows 8*(i/4) + i%4 (+ 4 for the second fragment of a pair), i = lane % 16
-template <bool IS_B> __device__ __forceinline__ int swizzle_k(int row) {
+template <bool IS_B, int SB> __device__ __forceinline__ int swizzle_k(int row) {
+    if constexpr (SB == 64) return IS_B ? (row >> 3) & 3 : (row >> 2) & 3;
     return IS_B ? ((row >> 1) & 1) | ((row >> 3) & 3) << 1 : (row >> 1) & 7;
 }
 template <bool IS_B, int ES, int R> __device__ __forceinline__ int swizzle_rows(int k) {
@@ -170,16 +169,20 @@ __device__ __forceinline__ u32x4 descriptor(const char *p) {
     const uint64_t a = (uint64_t)p;
     return u32x4{(unsigned)a, (unsigned)(a >> 32) & 0xffffu, 0x7ffffff0u, 0x00027000u};
 }
+// All but the wave's newest N loads have arrived, and all but its newest READS LDS reads
+template <int N, int READS = 15> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)" ::"n"(N), "n"(READS) : "memory"); }
+__device__ __forceinline__ void wave_barrier() { asm volatile("s_barrier" ::: "memory"); }
 // Every wave's loads to LDS have arrived, and every wave has read what it read before
 __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ unsigned lds_address(const char *p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
 
 // Loads of one operand's tiles of R rows: what a lane needs to know, found once
-template <class T, int R, bool ALONG_ROWS, bool IS_B, int WAVES, bool TWO>
+template <class T, int R, int SB, bool ALONG_ROWS, bool IS_B, int WAVES, bool TWO>
 struct TileLoad {
-    static constexpr int ES = sizeof(T), EPC = 16 / ES, KSTEP = TG_STEP_BYTES / ES;
-    static constexpr int BYTES = R * TG_STEP_BYTES;
+    static constexpr int ES = sizeof(T), EPC = 16 / ES, KSTEP = SB / ES;
+    static constexpr int BYTES = R * SB;
     static constexpr int NI = BYTES / 1024 / WAVES;  // load instructions of a wave
+    static constexpr int READS = !ALONG_ROWS ? 1 : ES == 2 ? 2 : 4;  // LDS reads of a fragment
     static_assert(NI * WAVES * 1024 == BYTES, "whole instructions");
     unsigned off[NI];  // byte offset of the lane's 16 bytes from the tile's first
     int kc[NI];        // their (first) k index within the step
@@ -189,7 +192,8 @@ struct TileLoad {
         for (int it = 0; it < NI; it++) {
             const int s = it * WAVES + wave;
             if constexpr (!ALONG_ROWS) {
-                const int row = s * 8 + (lane >> 3), c = (lane & 7) ^ swizzle_k<IS_B>(row);
+                constexpr int CPR = SB / 16;  // chunks of an LDS row
+                const int row = s * (64 / CPR) + lane / CPR, c = (lane % CPR) ^ swizzle_k<IS_B, SB>(row);
                 const int mem_row = TWO && row >= R / 2 ? row - R / 2 : row;
                 off[it] = mem_row < rows_left ? (unsigned)(mem_row * ld + c * 16) : TG_OUTSIDE;
                 kc[it] = c * EPC;
@@ -201,43 +205,43 @@ struct TileLoad {
             }
         }
     }
-    // the tile at p0 (TWO: its second half at p1), whose first k_left k indices exist
-    __device__ __forceinline__ void issue(unsigned lds, int wave, const char *p0, const char *p1, int k_left) const {
-        const u32x4 r0 = descriptor(p0), r1 = descriptor(TWO ? p1 : p0);
-#pragma unroll
-        for (int it = 0; it < NI; it++) {
-            const unsigned o = k_left >= KSTEP || kc[it] < k_left ? off[it] : TG_OUTSIDE;
-            load_to_lds(lds + (it * WAVES + wave) * 1024, o, TWO && it >= NI / 2 ? r1 : r0);
-        }
+    // instruction `it` of the tile at p0 (TWO: its second half at p1), whose first k_left k indices exist
+    __device__ __forceinline__ void issue(unsigned lds, int wave, int it, const char *p0, const char *p1, int k_left) const {
+        const unsigned o = k_left >= KSTEP || kc[it] < k_left ? off[it] : TG_OUTSIDE;
+        load_to_lds(lds + (it * WAVES + wave) * 1024, o, descriptor(TWO && it >= NI / 2 ? p1 : p0));
     }
-    // 16 bytes of a lane: sub-step kk (0: the first half of the step's k indices, 1: the second) of the fragment whose first row is `row0`;
-    // IS_B: of the pair's fragment `half`
-    static __device__ __forceinline__ u32x4 fragment(const char *lds, int row0, int half, int kk, int lane) {
+    // A lane's 16 bytes of the fragment whose first row is row0 (IS_B: of the pair's fragment `half`), sub-step kk (0: the first 64 bytes of k,
+    // 1: the next): where they begin in the tile
+    static __device__ __forceinline__ unsigned address(int row0, int half, int kk, int lane) {
         const int i = lane & 15, q = lane >> 4;
-        u32x4 f;
         if constexpr (!ALONG_ROWS) {
             const int row = IS_B ? row0 + 8 * (i >> 2) + 4 * half + (i & 3) : row0 + i;
-            f = *(const u32x4 *)(lds + row * TG_STEP_BYTES + (((4 * kk + q) ^ swizzle_k<IS_B>(row)) << 4));
+            return row * SB + (((4 * kk + q) ^ swizzle_k<IS_B, SB>(row)) << 4);
         } else if constexpr (ES == 2) {
-            // the lane's address: k index i / 4 of the group's four, rows 4*(i % 4) .. +3 of the fragment's sixteen
-            const int a = i & 3, row = IS_B ? row0 + 8 * a + 4 * half : row0 + 4 * a;
+            // for the transposing read: k index i / 4 of the group's four, rows 4*(i % 4) .. +3 of the fragment's sixteen
+            const int a = i & 3, row = IS_B ? row0 + 8 * a + 4 * half : row0 + 4 * a, k = 32 * kk + 8 * q + (i >> 2);
+            return k * (R * ES) + (((row >> 3) ^ swizzle_rows<IS_B, ES, R>(k)) << 4) + (row & 4) * 2;
+        } else {
+            const int row = IS_B ? row0 + 8 * (i >> 2) + 4 * half + (i & 3) : row0 + i, k = 16 * kk + 4 * q;
+            return k * (R * ES) + (((row >> 2) ^ swizzle_rows<IS_B, ES, R>(k)) << 4) + (row & 3) * 4;
+        }
+    }
+    // ... and what is there (the swizzle is the same for all that is read)
+    static __device__ __forceinline__ u32x4 read(const __attribute__((address_space(3))) char *p) {
+        u32x4 f;
+        if constexpr (!ALONG_ROWS) f = *(const __attribute__((address_space(3))) u32x4 *)p;
+        else if constexpr (ES == 2) {
             s16x4 h[2];
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                const int k = 32 * kk + 8 * q + 4 * j + (i >> 2);
-                const char *p = lds + k * (R * ES) + (((row >> 3) ^ swizzle_rows<IS_B, ES, R>(k)) << 4) + (row & 4) * 2;
-                h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
-            }
+            for (int j = 0; j < 2; j++) h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p + j * 4 * R * ES));
             __builtin_memcpy(&f, h, 16);
-        } else {
-            const int row = IS_B ? row0 + 8 * (i >> 2) + 4 * half + (i & 3) : row0 + i;
+        } else
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const int k = 16 * kk + 4 * q + j;
-                f[j] = *(const unsigned *)(lds + k * (R * ES) + (((row >> 2) ^ swizzle_rows<IS_B, ES, R>(k)) << 4) + (row & 3) * 4);
-            }
-        }
+            for (int j = 0; j < 4; j++) f[j] = *(const __attribute__((address_space(3))) unsigned *)(p + j * R * ES);
         return f;
+    }
+    static __device__ __forceinline__ u32x4 fragment(const char *tile, int row0, int half, int kk, int lane) {
+        return read((const __attribute__((address_space(3))) char *)tile + address(row0, half, kk, lane));
     }
 };
 
@@ -260,64 +264,248 @@ __device__ __forceinline__ int xcd_order(int wg, int total) {
     return x * per + (x < rest ? x : rest) + i;
 }
 
-// KG: groups of waves that share the k axis of a tile step by step, each with LDS stages of its own; group 0 adds up
-template <class T, int BM, int BN, int WM, int WN, int KG, bool A_ROWS, bool B_ROWS, int EPI>
-__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_kernel(GemmArgs G) {
-    constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32;
+// A workgroup's tile and its walk along the sources' k axes
+template <class T, int BM, int BN, bool A_ROWS, bool B_ROWS, int EPI, class LA, class LB, int EVERY>
+struct TileWalk {
+    static constexpr bool GATE = EPI == EPI_GATE;
+    const GemmProblem *P;
+    int m0, n0;
+    LA la;
+    LB lb;
+    int per_src, s0, s1, src, step;  // step: the next one to be issued, within its source
+    size_t a_step, b_step, a_tile, b_tile;
+    const char *pa, *pb, *pb1;
+    int wave;
+
+    __device__ __forceinline__ TileWalk(const GemmArgs &G, int wave_, int lane, int group) : wave(wave_) {
+        int tile = xcd_order(blockIdx.x, gridDim.x), pi = 0;
+        while (pi + 1 < G.n_problems && tile >= G.first[pi + 1]) pi++;
+        tile -= G.first[pi];
+        P = &G.p[pi];
+        constexpr int GROUP = 8;
+        const int band = tile / (GROUP * P->tiles_n), in_band = tile % (GROUP * P->tiles_n);
+        const int band_rows = min(GROUP, P->tiles_m - band * GROUP);
+        m0 = (band * GROUP + in_band % band_rows) * BM;
+        n0 = in_band / band_rows * (GATE ? BN / 2 : BN);
+        la.init(wave, lane, P->lda, P->M - m0);
+        lb.init(wave, lane, P->ldb, P->N - n0);
+        // steps s0 .. s1 - 1 of the sources', one source behind the other
+        per_src = (P->K + LA::KSTEP - 1) / LA::KSTEP;
+        const int steps = per_src * P->nsrc;
+        s0 = (int)((long long)steps * blockIdx.y / G.splits);
+        s1 = (int)((long long)steps * (blockIdx.y + 1) / G.splits);
+        a_step = A_ROWS ? LA::KSTEP * P->lda : LA::KSTEP * sizeof(T);
+        b_step = B_ROWS ? LA::KSTEP * P->ldb : LA::KSTEP * sizeof(T);
+        a_tile = A_ROWS ? (size_t)m0 * sizeof(T) : (size_t)m0 * P->lda;
+        b_tile = B_ROWS ? (size_t)n0 * sizeof(T) : (size_t)n0 * P->ldb;
+        src = 0;
+        step = s0 + group;
+        enter();
+    }
+    __device__ __forceinline__ void enter() {
+        while (step >= per_src && src + 1 < P->nsrc) {
+            step -= per_src;
+            src++;
+        }
+        pa = P->a[src] + a_tile + step * a_step;
+        pb = P->b[src] + b_tile + step * b_step;
+        pb1 = GATE ? P->b[1] + b_tile + step * b_step : nullptr;
+    }
+    static constexpr int LOADS = LA::NI + LB::NI;
+    // load instruction `l` of LOADS of the next step's tiles
+    __device__ __forceinline__ void issue(unsigned lds, int l) const {
+        const int k_left = P->K - step * LA::KSTEP;
+        if (l < LA::NI) la.issue(lds, wave, l, pa, nullptr, k_left);
+        else lb.issue(lds + LA::BYTES, wave, l - LA::NI, pb, pb1, k_left);
+    }
+    // moves on by EVERY steps
+    __device__ __forceinline__ void advance() {
+        step += EVERY;
+        if (EPI == EPI_STORE && step >= per_src && src + 1 < P->nsrc) return enter();
+        pa += EVERY * a_step;
+        pb += EVERY * b_step;
+        if constexpr (GATE) pb1 += EVERY * b_step;
+    }
+    __device__ __forceinline__ void issue_all(unsigned lds) {
+#pragma unroll
+        for (int l = 0; l < LOADS; l++) issue(lds, l);
+        advance();
+    }
+    // first LDS row of a wave's fragment pair p of B; GATE: even pairs are of the gate's weights, odd ones of the other's
+    template <int WN> static __device__ __forceinline__ int b_row(int wn, int p) { return GATE ? p % 2 * (BN / 2) + wn * (WN / 2) + p / 2 * 32 : wn * WN + 32 * p; }
+};
+
+// A wave's results to memory, 8 neighbouring columns at a time
+template <class T, int EPI, int FM, int PAIRS, int WN>
+__device__ __forceinline__ void write_tile(const GemmArgs &G, const GemmProblem &P, int m_wave, int n0, int wn, int lane, const f32x4 (&acc)[FM][2 * PAIRS]) {
     constexpr bool GATE = EPI == EPI_GATE;
-    typedef TileLoad<T, BM, A_ROWS, false, WAVES, false> LA;
-    typedef TileLoad<T, BN, B_ROWS, true, WAVES, GATE> LB;
+    static_assert(!GATE || PAIRS % 2 == 0, "a wave holds the same columns of both products");
+    const int i = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int f = 0; f < FM; f++) {
+        const int m = m_wave + 16 * f + i;
+        if (m >= P.M) continue;
+        auto eight = [&](int p, float (&v)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] = acc[f][2 * p + e / 4][e % 4];
+        };
+        float v0[8], v1[8];
+        if constexpr (GATE) {
+#pragma unroll
+            for (int p = 0; p < PAIRS; p += 2) {
+                const int n = n0 + wn * (WN / 2) + 16 * p + 8 * q;
+                if (n >= P.N) continue;
+                eight(p, v0);
+                eight(p + 1, v1);
+                if (G.splits > 1) {
+                    float *o = P.part + ((size_t)blockIdx.y * 2 * P.M + m) * P.ld_part + n;
+                    store_oct(o, v0);
+                    store_oct(o + (size_t)P.M * P.ld_part, v1);
+                } else
+                    epilogue8<T, EPI>(P.epi, m, n, v0, v1);
+            }
+        } else {
+#pragma unroll
+            for (int p = 0; p < PAIRS; p++) {
+                const int n = n0 + wn * WN + 32 * p + 8 * q;
+                if (n >= P.N) continue;
+                eight(p, v0);
+                if (G.splits > 1) store_oct(P.part + ((size_t)blockIdx.y * P.M + m) * P.ld_part + n, v0);
+                else epilogue8<T, EPI>(P.epi, m, n, v0, v0);
+            }
+        }
+    }
+}
+
+// Large tiles, two LDS stages of 128 bytes of k.  A step's products come in four quarters (two halves of k, two halves of A's
+// rows); while one quarter is formed, the next one's fragments come from LDS.  With the third quarter a wave has read all of
+// its stage, and the other stage has arrived: the step's one barrier stands there, behind it the last quarter is formed while
+// the next step's first fragments are read and the tiles of the step after that are requested into the stage just left.
+// The requests stand between that quarter's products, not at once: a load instruction keeps the memory path busy for 16 cycles.
+template <class T, int BM, int BN, int WM, int WN, bool A_ROWS, bool B_ROWS, int EPI>
+__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) gemm_kernel(GemmArgs G) {
+    constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32, SB = 128, HALF = FM / 2;
+    typedef TileLoad<T, BM, SB, A_ROWS, false, WAVES, false> LA;
+    typedef TileLoad<T, BN, SB, B_ROWS, true, WAVES, EPI == EPI_GATE> LB;
+    typedef TileWalk<T, BM, BN, A_ROWS, B_ROWS, EPI, LA, LB, 1> Walk;
+    constexpr int STAGE = LA::BYTES + LB::BYTES, LOADS = Walk::LOADS;
+    __shared__ __attribute__((aligned(1024))) char stages[2 * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN);
+    Walk w(G, wave, lane, 0);
+    const int n = w.s1 - w.s0;
+
+    f32x4 acc[FM][2 * PAIRS];
+#pragma unroll
+    for (int i = 0; i < FM; i++)
+#pragma unroll
+        for (int j = 0; j < 2 * PAIRS; j++) acc[i][j] = f32x4{0, 0, 0, 0};
+    u32x4 a[FM], b[2][2 * PAIRS];
+    // Lane addresses in LDS, of the stage at hand (an LDS instruction's offset does not reach the other one; the addresses are kept from the
+    // compiler, which would hold a set of registers for each).  Along k all fragments of a half step lie at constant distances,
+    // along rows the halves do, and the swizzle gives each fragment its own address
+    typedef const __attribute__((address_space(3))) char *Lds;
+    constexpr int NA = A_ROWS ? FM : 2, NB = !B_ROWS ? 2 : sizeof(T) == 2 ? PAIRS : 2 * PAIRS;
+    const unsigned lds = lds_address(stages);
+    unsigned at_a[NA], at_b[NB];
+#pragma unroll
+    for (int f = 0; f < NA; f++) at_a[f] = lds + (A_ROWS ? LA::address(wm + 16 * f, 0, 0, lane) : LA::address(wm, 0, f, lane));
+#pragma unroll
+    for (int f = 0; f < NB; f++) {
+        const int p = NB == PAIRS ? f : f / 2, h = NB == PAIRS ? 0 : f % 2;
+        at_b[f] = lds + LA::BYTES + (B_ROWS ? LB::address(Walk::template b_row<WN>(wn, p), h, 0, lane) : LB::address(Walk::template b_row<WN>(wn, 0), 0, f, lane));
+    }
+    auto move = [&](int by) {
+#pragma unroll
+        for (int f = 0; f < NA; f++) {
+            at_a[f] += by;
+            asm volatile("" : "+v"(at_a[f]));
+        }
+#pragma unroll
+        for (int f = 0; f < NB; f++) {
+            at_b[f] += by;
+            asm volatile("" : "+v"(at_b[f]));
+        }
+    };
+    constexpr int KHALF = LA::KSTEP / 2;  // k indices of a half step
+    auto read_a = [&](int f, int kk) {
+        a[f] = LA::read((Lds)(uintptr_t)at_a[A_ROWS ? f : kk] + (A_ROWS ? kk * KHALF * BM * (int)sizeof(T) : f * 16 * SB));
+    };
+    // B's fragments of a half step and the first half of A's; the second half of A's
+    auto read_first = [&](int kk) {
+#pragma unroll
+        for (int p = 0; p < PAIRS; p++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const Lds base = (Lds)(uintptr_t)at_b[!B_ROWS ? kk : NB == PAIRS ? p : 2 * p + h];
+                const int row = Walk::template b_row<WN>(0, p) - Walk::template b_row<WN>(0, 0);
+                b[kk][2 * p + h] = LB::read(base + (!B_ROWS ? (row + 4 * h) * SB : kk * KHALF * BN * (int)sizeof(T) + (NB == PAIRS ? 8 * h : 0)));
+            }
+#pragma unroll
+        for (int i = 0; i < HALF; i++) read_a(i, kk);
+    };
+    auto read_second = [&](int kk) {
+#pragma unroll
+        for (int i = HALF; i < FM; i++) read_a(i, kk);
+    };
+    // a quarter's products; among them the load instructions l0 .. l1 - 1 of a later step's tiles
+    auto multiply = [&](int kk, int from, int l0, int l1, unsigned stage) {
+#pragma unroll
+        for (int i = 0; i < HALF; i++) {
+#pragma unroll
+            for (int j = 0; j < 2 * PAIRS; j++) acc[from + i][j] = mma<T>(b[kk][j], a[from + i], acc[from + i][j]);
+#pragma unroll
+            for (int l = l0; l < l1; l++)
+                if ((l - l0) * HALF / (l1 - l0) == i) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    w.issue(stage, l);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        }
+    };
+    // Requests run up to two steps past the last one: they bring zeros, or k indices of another part, to stages that nobody reads any more
+    w.issue_all(lds);
+    w.issue_all(lds + STAGE);
+    wait_loads<LOADS>();
+    wave_barrier();
+    read_first(0);
+    int other = STAGE;  // from the stage at hand to the other one
+    unsigned stage = lds;
+    for (int t = 0; t < n; t++) {
+        read_second(0);
+        multiply(0, 0, 0, 0, 0);
+        read_first(1);
+        multiply(0, HALF, 0, 0, 0);
+        read_second(1);
+        multiply(1, 0, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);  // the products of what was read stay before
+        tile_barrier();
+        move(other);
+        read_first(0);
+        multiply(1, HALF, 0, LOADS, stage);
+        w.advance();
+        stage += other;
+        other = -other;
+    }
+    wait_loads<0>();
+    write_tile<T, EPI, FM, PAIRS, WN>(G, *w.P, w.m0 + wm, w.n0, wn, lane, acc);
+}
+
+// Small tiles, for products that are bound by latency: KG groups of waves share the k axis step by step, each with two LDS
+// stages of 128 bytes of k of its own; group 0 adds up the groups' sums in their order.
+template <class T, int BM, int BN, int WM, int WN, int KG, bool A_ROWS, bool B_ROWS, int EPI>
+__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_small_kernel(GemmArgs G) {
+    constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32, SB = 128;
+    typedef TileLoad<T, BM, SB, A_ROWS, false, WAVES, false> LA;
+    typedef TileLoad<T, BN, SB, B_ROWS, true, WAVES, EPI == EPI_GATE> LB;
+    typedef TileWalk<T, BM, BN, A_ROWS, B_ROWS, EPI, LA, LB, KG> Walk;
     constexpr int STAGE = LA::BYTES + LB::BYTES;
     __shared__ __attribute__((aligned(1024))) char stages[KG * 2 * STAGE];
     const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave_of_all % WAVES, group = wave_of_all / WAVES;
     char *const stage0 = stages + group * 2 * STAGE, *const stage1 = stage0 + STAGE;
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN);
+    Walk w(G, wave, lane, group);
 
-    int tile = xcd_order(blockIdx.x, gridDim.x), pi = 0;
-    while (pi + 1 < G.n_problems && tile >= G.first[pi + 1]) pi++;
-    tile -= G.first[pi];
-    const GemmProblem &P = G.p[pi];
-    constexpr int GROUP = 8;
-    const int band = tile / (GROUP * P.tiles_n), in_band = tile % (GROUP * P.tiles_n);
-    const int band_rows = min(GROUP, P.tiles_m - band * GROUP);
-    const int tm = band * GROUP + in_band % band_rows, tn = in_band / band_rows;
-    constexpr int COLS = GATE ? BN / 2 : BN;  // results' columns of a tile
-    const int m0 = tm * BM, n0 = tn * COLS;
-
-    LA la;
-    LB lb;
-    la.init(wave, lane, P.lda, P.M - m0);
-    lb.init(wave, lane, P.ldb, P.N - n0);
-    // k indices [step s0, step s1) of the sources' steps, one behind the other
-    const int K = P.K, per_src = (K + LA::KSTEP - 1) / LA::KSTEP, steps = per_src * P.nsrc;
-    const int s0 = (int)((long long)steps * blockIdx.y / G.splits), s1 = (int)((long long)steps * (blockIdx.y + 1) / G.splits);
-    const size_t a_step = A_ROWS ? LA::KSTEP * P.lda : TG_STEP_BYTES, b_step = B_ROWS ? LA::KSTEP * P.ldb : TG_STEP_BYTES;
-    const size_t a_tile = A_ROWS ? (size_t)m0 * sizeof(T) : (size_t)m0 * P.lda, b_tile = B_ROWS ? (size_t)n0 * sizeof(T) : (size_t)n0 * P.ldb;
-    int src = 0, step = s0 + group;  // of the source
-    auto enter = [&]() {
-        while (step >= per_src && src + 1 < P.nsrc) {
-            step -= per_src;
-            src++;
-        }
-    };
-    enter();
-    const char *pa = P.a[src] + a_tile + step * a_step, *pb = P.b[src] + b_tile + step * b_step;
-    const char *pb1 = GATE ? P.b[1] + b_tile + step * b_step : nullptr;
-    auto issue = [&](const char *st) {
-        const unsigned at = lds_address(st);
-        const int k_left = K - step * LA::KSTEP;
-        la.issue(at, wave, pa, nullptr, k_left);
-        lb.issue(at + LA::BYTES, wave, pb, pb1, k_left);
-        pa += KG * a_step;
-        pb += KG * b_step;
-        if constexpr (GATE) pb1 += KG * b_step;
-        step += KG;
-        if (EPI == EPI_STORE && step >= per_src && src + 1 < P.nsrc) {
-            enter();
-            pa = P.a[src] + a_tile + step * a_step;
-            pb = P.b[src] + b_tile + step * b_step;
-        }
-    };
     f32x4 acc[FM][2 * PAIRS];
 #pragma unroll
     for (int i = 0; i < FM; i++)
@@ -328,12 +516,9 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_kernel(G
 #pragma unroll
         for (int kk = 0; kk < 2; kk++) {
 #pragma unroll
-            for (int p = 0; p < PAIRS; p++) {
-                // GATE: pair 0 is of the gate's weights, pair 1 of the other's
-                const int row0 = GATE ? p * (BN / 2) + wn * 32 : wn * WN + 32 * p;
-                b[2 * p] = LB::fragment(st + LA::BYTES, row0, 0, kk, lane);
-                b[2 * p + 1] = LB::fragment(st + LA::BYTES, row0, 1, kk, lane);
-            }
+            for (int p = 0; p < PAIRS; p++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) b[2 * p + h] = LB::fragment(st + LA::BYTES, Walk::template b_row<WN>(wn, p), h, kk, lane);
 #pragma unroll
             for (int i = 0; i < FM; i++) {
                 const u32x4 a = LA::fragment(st, wm + 16 * i, 0, kk, lane);
@@ -342,18 +527,16 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_kernel(G
             }
         }
     };
-    static_assert(!GATE || WN == 64, "a wave holds 32 columns of both products");
-
-    const int rounds = (s1 - s0 + KG - 1) / KG, own = (s1 - s0 - group + KG - 1) / KG;  // of the workgroup, of this group
-    if (own > 0) issue(stage0);
+    const int rounds = (w.s1 - w.s0 + KG - 1) / KG, own = (w.s1 - w.s0 - group + KG - 1) / KG;  // of the workgroup, of this group
+    if (own > 0) w.issue_all(lds_address(stage0));
     for (int r = 0; r < rounds; r += 2) {
         tile_barrier();
-        if (r + 1 < own) issue(stage1);
-        if (KG == 1 || r < own) multiply(stage0);
+        if (r + 1 < own) w.issue_all(lds_address(stage1));
+        if (r < own) multiply(stage0);
         if (r + 1 < rounds) {
             tile_barrier();
-            if (r + 2 < own) issue(stage0);
-            if (KG == 1 || r + 1 < own) multiply(stage1);
+            if (r + 2 < own) w.issue_all(lds_address(stage0));
+            if (r + 1 < own) multiply(stage1);
         }
     }
     if constexpr (KG > 1) {
@@ -374,39 +557,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_kernel(G
 #pragma unroll
                 for (int j = 0; j < 2 * PAIRS; j++) acc[f][j] += sums[((g * FM + f) * 2 * PAIRS + j) * WAVES * 64 + wave * 64 + lane];
     }
-
-    const int i = lane & 15, q = lane >> 4;
-#pragma unroll
-    for (int f = 0; f < FM; f++) {
-        const int m = m0 + wm + 16 * f + i;
-        if (m >= P.M) continue;
-        auto eight = [&](int p, float (&v)[8]) {
-#pragma unroll
-            for (int e = 0; e < 8; e++) v[e] = acc[f][2 * p + e / 4][e % 4];
-        };
-        float v0[8], v1[8];
-        if constexpr (GATE) {
-            const int n = n0 + wn * 32 + 8 * q;
-            if (n >= P.N) continue;
-            eight(0, v0);
-            eight(1, v1);
-            if (G.splits > 1) {
-                float *o = P.part + ((size_t)blockIdx.y * 2 * P.M + m) * P.ld_part + n;
-                store_oct(o, v0);
-                store_oct(o + (size_t)P.M * P.ld_part, v1);
-            } else
-                epilogue8<T, EPI>(P.epi, m, n, v0, v1);
-        } else {
-#pragma unroll
-            for (int p = 0; p < PAIRS; p++) {
-                const int n = n0 + wn * WN + 32 * p + 8 * q;
-                if (n >= P.N) continue;
-                eight(p, v0);
-                if (G.splits > 1) store_oct(P.part + ((size_t)blockIdx.y * P.M + m) * P.ld_part + n, v0);
-                else epilogue8<T, EPI>(P.epi, m, n, v0, v0);
-            }
-        }
-    }
+    write_tile<T, EPI, FM, PAIRS, WN>(G, *w.P, w.m0 + wm, w.n0, wn, lane, acc);
 }
 
 // Sum of the parts of a split k axis, always in the same order, and the epilogue
