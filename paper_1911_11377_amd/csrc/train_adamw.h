@@ -59,6 +59,9 @@ template <bool WHOLE, class T> __device__ __forceinline__ void store4(T *p, int6
 template <class T> __device__ __forceinline__ bool at4(const T *p) { return ((uintptr_t)p & (4 * sizeof(T) - 1)) == 0; }
 
 // largest word of a wave: rotations by 1, 2, 4, 8 within rows of 16 lanes, then the four rows' values
+#ifdef CKKSMI_EMULATE
+#define wave_max emu_wave_max
+#else
 __device__ __forceinline__ unsigned wave_max(unsigned v) {
 #define TA_ROTATED(n) \
     { \
@@ -75,6 +78,7 @@ __device__ __forceinline__ unsigned wave_max(unsigned v) {
     }
     return m;
 }
+#endif
 
 // 8-bit codes: FRACTION bits behind the leading one, 4 bits of exponent, values in units; see ckksmi_train.h.  The code is the upper
 // part of the word of a 32-bit number scaled by 2^-(126 + FRACTION): codes without an exponent are its subnormal numbers
@@ -233,7 +237,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwArgs A) {
     typedef typename std::conditional<BITS == 8, unsigned char, float>::type State;
     const bool aligned = at4((P *)t.p) && at4((const G *)t.grad) && at4((State *)t.m) && at4((State *)t.v) && at4((const __bf16 *)t.copy);
     const unsigned tensor = (unsigned)(A.tensor0 + lo);
-    int64_t first = begin + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 256;
+    int64_t first = begin + TG_UNIFORM((int)(threadIdx.x >> 6)) * 256;
     if (aligned && begin + TA_CHUNK <= t.n) return adamw_chunk<P, G, BITS, true, TA_CHUNK / 1024>(A, t, first, tensor);
     // a tensor's end: its whole blocks without conditions likewise
 #pragma unroll 1
@@ -249,7 +253,7 @@ struct ReadStatesArgs {
     int n;
 };
 template <bool WHOLE> __device__ __forceinline__ void adamw_read_chunk(const ReadStatesArgs::One &t, int64_t begin) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = TG_UNIFORM((int)(threadIdx.x >> 6));
     // all blocks are requested before the first is written
     constexpr int BLOCKS = TA_CHUNK / 1024;
     unsigned char mc[BLOCKS][4], vc[BLOCKS][4];

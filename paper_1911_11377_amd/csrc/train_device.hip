@@ -88,6 +88,9 @@ struct Shape { int tile, splits; };
 struct TileShape { int bm, bn; };
 constexpr TileShape kTiles[3] = {{256, 256}, {128, 128}, {32, 128}};
 constexpr int kMaxSplits = 32;
+#ifndef TG_ENOUGH_TILES
+#define TG_ENOUGH_TILES 192  // three quarters of the compute units (the tests' stand-in sets it)
+#endif
 
 int tiles_of(const GemmProblem &p, const TileShape &t, bool gate, GemmProblem *out) {
     const int cols = gate ? t.bn / 2 : t.bn;
@@ -96,20 +99,30 @@ int tiles_of(const GemmProblem &p, const TileShape &t, bool gate, GemmProblem *o
     return tm * tn;
 }
 
-// The largest tile of which there are enough for most compute units; below that, tiles of 32 rows whose steps are shared by four groups of waves
-// (small products, bound by latency), or larger tiles with the k axis in parts where the operands' bytes count
+inline int k_steps(const GemmProblem &p, size_t es) { return (int)(((size_t)p.K * es + 127) / 128) * p.nsrc; }  // of 128 bytes
+
+// Tile and parts of the k axis.  Measured, us of one pass against the best (bf16 unless said):
+//   enough 256 x 256 tiles for three quarters of the compute units: those
+//       (gate, 2048 rows, 1024 -> 4096: 256 x 256 0, 128 x 128 +0.5, 32 x 128 +16)
+//   enough 128 x 128 tiles likewise: those, the k axis whole (dx, 16384 rows, 500 -> 200: whole 0, two parts +7); f32, which the matrix cores
+//       bound rather than the operands' bytes, from two a compute unit on (weights' gradients, 500 rows of 2000 x 1000, 304 tiles: 32 x 128 -17 of 137)
+//   few tiles of much work: 128 x 128 with the k axis in parts (2048 x 1024 from 4096: 4 parts 0, 2 parts +3, 32 x 128 whole +4, 256 x 256 in 4 parts +9)
+//   else 32 x 128, in parts where that leaves compute units idle
+//       (f32 gate, 1024 rows, 3136 -> 256: 2 parts 0, 4 and 8 parts +2; 128 x 128 in 8 parts +5, in 16 +11)
 Shape choose(const GemmProblem *p, int n, bool gate, size_t es) {
-    int tiles[3] = {0, 0, 0};
+    long long tiles[3] = {0, 0, 0};
     double flops = 0;
     for (int i = 0; i < n; i++) {
         for (int t = 0; t < 3; t++) tiles[t] += tiles_of(p[i], kTiles[t], gate, nullptr);
         flops += 2.0 * p[i].M * p[i].N * p[i].K * (gate ? 2 : p[i].nsrc);
     }
-    const int steps = (int)(((size_t)p[0].K * es + 127) / 128) * p[0].nsrc;  // of 128 bytes
-    if (es == 2 && tiles[0] >= 192) return Shape{0, 1};
-    if (tiles[1] >= 192) return Shape{1, std::max(1, std::min(512 / tiles[1], steps / 8))};
-    if (flops > (es == 2 ? 4e9 : 1e9) && p[0].M > 64) return Shape{1, std::max(1, std::min(std::min(512 / std::max(1, tiles[1]), steps / 4), kMaxSplits))};
-    return Shape{2, std::max(1, std::min(std::min(256 / std::max(1, tiles[2]), steps / 16), kMaxSplits))};
+    for (long long &t : tiles) t = std::max(t, 1LL);
+    const int steps = k_steps(p[0], es);
+    auto parts = [&](long long wanted, int least_steps) { return (int)std::max(1LL, std::min(std::min(wanted, (long long)steps / least_steps), (long long)kMaxSplits)); };
+    if (es == 2 && tiles[0] >= TG_ENOUGH_TILES) return Shape{0, 1};
+    if (tiles[1] >= (es == 2 ? TG_ENOUGH_TILES : 8 * TG_ENOUGH_TILES / 3)) return Shape{1, 1};
+    if (es == 2 && flops > 4e9 && p[0].M > 64) return Shape{1, parts(512 / tiles[1], 4)};
+    return Shape{2, parts(384 / tiles[2], 8)};
 }
 
 size_t part_bytes(const GemmProblem &p, int splits, bool gate) {
@@ -141,7 +154,10 @@ void launch_gemm(ckksmi_ctx *c, GemmProblem *p, int n, Carve w, hipStream_t st) 
     if constexpr (sizeof(T) == 2)
         if (s.tile == 0) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 256, 256, 128, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(512), st, G);
     if (s.tile == 1) KL(c, CKKSMI_K_GEMM, flops, (gemm_kernel<T, 128, 128, 64, 64, A_ROWS, B_ROWS, EPI>), grid, dim3(256), st, G);
-    if (s.tile == 2) KL(c, CKKSMI_K_GEMM, flops, (gemm_small_kernel<T, 32, 128, 16, 64, 4, A_ROWS, B_ROWS, EPI>), grid, dim3(1024), st, G);
+    // four groups of waves take a compute unit each: where there are more tiles than those, or few steps to share, one group a tile
+    const bool groups = s.tile == 2 && total * s.splits <= 256 && k_steps(p[0], sizeof(T)) > 2 * s.splits;
+    if (groups) KL(c, CKKSMI_K_GEMM, flops, (gemm_small_kernel<T, 32, 128, 16, 64, 4, A_ROWS, B_ROWS, EPI>), grid, dim3(1024), st, G);
+    else if (s.tile == 2) KL(c, CKKSMI_K_GEMM, flops, (gemm_small_kernel<T, 32, 128, 16, 64, 1, A_ROWS, B_ROWS, EPI>), grid, dim3(256), st, G);
     if (s.splits > 1) KL(c, CKKSMI_K_GEMM_JOIN, flops, (gemm_join_kernel<T, EPI>), dim3(join, n), dim3(256), st, G);
 }
 

@@ -161,20 +161,47 @@ template <bool IS_B, int ES, int R> __device__ __forceinline__ int swizzle_rows(
 }
 
 // 16 bytes a lane from a descriptor's memory to LDS: lane l's to lds + 16 l.  In assembly, so that the compiler, which takes every
-// such load for a write to all of the LDS, does not wait for it before it reads the other stage: tile_barrier() waits
+// such load for a write to all of the LDS, does not wait for it before it reads the other stage: tile_barrier() waits.
+// (No register is written by it.)
+#ifdef CKKSMI_EMULATE
+#define load_to_lds emu_load_to_lds
+#define mfma_bf16 emu_mfma_bf16
+#define mfma_f16 emu_mfma_f16
+#define mfma_f32 emu_mfma_f32
+static inline u32x4 descriptor(const char *p) { return u32x4{(unsigned)(uintptr_t)p, (unsigned)((uintptr_t)p >> 32), 0x7ffffff0u, 0}; }
+template <int N> static inline void wait_loads() { emu_wait_loads(N); }
+static inline void wave_barrier() { __syncthreads(); }
+static inline void tile_barrier() { emu_wait_loads(0); __syncthreads(); }
+static inline LdsAddress lds_address(const char *p) { return (uintptr_t)p; }
+static inline LdsPointer lds_pointer(LdsAddress a) { return (const char *)a; }
+static inline u32x4 lds_read16(LdsPointer p) { return *(const u32x4 *)emu_lds_check(p, 16); }
+static inline unsigned lds_read4(LdsPointer p) { return *(const unsigned *)emu_lds_check(p, 4); }
+static inline s16x4 lds_read_transposed(LdsPointer p) { return emu_read_transposed(emu_lds_check(p, 8)); }
+#else
 __device__ __forceinline__ void load_to_lds(unsigned lds, unsigned offset, u32x4 descriptor) {
     asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(descriptor) : "memory");
 }
+#define mfma_bf16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
+#define mfma_f16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0)
+#define mfma_f32(a, b, c) __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0)
 __device__ __forceinline__ u32x4 descriptor(const char *p) {
     const uint64_t a = (uint64_t)p;
     return u32x4{(unsigned)a, (unsigned)(a >> 32) & 0xffffu, 0x7ffffff0u, 0x00027000u};
 }
-// All but the wave's newest N loads have arrived, and all but its newest READS LDS reads
-template <int N, int READS = 15> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)" ::"n"(N), "n"(READS) : "memory"); }
+// All but the wave's newest N loads have arrived
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void wave_barrier() { asm volatile("s_barrier" ::: "memory"); }
 // Every wave's loads to LDS have arrived, and every wave has read what it read before
 __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-__device__ __forceinline__ unsigned lds_address(const char *p) { return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
+__device__ __forceinline__ LdsAddress lds_address(const char *p) { return (unsigned)(uintptr_t)(LdsPointer)p; }
+__device__ __forceinline__ LdsPointer lds_pointer(LdsAddress a) { return (LdsPointer)(uintptr_t)a; }
+__device__ __forceinline__ u32x4 lds_read16(LdsPointer p) { return *(const __attribute__((address_space(3))) u32x4 *)p; }
+__device__ __forceinline__ unsigned lds_read4(LdsPointer p) { return *(const __attribute__((address_space(3))) unsigned *)p; }
+// a group of 16 lanes, lane i at 4 values of row i / 4: lane i gets the rows' values i
+__device__ __forceinline__ s16x4 lds_read_transposed(LdsPointer p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
+}
+#endif
 
 // Loads of one operand's tiles of R rows: what a lane needs to know, found once
 template <class T, int R, int SB, bool ALONG_ROWS, bool IS_B, int WAVES, bool TWO>
@@ -206,7 +233,7 @@ struct TileLoad {
         }
     }
     // instruction `it` of the tile at p0 (TWO: its second half at p1), whose first k_left k indices exist
-    __device__ __forceinline__ void issue(unsigned lds, int wave, int it, const char *p0, const char *p1, int k_left) const {
+    __device__ __forceinline__ void issue(LdsAddress lds, int wave, int it, const char *p0, const char *p1, int k_left) const {
         const unsigned o = k_left >= KSTEP || kc[it] < k_left ? off[it] : TG_OUTSIDE;
         load_to_lds(lds + (it * WAVES + wave) * 1024, o, descriptor(TWO && it >= NI / 2 ? p1 : p0));
     }
@@ -227,33 +254,33 @@ struct TileLoad {
         }
     }
     // ... and what is there (the swizzle is the same for all that is read)
-    static __device__ __forceinline__ u32x4 read(const __attribute__((address_space(3))) char *p) {
+    static __device__ __forceinline__ u32x4 read(LdsPointer p) {
         u32x4 f;
-        if constexpr (!ALONG_ROWS) f = *(const __attribute__((address_space(3))) u32x4 *)p;
+        if constexpr (!ALONG_ROWS) f = lds_read16(p);
         else if constexpr (ES == 2) {
             s16x4 h[2];
 #pragma unroll
-            for (int j = 0; j < 2; j++) h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p + j * 4 * R * ES));
+            for (int j = 0; j < 2; j++) h[j] = lds_read_transposed(p + j * 4 * R * ES);
             __builtin_memcpy(&f, h, 16);
         } else
 #pragma unroll
-            for (int j = 0; j < 4; j++) f[j] = *(const __attribute__((address_space(3))) unsigned *)(p + j * R * ES);
+            for (int j = 0; j < 4; j++) f[j] = lds_read4(p + j * R * ES);
         return f;
     }
     static __device__ __forceinline__ u32x4 fragment(const char *tile, int row0, int half, int kk, int lane) {
-        return read((const __attribute__((address_space(3))) char *)tile + address(row0, half, kk, lane));
+        return read((LdsPointer)tile + address(row0, half, kk, lane));
     }
 };
 
 template <class T> __device__ __forceinline__ f32x4 mma(const u32x4 &first, const u32x4 &second, f32x4 c) {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int j = 0; j < 4; j++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(first[j]), __uint_as_float(second[j]), c, 0, 0, 0);
+        for (int j = 0; j < 4; j++) c = mfma_f32(__uint_as_float(first[j]), __uint_as_float(second[j]), c);
         return c;
     } else if constexpr (__is_same(T, __bf16)) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, first), __builtin_bit_cast(bf16x8, second), c, 0, 0, 0);
+        return mfma_bf16(__builtin_bit_cast(bf16x8, first), __builtin_bit_cast(bf16x8, second), c);
     } else {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, first), __builtin_bit_cast(f16x8, second), c, 0, 0, 0);
+        return mfma_f16(__builtin_bit_cast(f16x8, first), __builtin_bit_cast(f16x8, second), c);
     }
 }
 
@@ -313,7 +340,7 @@ struct TileWalk {
     }
     static constexpr int LOADS = LA::NI + LB::NI;
     // load instruction `l` of LOADS of the next step's tiles
-    __device__ __forceinline__ void issue(unsigned lds, int l) const {
+    __device__ __forceinline__ void issue(LdsAddress lds, int l) const {
         const int k_left = P->K - step * LA::KSTEP;
         if (l < LA::NI) la.issue(lds, wave, l, pa, nullptr, k_left);
         else lb.issue(lds + LA::BYTES, wave, l - LA::NI, pb, pb1, k_left);
@@ -326,7 +353,7 @@ struct TileWalk {
         pb += EVERY * b_step;
         if constexpr (GATE) pb1 += EVERY * b_step;
     }
-    __device__ __forceinline__ void issue_all(unsigned lds) {
+    __device__ __forceinline__ void issue_all(LdsAddress lds) {
 #pragma unroll
         for (int l = 0; l < LOADS; l++) issue(lds, l);
         advance();
@@ -390,7 +417,8 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) g
     typedef TileWalk<T, BM, BN, A_ROWS, B_ROWS, EPI, LA, LB, 1> Walk;
     constexpr int STAGE = LA::BYTES + LB::BYTES, LOADS = Walk::LOADS;
     __shared__ __attribute__((aligned(1024))) char stages[2 * STAGE];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    TG_LDS(stages);
+    const int lane = threadIdx.x & 63, wave = TG_UNIFORM((int)(threadIdx.x >> 6));
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN);
     Walk w(G, wave, lane, 0);
     const int n = w.s1 - w.s0;
@@ -404,10 +432,9 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) g
     // Lane addresses in LDS, of the stage at hand (an LDS instruction's offset does not reach the other one; the addresses are kept from the
     // compiler, which would hold a set of registers for each).  Along k all fragments of a half step lie at constant distances,
     // along rows the halves do, and the swizzle gives each fragment its own address
-    typedef const __attribute__((address_space(3))) char *Lds;
     constexpr int NA = A_ROWS ? FM : 2, NB = !B_ROWS ? 2 : sizeof(T) == 2 ? PAIRS : 2 * PAIRS;
-    const unsigned lds = lds_address(stages);
-    unsigned at_a[NA], at_b[NB];
+    const LdsAddress lds = lds_address(stages);
+    LdsAddress at_a[NA], at_b[NB];
 #pragma unroll
     for (int f = 0; f < NA; f++) at_a[f] = lds + (A_ROWS ? LA::address(wm + 16 * f, 0, 0, lane) : LA::address(wm, 0, f, lane));
 #pragma unroll
@@ -419,17 +446,17 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) g
 #pragma unroll
         for (int f = 0; f < NA; f++) {
             at_a[f] += by;
-            asm volatile("" : "+v"(at_a[f]));
+            TG_OPAQUE(at_a[f]);
         }
 #pragma unroll
         for (int f = 0; f < NB; f++) {
             at_b[f] += by;
-            asm volatile("" : "+v"(at_b[f]));
+            TG_OPAQUE(at_b[f]);
         }
     };
     constexpr int KHALF = LA::KSTEP / 2;  // k indices of a half step
     auto read_a = [&](int f, int kk) {
-        a[f] = LA::read((Lds)(uintptr_t)at_a[A_ROWS ? f : kk] + (A_ROWS ? kk * KHALF * BM * (int)sizeof(T) : f * 16 * SB));
+        a[f] = LA::read(lds_pointer(at_a[A_ROWS ? f : kk]) + (A_ROWS ? kk * KHALF * BM * (int)sizeof(T) : f * 16 * SB));
     };
     // B's fragments of a half step and the first half of A's; the second half of A's
     auto read_first = [&](int kk) {
@@ -437,7 +464,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) g
         for (int p = 0; p < PAIRS; p++)
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const Lds base = (Lds)(uintptr_t)at_b[!B_ROWS ? kk : NB == PAIRS ? p : 2 * p + h];
+                const LdsPointer base = lds_pointer(at_b[!B_ROWS ? kk : NB == PAIRS ? p : 2 * p + h]);
                 const int row = Walk::template b_row<WN>(0, p) - Walk::template b_row<WN>(0, 0);
                 b[kk][2 * p + h] = LB::read(base + (!B_ROWS ? (row + 4 * h) * SB : kk * KHALF * BN * (int)sizeof(T) + (NB == PAIRS ? 8 * h : 0)));
             }
@@ -449,7 +476,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) g
         for (int i = HALF; i < FM; i++) read_a(i, kk);
     };
     // a quarter's products; among them the load instructions l0 .. l1 - 1 of a later step's tiles
-    auto multiply = [&](int kk, int from, int l0, int l1, unsigned stage) {
+    auto multiply = [&](int kk, int from, int l0, int l1, LdsAddress stage) {
 #pragma unroll
         for (int i = 0; i < HALF; i++) {
 #pragma unroll
@@ -457,9 +484,9 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) g
 #pragma unroll
             for (int l = l0; l < l1; l++)
                 if ((l - l0) * HALF / (l1 - l0) == i) {
-                    __builtin_amdgcn_sched_barrier(0);
+                    TG_SCHEDULED();
                     w.issue(stage, l);
-                    __builtin_amdgcn_sched_barrier(0);
+                    TG_SCHEDULED();
                 }
         }
     };
@@ -470,7 +497,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) g
     wave_barrier();
     read_first(0);
     int other = STAGE;  // from the stage at hand to the other one
-    unsigned stage = lds;
+    LdsAddress stage = lds;
     for (int t = 0; t < n; t++) {
         read_second(0);
         multiply(0, 0, 0, 0, 0);
@@ -478,7 +505,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) g
         multiply(0, HALF, 0, 0, 0);
         read_second(1);
         multiply(1, 0, 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);  // the products of what was read stay before
+        TG_SCHEDULED();  // the products of what was read stay before
         tile_barrier();
         move(other);
         read_first(0);
@@ -501,7 +528,8 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_small_ke
     typedef TileWalk<T, BM, BN, A_ROWS, B_ROWS, EPI, LA, LB, KG> Walk;
     constexpr int STAGE = LA::BYTES + LB::BYTES;
     __shared__ __attribute__((aligned(1024))) char stages[KG * 2 * STAGE];
-    const int lane = threadIdx.x & 63, wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave_of_all % WAVES, group = wave_of_all / WAVES;
+    TG_LDS(stages);
+    const int lane = threadIdx.x & 63, wave_of_all = TG_UNIFORM((int)(threadIdx.x >> 6)), wave = wave_of_all % WAVES, group = wave_of_all / WAVES;
     char *const stage0 = stages + group * 2 * STAGE, *const stage1 = stage0 + STAGE;
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN);
     Walk w(G, wave, lane, group);
@@ -594,11 +622,17 @@ template <class T> __global__ void __launch_bounds__(256) pad_rows_kernel(CopyAr
     constexpr int EPC = 16 / sizeof(T);
     const size_t id = (size_t)(blockIdx.x - C.first) * 256 + threadIdx.x;
     if (id >= C.rows * C.chunks) return;
-    const size_t r = id / C.chunks;
-    const int c = (int)(id % C.chunks) * EPC;
+    // (most copies are small enough for a 32-bit division)
+    const size_t r = id >> 32 ? id / C.chunks : (unsigned)id / (unsigned)C.chunks;
+    const int c = (int)(id - r * C.chunks) * EPC;
     const T *s = (const T *)(C.src + r * C.ld_src) + c;
-    T v[EPC];
+    u32x4 w;
+    if (c + EPC <= C.cols) __builtin_memcpy(&w, s, 16);
+    else {
+        T v[EPC];
 #pragma unroll
-    for (int e = 0; e < EPC; e++) v[e] = c + e < C.cols ? s[e] : (T)0.0f;
-    *(u32x4 *)(C.dst + r * C.ld_dst + (size_t)c * sizeof(T)) = *(const u32x4 *)v;
+        for (int e = 0; e < EPC; e++) v[e] = c + e < C.cols ? s[e] : (T)0.0f;
+        __builtin_memcpy(&w, v, 16);
+    }
+    *(u32x4 *)(C.dst + r * C.ld_dst + (size_t)c * sizeof(T)) = w;
 }

@@ -35,7 +35,7 @@ template <class T, int EPI, int MT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) rows_kernel(RowsArgs R) {
     constexpr int MATS = EPI == EPI_GATE ? 2 : 1, EPC = 16 / sizeof(T), RUN = 128 / sizeof(T);
     __shared__ f32x4 sums[WAVES][MATS][MT][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = TG_UNIFORM((int)(threadIdx.x >> 6)), i = lane & 15, q = lane >> 4;
     const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
     // rows beyond the end repeat the last one: their results are not stored
     const char *w[MATS], *x[MT];
@@ -48,23 +48,51 @@ __global__ void __launch_bounds__(64 * WAVES) rows_kernel(RowsArgs R) {
     for (int a = 0; a < MATS; a++)
 #pragma unroll
         for (int t = 0; t < MT; t++) acc[a][t] = f32x4{0, 0, 0, 0};
-#pragma unroll 2
-    for (int k0 = wave * RUN; k0 < R.K; k0 += WAVES * RUN) {
-        u32x4 fw[MATS][2], fx[MT][2];
+    // a run of 128 bytes a row: two sub-steps of four chunks
+    struct Run { u32x4 w[MATS][2], x[MT][2]; };
+    auto load = [&](Run &f, int k0) {  // all of it exists
 #pragma unroll
         for (int s = 0; s < 2; s++) {
             const int k = k0 + (4 * s + q) * EPC;
 #pragma unroll
-            for (int a = 0; a < MATS; a++) fw[a][s] = row_chunk<T>(w[a], k, R.K);
+            for (int a = 0; a < MATS; a++) __builtin_memcpy(&f.w[a][s], w[a] + (size_t)k * sizeof(T), 16);
 #pragma unroll
-            for (int t = 0; t < MT; t++) fx[t][s] = row_chunk<T>(x[t], k, R.K);
+            for (int t = 0; t < MT; t++) __builtin_memcpy(&f.x[t][s], x[t] + (size_t)k * sizeof(T), 16);
         }
+    };
+    auto load_end = [&](Run &f, int k0) {  // some of it, or nothing: zeros
+        if (k0 >= R.K) {
+            f = Run{};
+            return;
+        }
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+            const int k = k0 + (4 * s + q) * EPC;
+#pragma unroll
+            for (int a = 0; a < MATS; a++) f.w[a][s] = row_chunk<T>(w[a], k, R.K);
+#pragma unroll
+            for (int t = 0; t < MT; t++) f.x[t][s] = row_chunk<T>(x[t], k, R.K);
+        }
+    };
+    auto multiply = [&](const Run &f) {
 #pragma unroll
         for (int s = 0; s < 2; s++)
 #pragma unroll
             for (int a = 0; a < MATS; a++)
 #pragma unroll
-                for (int t = 0; t < MT; t++) acc[a][t] = mma<T>(fw[a][s], fx[t][s], acc[a][t]);
+                for (int t = 0; t < MT; t++) acc[a][t] = mma<T>(f.w[a][s], f.x[t][s], acc[a][t]);
+    };
+    constexpr int AHEAD = MATS + MT <= 2 ? 4 : 2;  // runs whose loads are under way together
+    for (int k0 = wave * RUN; k0 < R.K; k0 += AHEAD * WAVES * RUN) {
+        Run f[AHEAD];
+#pragma unroll
+        for (int r = 0; r < AHEAD; r++) {
+            const int kr = k0 + r * WAVES * RUN;
+            if (kr + RUN <= R.K) load(f[r], kr);
+            else load_end(f[r], kr);
+        }
+#pragma unroll
+        for (int r = 0; r < AHEAD; r++) multiply(f[r]);
     }
 #pragma unroll
     for (int a = 0; a < MATS; a++)

@@ -1,6 +1,8 @@
 // Element types, activations and small helpers of the cleartext training kernels.
 #pragma once
+#ifndef CKKSMI_EMULATE
 #include <hip/hip_runtime.h>
+#endif
 
 #include <cstdint>
 
@@ -12,6 +14,23 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// What the kernels use of the machine beyond plain HIP; with CKKSMI_EMULATE the tests' stand-in on the CPU has it instead
+#ifdef CKKSMI_EMULATE
+typedef uintptr_t LdsAddress;
+typedef const char *LdsPointer;
+#define TG_LDS(array) emu_lds_range(array, sizeof(array))
+#define TG_OPAQUE(x) (void)0
+#define TG_SCHEDULED() (void)0
+#define TG_UNIFORM(x) (x)
+#else
+typedef unsigned LdsAddress;
+typedef const __attribute__((address_space(3))) char *LdsPointer;
+#define TG_LDS(array) (void)0
+#define TG_OPAQUE(x) asm volatile("" : "+v"(x))  // the compiler knows nothing of x's value
+#define TG_SCHEDULED() __builtin_amdgcn_sched_barrier(0)  // no instruction moves across
+#define TG_UNIFORM(x) __builtin_amdgcn_readfirstlane(x)
+#endif
 
 template <int DT> struct ElementOf;
 template <> struct ElementOf<CKKSMI_F32> { typedef float type; };
