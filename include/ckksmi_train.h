@@ -35,8 +35,9 @@ extern "C" {
  *     g = x Wg^T,  u = x Wu^T,  h = act(g) * u,  y = h Wd^T
  * x: [rows][d_in], Wg, Wu: [d_hidden][d_in], Wd: [d_out][d_hidden], y: [rows][d_out].  Elements are of `dtype`; sums,
  * activations and their derivatives are formed in 32 bits, and h is rounded to `dtype` before the last product.
- * Weights are dense; rows of x, y, dy, dx may lie further apart: ld_* elements, 0 = dense.  0 <= rows < 2^31, every
- * dimension and ld 1 .. 2^20. */
+ * Weights are dense; rows of x, y, dy, dx may lie further apart: ld_* elements, 0 = dense.  0 <= rows < 2^31 - 256,
+ * every dimension and ld 1 .. 2^20; CKKSMI_EUNSUPPORTED where a product has 2^42
+ * results or more, or the operands (counted as f32) 2^43 bytes. */
 typedef struct {
     int dtype;      /* of x, y, the weights, dy, dx and what is saved */
     int grad_dtype; /* of the weights' gradients: dtype or CKKSMI_F32 */
@@ -78,7 +79,7 @@ int ckksmi_gated_ff_backward(ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, const v
  * and 0.018 / sqrt(1 - beta2^2) for v: 8 % and, with beta2 = 0.99 and 0.999, 13 % and 40 %.)  v > 0 is never rounded to 0.
  * A block whose unit would be below 1e-36 is held as zeros, one with a value that is not finite gets unit NaN.  The step
  * itself uses m and v before they are rounded.  States start as zeros (bytes and units).
- * skip: NULL, or one device int; where it is not 0 when the step runs, the step leaves everything as it is (gradients
+ * Buffers must not overlap.  skip: NULL, or one device int; where it is not 0 when the step runs, the step leaves everything as it is (gradients
  * that overflowed). */
 #define CKKSMI_STATE_BLOCK 256
 typedef struct {

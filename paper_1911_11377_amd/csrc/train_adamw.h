@@ -1,10 +1,15 @@
 // AdamW over many tensors in one launch.
 //
-// Every element is read once and written once, with some 20 operations in between (60 with 8-bit states): memory bounds
-// the step.  A workgroup takes 4096 neighbouring elements of one tensor, found in a table of tensors that travels as a kernel
-// argument; a wave takes 256 of them at a time, 4 neighbouring ones a lane, which is one block of the 8-bit states: its
-// largest magnitudes are found among the wave's lanes and no step needs LDS or a second pass.
+// Every element is read once and written once, with some 40 operations in between (exact quotient and root among them; 100 with
+// 8-bit states).  A workgroup takes 4096 neighbouring elements of one tensor, found in a table of tensors that travels as a
+// kernel argument; a wave takes 256 of them at a time, 4 neighbouring ones a lane, which is one block of the 8-bit states: its
+// largest magnitudes are found among the wave's lanes and no step needs LDS or a second pass.  The next block is on its way
+// while one is computed; blocks that are whole and aligned take a path without conditions (with conditions 736 us instead of
+// 640 for the second case below).
 // Products and sums are rounded one by one (no fused multiply-add): an element's result depends on nothing but its inputs.
+// Measured: 32-bit states, 306M f32 parameters, bf16 gradients and copies 1.62 ms (28 bytes an element, 5.3 TB/s: what a copy
+// reaches); 8-bit states, 221M bf16 parameters 0.64 ms (10 bytes, 3.5 TB/s: bound by its instructions), read back 0.37 ms
+// (10 bytes, 6.0 TB/s, mostly writes); 160 tensors of 1 to 4M elements, 8-bit states 0.25 ms with reading back (four launches each).
 #pragma once
 #include <type_traits>
 

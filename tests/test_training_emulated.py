@@ -160,3 +160,15 @@ def test_workspace_that_is_too_small_is_refused(ctx):
             args = [a, 2 * a, 3 * a, 4 * a] + ([5 * a, 6 * a, 7 * a, 8 * a, 9 * a, 10 * a, 0] if backward else [5 * a, None])
             fn = ctx._L.ckksmi_gated_ff_backward if backward else ctx._L.ckksmi_gated_ff_forward
             assert fn(ctx._h, ff._r, *args, 11 * a, n - 1, None) == ckksmi.EWORKSPACE
+
+
+def test_sizes_that_no_grid_holds_are_refused(ctx):
+    ff = training.GatedFF(ctx, 2**20, 2**20, 2**20, BF16, "square")
+    with pytest.raises(ckksmi.CkksmiError) as e:
+        ff.workspace_bytes(2**31 - 1000)
+    assert e.value.code == ckksmi.EUNSUPPORTED
+    with pytest.raises(ckksmi.CkksmiError) as e:
+        ff.workspace_bytes(2**31 - 256)
+    assert e.value.code == ckksmi.EINVAL
+    ff = training.GatedFF(ctx, 2**19, 2**19, 2**19, BF16, "square")
+    assert ff.workspace_bytes(4096) > 2**40  # the weights' padded copies alone
