@@ -416,7 +416,7 @@ __device__ __forceinline__ void write_tile(const GemmArgs &G, const GemmProblem 
 // a quarter of the time), down 0.47 ms (1.17), dh 0.80 ms (0.69; 0.8 GB read and 0.54 GB written after the products), dx 0.84 ms
 // (1.30), weights' gradients 1.29 ms (1.28); both products of 4096^3 330 us (1.25).
 template <class T, int BM, int BN, int WM, int WN, bool A_ROWS, bool B_ROWS, int EPI>
-__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), WN > 64 ? 1 : 2) gemm_kernel(GemmArgs G) {
+__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) gemm_kernel(GemmArgs G) {
     constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32, SB = 128, HALF = FM / 2;
     typedef TileLoad<T, BM, SB, A_ROWS, false, WAVES, false> LA;
     typedef TileLoad<T, BN, SB, B_ROWS, true, WAVES, EPI == EPI_GATE> LB;
@@ -621,7 +621,7 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(GemmArgs G) {
 
 // Copies with rows padded to whole 16-byte chunks (zeros behind the last column), for operands whose rows do not begin on them: one launch for
 // all of a call's, 5.4 us for the 2.7 MB of 333 rows of 517 -> 1021 -> 129
-#define TG_COPIES 6
+#define TG_COPIES 5  // of one call: x, three weight matrices, dy
 struct CopyArgs {
     struct One { const char *src; char *dst; size_t ld_src, ld_dst; int cols, chunks; size_t rows; unsigned first; } c[TG_COPIES];
     int n;

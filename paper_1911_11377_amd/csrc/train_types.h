@@ -10,7 +10,6 @@
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
@@ -31,12 +30,6 @@ typedef const __attribute__((address_space(3))) char *LdsPointer;
 #define TG_SCHEDULED() __builtin_amdgcn_sched_barrier(0)  // no instruction moves across
 #define TG_UNIFORM(x) __builtin_amdgcn_readfirstlane(x)
 #endif
-
-template <int DT> struct ElementOf;
-template <> struct ElementOf<CKKSMI_F32> { typedef float type; };
-template <> struct ElementOf<CKKSMI_BF16> { typedef __bf16 type; };
-template <> struct ElementOf<CKKSMI_F16> { typedef _Float16 type; };
-template <int DT> using element = typename ElementOf<DT>::type;
 
 inline size_t element_bytes(int dtype) { return dtype == CKKSMI_F32 ? 4 : 2; }
 
@@ -87,12 +80,12 @@ __device__ __forceinline__ void load_oct24(const uint16_t *hi, const uint8_t *lo
 
 struct Activation { int kind; float c[4]; };
 
-// act(g) in 32 bits
+// act(g) in 32 bits (the same bits as act_both's: an answer does not depend on whether the pass saves)
 __device__ __forceinline__ float act_value(const Activation &A, float g) {
     switch (A.kind) {
         case CKKSMI_ACT_POLY: return ((A.c[3] * g + A.c[2]) * g + A.c[1]) * g + A.c[0];
         case CKKSMI_ACT_RELU: return g > 0.0f ? g : g * 0.0f;  // a NaN stays one
-        case CKKSMI_ACT_SILU: return g / (1.0f + expf(-g));
+        case CKKSMI_ACT_SILU: return g * (1.0f / (1.0f + expf(-g)));
         default: return g * (0.5f * (1.0f + erff(g * 0.70710678f)));
     }
 }

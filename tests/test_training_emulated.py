@@ -65,8 +65,9 @@ def test_block(ctx, size, dtype):
     run_block(ctx, *size, dtype)
 
 
-@pytest.mark.parametrize("size,dtype,grads,act", [((9, 24, 16, 8), BF16, F32, "silu"), ((70, 40, 24, 17), F16, F32, "gelu"), ((40, 16, 136, 8), BF16, None, "relu")],
-                         ids=["fine", "fine16", "relu"])
+@pytest.mark.parametrize("size,dtype,grads,act", [((9, 24, 16, 8), BF16, F32, "silu"), ((70, 40, 24, 17), F16, F32, "gelu"), ((40, 16, 136, 8), BF16, None, "relu"),
+                                                   ((1, 107, 8, 19), F32, None, "silu"), ((70, 33, 40, 7), F32, None, "gelu")],
+                         ids=["fine", "fine16", "relu", "silu-f32", "gelu-f32"])
 def test_block_with_other_gradients_and_activations(ctx, size, dtype, grads, act):
     run_block(ctx, *size, dtype, act, grads)
 
@@ -89,7 +90,7 @@ def test_a_split_k_axis(ctx):
 
 
 @pytest.mark.parametrize("size,dtype,grads,enough", [((130, 72, 140, 136), BF16, None, 3), ((260, 24, 70, 129), F16, F32, 3), ((200, 40, 140, 130), F32, None, 1),
-                                                     ((300, 200, 140, 264), BF16, None, 1), ((270, 72, 260, 33), F16, F32, 1)],
+                                                     ((300, 136, 140, 72), BF16, None, 1), ((270, 72, 260, 33), F16, F32, 1)],
                          ids=["128", "128-fine", "128-f32", "256", "256-fine"])
 def test_large_tiles(ctx, size, dtype, grads, enough):
     """tiles of 128 x 128 and 256 x 256 with ragged edges, k axes of one to five steps, sums of several products"""

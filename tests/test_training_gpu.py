@@ -100,6 +100,17 @@ def test_activations(ctx, act, dtype):
     b.check()
 
 
+@pytest.mark.parametrize("act", ["poly3", "relu", "silu", "gelu"])
+@pytest.mark.parametrize("rows", [1, 40, 130])
+def test_answers_do_not_depend_on_what_is_saved(ctx, act, rows):
+    b = Block(ctx, rows, 107, 72, 19, F32, act, seed=21)
+    b.forward()
+    y = b.y.clone()
+    b.y.fill_(math.nan)
+    b.forward(saved=False)
+    assert torch.equal(b.y, y)
+
+
 @pytest.mark.parametrize("size", [(4100, 72, 1600, 2000), (2048, 1024, 4096, 1024), (5000, 1100, 1030, 1536)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("dtype", [BF16, F16], ids=["bf16", "f16"])
 def test_block_of_many_tiles(ctx, size, dtype):
