@@ -162,7 +162,8 @@ template <bool IS_B, int ES, int R> __device__ __forceinline__ int swizzle_rows(
 
 // 16 bytes a lane from a descriptor's memory to LDS: lane l's to lds + 16 l.  In assembly, so that the compiler, which takes every
 // such load for a write to all of the LDS, does not wait for it before it reads the other stage: tile_barrier() waits.
-// (No register is written by it.)
+// (No vector register is written by it.  The load takes its LDS address from m0 and has to stand one wait state behind the write of m0:
+// the compiler fills none in inside a block.)
 #ifdef CKKSMI_EMULATE
 #define load_to_lds emu_load_to_lds
 #define mfma_bf16 emu_mfma_bf16
@@ -179,7 +180,7 @@ static inline unsigned lds_read4(LdsPointer p) { return *(const unsigned *)emu_l
 static inline s16x4 lds_read_transposed(LdsPointer p) { return emu_read_transposed(emu_lds_check(p, 8)); }
 #else
 __device__ __forceinline__ void load_to_lds(unsigned lds, unsigned offset, u32x4 descriptor) {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(descriptor) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(descriptor) : "memory", "m0");
 }
 #define mfma_bf16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
 #define mfma_f16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0)
