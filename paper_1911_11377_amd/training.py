@@ -70,6 +70,8 @@ class GatedFF:
             raise ValueError("expected [%s][%d] of %s, got %s of %s" % ("rows" if rows is None else rows, width, dtype, tuple(x.shape), x.dtype))
         if x.stride(1) != 1 and width > 1:
             raise ValueError("rows must be contiguous")
+        if x.shape[0] > 1 and x.stride(0) < width:  # (0, a row repeated by expand(), would be taken for dense rows)
+            raise ValueError("rows must not overlap: %d elements apart, %d wide" % (x.stride(0), width))
         return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else width
 
     def _matrix(self, w, d0, d1, dtype):
