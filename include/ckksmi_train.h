@@ -47,7 +47,7 @@ typedef struct {
     int64_t ld_x, ld_y, ld_dy, ld_dx;
 } ckksmi_gated_ff;
 
-/* bytes of workspace of the forward (backward = 0) or of either pass (backward = 1); of what a forward pass saves for the
+/* bytes of workspace of the forward (backward = 0) or of either pass (backward = 1) on up to `rows` rows (never less for more rows); of what a forward pass saves for the
  * backward pass: act(g), u act'(g) and h, 8 bytes per row and hidden unit for 16-bit types (with f32 gradients 12 for f16, 14 for bf16), 12 for f32 */
 int ckksmi_gated_ff_workspace_bytes(const ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, int backward, size_t *bytes);
 int ckksmi_gated_ff_saved_bytes(const ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, size_t *bytes);

@@ -93,6 +93,9 @@ struct Shape { int tile, splits; };
 struct TileShape { int bm, bn; };
 constexpr TileShape kTiles[3] = {{256, 256}, {128, 128}, {32, 128}};
 constexpr int kMaxSplits = 32;
+// a k axis in parts: workgroups that the parts together may come to, and steps of 128 bytes that each has at least (128 x 128, 32 x 128)
+constexpr int kParts[2] = {512, 384}, kPartSteps[2] = {4, 8};
+constexpr double kMuchWork = 4e9;  // operations
 #ifndef TG_ENOUGH_TILES
 #define TG_ENOUGH_TILES 192  // three quarters of the compute units (the tests' stand-in sets it)
 #endif
@@ -123,15 +126,28 @@ Shape choose(const GemmProblem *p, int n, bool gate, size_t es) {
     }
     for (long long &t : tiles) t = std::max(t, 1LL);
     const int steps = k_steps(p[0], es);
-    auto parts = [&](long long wanted, int least_steps) { return (int)std::max(1LL, std::min(std::min(wanted, (long long)steps / least_steps), (long long)kMaxSplits)); };
+    auto parts = [&](int t) { return (int)std::max(1LL, std::min(std::min(kParts[t - 1] / tiles[t], (long long)steps / kPartSteps[t - 1]), (long long)kMaxSplits)); };
     if (es == 2 && tiles[0] >= TG_ENOUGH_TILES) return Shape{0, 1};
     if (tiles[1] >= (es == 2 ? TG_ENOUGH_TILES : 8 * TG_ENOUGH_TILES / 3)) return Shape{1, 1};
-    if (es == 2 && flops > 4e9 && p[0].M > 64) return Shape{1, parts(512 / tiles[1], 4)};
-    return Shape{2, parts(384 / tiles[2], 8)};
+    if (es == 2 && flops > kMuchWork && p[0].M > 64) return Shape{1, parts(1)};
+    return Shape{2, parts(2)};
 }
 
 size_t part_bytes(const GemmProblem &p, int splits, bool gate) {
     return splits > 1 ? (size_t)splits * (gate ? 2 : 1) * p.M * round_up(p.N, 8) * sizeof(float) : 0;
+}
+
+// At least part_bytes() of the product on p.M rows and on any number below: fewer rows are fewer tiles, which choose() gives more parts, so
+// the need itself goes up and down with the rows.  Parts x tiles are kParts at most, a tile's results lie in bm x bn values
+// (both factors of a gate's among them), and the parts' number is bounded by the k axis, which does not depend on the rows
+size_t part_bytes_up_to(const GemmProblem &p, bool gate, size_t es) {
+    auto most = [&](int t) {
+        const size_t parts = std::min(k_steps(p, es) / kPartSteps[t - 1], kMaxSplits);
+        const size_t of_tiles = (size_t)kParts[t - 1] * kTiles[t].bm * kTiles[t].bn * sizeof(float);
+        return parts > 1 ? std::min(part_bytes(p, (int)parts, gate), of_tiles) : 0;
+    };
+    const bool much = es == 2 && 2.0 * p.M * p.N * p.K * (gate ? 2 : p.nsrc) > kMuchWork && p.M > 64;
+    return std::max(much ? most(1) : 0, most(2));
 }
 
 // Up to TG_PROBLEMS products of one kind in a launch; `w` gives the memory for a split k axis
@@ -201,11 +217,12 @@ template <class T> struct Operands {
     }
 };
 
-// the products' shapes alone, for the workspace: as the passes below form them
+// the products' shapes alone, for the workspace: as the passes below form them.  Never less for more rows: a workspace serves any number
+// of rows up to the one it was made for (the weights' gradients have the rows for their k axis, and a longer one has no fewer parts)
 size_t split_bytes(const ckksmi_gated_ff &f, bool backward) {
     const FF d(f);
     const Matrix none{nullptr, 0};
-    auto one = [&](GemmProblem p, bool gate) { return part_bytes(p, choose(&p, 1, gate, d.es).splits, gate) + 256; };
+    auto one = [&](const GemmProblem &p, bool gate) { return part_bytes_up_to(p, gate, d.es) + 256; };
     size_t most = std::max(one(product(none, none, d.M, d.H, d.K), true), one(product(none, none, d.M, d.O, d.H), false));
     if (!backward || d.M == 0) return most;
     GemmProblem dx = product(none, none, d.M, d.K, d.H);

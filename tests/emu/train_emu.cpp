@@ -231,3 +231,22 @@ extern "C" ckksmi_ctx *emu_train_context() {
     return c;
 }
 extern "C" void emu_train_context_free(ckksmi_ctx *c) { delete c; }
+
+// what the k axes in parts take of the workspace at this number of rows, largest launch of a pass
+extern "C" size_t emu_split_need(const ckksmi_gated_ff *f, int backward) {
+    const FF d(*f);
+    const Matrix none{nullptr, 0};
+    auto launch = [&](std::vector<GemmProblem> p, bool gate) {
+        const int splits = choose(p.data(), (int)p.size(), gate, d.es).splits;
+        size_t sum = 0;
+        for (const GemmProblem &q : p) sum += round_up(part_bytes(q, splits, gate), 256);
+        return sum;
+    };
+    if (!backward) return std::max(launch({product(none, none, d.M, d.H, d.K)}, true), launch({product(none, none, d.M, d.O, d.H)}, false));
+    GemmProblem dx = product(none, none, d.M, d.K, d.H), dw = product(none, none, d.H, d.K, d.M), down = product(none, none, d.O, d.H, d.M);
+    dx.nsrc = 2;
+    dw.nsrc = down.nsrc = d.parts(f->dtype);
+    return std::max(launch({dw, dw, down}, false), std::max(launch({product(none, none, d.M, d.H, d.O)}, false), launch({dx}, false)));
+}
+// ... and what the workspace has for them
+extern "C" size_t emu_split_room(const ckksmi_gated_ff *f, int backward) { return split_bytes(*f, backward); }

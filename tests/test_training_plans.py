@@ -1,5 +1,5 @@
 """Plans of training.py and head.py on the CPU stand-in: what they refuse, what they ask for and what a call is given."""
-import math
+import ctypes as C
 
 import pytest
 import torch
@@ -56,3 +56,42 @@ def test_rows_that_lie_on_each_other_are_refused(which, width):
     # one row has no distance, and rows further apart are taken as they are
     ff.forward(torch.zeros(1, width).expand(1, width), *w, torch.zeros(1, width), room)
     ff.forward(torch.zeros(rows, width + 3)[:, :width], *w, torch.zeros(rows, width), room)
+
+
+WIDTHS = [(1024, 4096, 1024), (4096, 4096, 4096), (3136, 256, 2), (517, 1021, 129), (8, 8, 8), (40, 24, 8192), (8192, 64, 1000), (2048, 8192, 2048), (2000, 4000, 4000)]
+ROWS = sorted({0, 1, 2, 63, 64, 65, 32768, 40000} | {32 * i + j for i in range(1, 200, 3) for j in (-1, 0, 1)} | {128 * i + j for i in range(1, 80) for j in (0, 1)})
+
+
+@pytest.mark.parametrize("grads", ["same", "f32"])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("widths", WIDTHS, ids=lambda s: "x".join(map(str, s)))
+def test_a_workspace_holds_any_smaller_number_of_rows(ctx, widths, dtype, grads):
+    """workspace_bytes(rows) is for calls on up to `rows` rows: more rows never ask for less, and what is asked for holds what the split k axes
+    take at this number of rows"""
+    ff = training.GatedFF(ctx, *widths, dtype, "square", F32 if grads == "f32" else None)
+    for name in ("emu_split_need", "emu_split_room"):
+        getattr(ctx._L, name).restype = C.c_size_t
+    for backward in (False, True):
+        before = 0
+        for rows in ROWS:
+            n = ff.workspace_bytes(rows, backward=backward)
+            assert n >= before, (rows, backward, n, before)
+            before = n
+            ff._s.rows = rows
+            if rows:
+                need, room = (f(ff._r, int(backward)) for f in (ctx._L.emu_split_need, ctx._L.emu_split_room))
+                assert need <= room, (rows, backward, need, room)
+
+
+def test_a_short_last_batch_trains_in_the_same_workspace(ctx):
+    """a head made for 1537 rows (gate: 49 tiles, 7 parts) takes a step on 1536 (48 tiles, 8 parts, more memory) and on a few"""
+    from paper_1911_11377_amd import head
+
+    g = torch.Generator().manual_seed(3)
+    weights = [ctx.guarded(torch.randn(s, generator=g) * s[1] ** -0.5) for s in ((2, 2048), (2, 2048), (2, 2))]
+    h = head.GatedHead(ctx, 1537, weights, "square", F32, lambda shape, t: ctx.guarded(torch.zeros(shape, dtype=t)))
+    for rows in (1536, 33, 0):
+        x = ctx.guarded(torch.randn((rows, 2048), generator=g))
+        h.step(x, lambda y, dy: dy.copy_(y * (1 / max(1, y.numel()))), 1e-3)
+        assert all(bool(torch.isfinite(w).all()) for w in weights)
+    assert ctx.errors() == 0
