@@ -84,7 +84,7 @@ struct Activation { int kind; float c[4]; };
 __device__ __forceinline__ float act_value(const Activation &A, float g) {
     switch (A.kind) {
         case CKKSMI_ACT_POLY: return ((A.c[3] * g + A.c[2]) * g + A.c[1]) * g + A.c[0];
-        case CKKSMI_ACT_RELU: return g > 0.0f ? g : g * 0.0f;  // a NaN stays one
+        case CKKSMI_ACT_RELU: return g < 0.0f ? 0.0f : g;  // (a NaN stays one)
         case CKKSMI_ACT_SILU: return g * (1.0f / (1.0f + expf(-g)));
         default: return g * (0.5f * (1.0f + erff(g * 0.70710678f)));
     }
@@ -97,7 +97,7 @@ __device__ __forceinline__ void act_both(const Activation &A, float g, float &a,
             da = (3.0f * A.c[3] * g + 2.0f * A.c[2]) * g + A.c[1];
             return;
         case CKKSMI_ACT_RELU:
-            a = g > 0.0f ? g : g * 0.0f;
+            a = g < 0.0f ? 0.0f : g;
             da = g > 0.0f ? 1.0f : 0.0f;
             return;
         case CKKSMI_ACT_SILU: {

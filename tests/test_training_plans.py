@@ -95,3 +95,23 @@ def test_a_short_last_batch_trains_in_the_same_workspace(ctx):
         h.step(x, lambda y, dy: dy.copy_(y * (1 / max(1, y.numel()))), 1e-3)
         assert all(bool(torch.isfinite(w).all()) for w in weights)
     assert ctx.errors() == 0
+
+
+@pytest.mark.parametrize("dtype,rows", [(BF16, 3), (F32, 3), (BF16, 70)], ids=["bf16", "f32", "bf16-tiles"])
+def test_relu_of_minus_infinity_is_zero(ctx, dtype, rows):
+    """finite operands whose gate sums pass the type's range: max(g, 0) is 0 below it, infinite above, and a NaN stays one"""
+    ff = training.GatedFF(ctx, 8, 8, 8, dtype, "relu")
+    x = torch.full((rows, 8), 1.0, dtype=dtype)
+    x[0], x[1], x[2, 3] = 3e38, -3e38, float("nan")
+    wg, wu = torch.full((8, 8), -1.0, dtype=dtype), torch.zeros(8, 8, dtype=dtype)
+    wu[:, 0] = 2.0**-120
+    wd = torch.ones(8, 8, dtype=dtype)
+    x, wg, wu, wd, dy = (ctx.guarded(t) for t in (x, wg, wu, wd, torch.ones(rows, 8, dtype=dtype)))
+    y, dx, dw = ctx.guarded(torch.ones(rows, 8, dtype=dtype)), ctx.guarded(torch.ones(rows, 8, dtype=dtype)), [ctx.guarded(torch.ones(8, 8, dtype=dtype)) for _ in range(3)]
+    saved, ws = (ctx.guarded(torch.full((max(16, n),), 255, dtype=torch.uint8)) for n in (ff.saved_bytes(rows), ff.workspace_bytes(rows, backward=True)))
+    for keep in (saved, None):
+        ff.forward(x, wg, wu, wd, y, ws, saved=keep)
+        assert bool((y[0] == 0).all()) and bool((y[1] == -float("inf")).all()) and bool(torch.isnan(y[2]).all())
+        assert bool((y[3:] == 0).all())
+    ff.backward(x, wg, wu, wd, saved, dy, dx, *dw, ws)
+    assert bool((dx[0] == 0).all())  # neither the gate's derivative nor its value is anything but 0 there
