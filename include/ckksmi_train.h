@@ -48,7 +48,7 @@ typedef struct {
 } ckksmi_gated_ff;
 
 /* bytes of workspace of the forward (backward = 0) or of either pass (backward = 1) on up to `rows` rows (never less for more rows); of what a forward pass saves for the
- * backward pass: act(g), u act'(g) and h, 8 bytes per row and hidden unit for 16-bit types (with f32 gradients 12 for f16, 14 for bf16), 12 for f32 */
+ * backward pass: act(g), u act'(g) and h, 8 bytes per row and hidden unit for 16-bit types (with f32 gradients 16 for f16, 14 for bf16), 12 for f32 */
 int ckksmi_gated_ff_workspace_bytes(const ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, int backward, size_t *bytes);
 int ckksmi_gated_ff_saved_bytes(const ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, size_t *bytes);
 /* saved: NULL (nothing is kept: answering requests) or a buffer for the backward pass.  y must not overlap an input. */
@@ -58,8 +58,10 @@ int ckksmi_gated_ff_forward(ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, const vo
  *     dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x,  dWd = dy^T h.
  * saved: what the forward pass on the same x and weights left.  dx may be NULL (a first layer needs none).  accumulate != 0: the weights'
  * gradients are added to what the buffers hold.  dg and du are rounded to `dtype` between the products; where the gradients are
- * f32 and `dtype` is not, they and h enter the weights' gradients as sums of two (f16) or three (bf16) values of `dtype`, at as
- * many times these products' cost, and the gradients are as good as f32 operands' would be.  Outputs must not overlap inputs.  The sums' order depends on the sizes alone: equal calls give equal bits. */
+ * f32 and `dtype` is not, h, dg and du enter the weights' gradients as sums of three bf16 values, x and dy of f16 as sums of two, at
+ * three (bf16) or five (f16) times these products' cost: the gradients are as good as f32 operands' would be, over the range of
+ * f32.  (The sums for dx and y take h, dg and du as values of `dtype`, with its range.)  Outputs must not overlap inputs.  The sums' order
+ * depends on the sizes alone: equal calls give equal bits. */
 int ckksmi_gated_ff_backward(ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, const void *x, const void *w_gate, const void *w_up, const void *w_down,
                              const void *saved, const void *dy, void *dx, void *dw_gate, void *dw_up, void *dw_down, int accumulate,
                              void *ws, size_t ws_bytes, void *stream);

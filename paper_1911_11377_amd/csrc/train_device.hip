@@ -66,12 +66,14 @@ struct FF {  // a call's sizes
         : es(element_bytes(f.dtype)), ges(element_bytes(f.grad_dtype)), M((size_t)f.rows), K((size_t)f.d_in), H((size_t)f.d_hidden), O((size_t)f.d_out), ldh(round_up(H, 8)) {}
     size_t hidden_bytes() const { return round_up(M * ldh * es, 256); }
     bool fine() const { return es == 2 && ges == 4; }  // f32 gradients of 16-bit operands
-    // 16-bit values whose sum h, dg and du enter the weights' gradients as: 24 bits of bf16, 22 of f16
-    int parts(int dtype) const { return !fine() ? 1 : dtype == CKKSMI_BF16 ? 3 : 2; }
-    // what a forward pass saves: act(g), u act'(g) (4 bytes, or 2 + 1), h in its parts
+    // then h, dg and du enter the weights' gradients as sums of three bf16 parts.  Arrays that each is kept in: rounded to its type, for bf16 the
+    // first part too; and the products that the gradients are the sum of: x and dy are one bf16 value, or (f16) two
+    int arrays(int dtype) const { return !fine() ? 1 : dtype == CKKSMI_BF16 ? 3 : 4; }
+    int sources(int dtype) const { return !fine() ? 1 : dtype == CKKSMI_BF16 ? 3 : 5; }
+    // what a forward pass saves: act(g), u act'(g) (4 bytes, or 2 + 1), h in its arrays
     size_t kept_bytes() const { return fine() ? round_up(M * ldh * 4, 256) : hidden_bytes(); }
     size_t low_bytes() const { return es == 2 && !fine() ? round_up(M * ldh, 256) : 0; }
-    size_t saved_bytes(int dtype) const { return 2 * kept_bytes() + 2 * low_bytes() + parts(dtype) * hidden_bytes(); }
+    size_t saved_bytes(int dtype) const { return 2 * kept_bytes() + 2 * low_bytes() + arrays(dtype) * hidden_bytes(); }
     Kept kept(const void *saved) const {
         char *p = (char *)saved;
         uint8_t *low = (uint8_t *)p + 2 * kept_bytes();
@@ -206,14 +208,25 @@ template <class T> struct Operands {
         const size_t ld_dst = round_up(cols * es, 16);
         char *dst = w.take(rows * ld_dst);  // counted whether needed or not: the workspace's size does not depend on addresses
         if (aligned(src, 16) && ld % 16 == 0 && cols * es % 16 == 0) return Matrix{(const char *)src, ld};
-        CopyArgs::One &o = C.c[C.n++];
-        o.src = (const char *)src; o.dst = dst; o.ld_src = ld; o.ld_dst = ld_dst; o.cols = (int)cols; o.chunks = (int)(ld_dst / 16); o.rows = rows;
-        o.first = blocks;
-        blocks += (unsigned)((rows * o.chunks + 255) / 256);
+        copy(src, ld, rows, cols, dst, ld_dst, 0);
         return Matrix{dst, ld_dst};
     }
-    void run(ckksmi_ctx *c, hipStream_t st) {
-        if (blocks) KL(c, CKKSMI_K_GEMM_COPY, blocks, pad_rows_kernel<T>, dim3(blocks), dim3(256), st, C);
+    // two bf16 arrays whose sum the operand is, for run<true>()
+    Matrix split(const void *src, size_t ld, size_t rows, size_t cols, size_t &apart, Carve &w) {
+        const size_t ld_dst = round_up(cols * sizeof(T), 16);
+        apart = round_up(rows * ld_dst, 256);
+        char *dst = w.take(2 * apart);
+        copy(src, ld, rows, cols, dst, ld_dst, apart);
+        return Matrix{dst, ld_dst};
+    }
+    void copy(const void *src, size_t ld, size_t rows, size_t cols, char *dst, size_t ld_dst, size_t split) {
+        CopyArgs::One &o = C.c[C.n++];
+        o.src = (const char *)src; o.dst = dst; o.ld_src = ld; o.ld_dst = ld_dst; o.cols = (int)cols; o.chunks = (int)(ld_dst / 16); o.rows = rows; o.split = split;
+        o.first = blocks;
+        blocks += (unsigned)((rows * o.chunks + 255) / 256);
+    }
+    template <bool SPLIT = false> void run(ckksmi_ctx *c, hipStream_t st) {
+        if (blocks) KL(c, CKKSMI_K_GEMM_COPY, blocks, (pad_rows_kernel<T, SPLIT>), dim3(blocks), dim3(256), st, C);
     }
 };
 
@@ -229,7 +242,7 @@ size_t split_bytes(const ckksmi_gated_ff &f, bool backward) {
     dx.nsrc = 2;
     most = std::max(most, std::max(one(product(none, none, d.M, d.H, d.O), false), one(dx, false)));
     GemmProblem dw[3] = {product(none, none, d.H, d.K, d.M), product(none, none, d.H, d.K, d.M), product(none, none, d.O, d.H, d.M)};
-    for (GemmProblem &p : dw) p.nsrc = d.parts(f.dtype);
+    for (GemmProblem &p : dw) p.nsrc = d.sources(f.dtype);
     const int splits = choose(dw, 3, false, d.es).splits;
     return std::max(most, part_bytes(dw[0], splits, false) * 2 + part_bytes(dw[2], splits, false) + 768);
 }
@@ -239,7 +252,8 @@ size_t workspace_of(const ckksmi_gated_ff &f, bool backward) {
     auto rows = [&](size_t r, size_t cols) { return round_up(r * round_up(cols * d.es, 16), 256); };
     const size_t weights = 2 * rows(d.H, d.K) + rows(d.O, d.H);
     const size_t forward = rows(d.M, d.K) + weights + d.hidden_bytes();
-    const size_t back = rows(d.M, d.K) + weights + rows(d.M, d.O) + 2 * d.parts(f.dtype) * d.hidden_bytes();
+    const size_t split = f.dtype == CKKSMI_F16 && d.fine() ? 2 * (rows(d.M, d.K) + rows(d.M, d.O)) : 0;
+    const size_t back = rows(d.M, d.K) + weights + rows(d.M, d.O) + split + 2 * d.arrays(f.dtype) * d.hidden_bytes();
     return (backward ? std::max(forward, back) : forward) + split_bytes(f, backward);
 }
 
@@ -268,8 +282,8 @@ int forward(ckksmi_ctx *c, const ckksmi_gated_ff &f, const void *x, const void *
     EpiArgs to_hidden;
     memset(&to_hidden, 0, sizeof(to_hidden));
     if (keep) to_hidden.kept = d.kept(keep);
-    to_hidden.parts = keep ? d.parts(f.dtype) : 1;
-    to_hidden.part_bytes = d.hidden_bytes();
+    to_hidden.arrays = keep ? d.arrays(f.dtype) : 1;
+    to_hidden.array_bytes = d.hidden_bytes();
     to_hidden.ldo = d.ldh; to_hidden.N = (int)d.H; to_hidden.act = activation_of(f);
     if (d.M <= kFewRows) {
         RowsArgs R;
@@ -308,17 +322,25 @@ int backward(ckksmi_ctx *c, const ckksmi_gated_ff &f, const void *x, const void 
              void *dwg, void *dwu, void *dwd, bool accumulate, Carve w, hipStream_t st) {
     const FF d(f);
     Guard guard(c);
-    Operands<T> ops;
-    const Matrix mx = ops.use(x, ld_bytes(f.ld_x, d.K, d.es), d.M, d.K, w), mg = ops.use(wg, d.K * d.es, d.H, d.K, w), mu = ops.use(wu, d.K * d.es, d.H, d.K, w);
-    const Matrix md = ops.use(wd, d.H * d.es, d.O, d.H, w), mdy = ops.use(dy, ld_bytes(f.ld_dy, d.O, d.es), d.M, d.O, w);
-    const int parts = d.parts(f.dtype);
-    char *dg = w.take(parts * d.hidden_bytes()), *du = w.take(parts * d.hidden_bytes());
+    Operands<T> ops, halves;
+    constexpr bool f16 = __is_same(T, _Float16);
+    const size_t ldx = ld_bytes(f.ld_x, d.K, d.es), lddy = ld_bytes(f.ld_dy, d.O, d.es);
+    const Matrix mg = ops.use(wg, d.K * d.es, d.H, d.K, w), mu = ops.use(wu, d.K * d.es, d.H, d.K, w), md = ops.use(wd, d.H * d.es, d.O, d.H, w);
+    const Matrix mdy = ops.use(dy, lddy, d.M, d.O, w);
+    // x and dy as the weights' gradients take them
+    size_t x_apart = 0, dy_apart = 0;
+    const bool split = f16 && d.fine();
+    const Matrix gx = split ? halves.split(x, ldx, d.M, d.K, x_apart, w) : ops.use(x, ldx, d.M, d.K, w);
+    const Matrix gdy = split ? halves.split(dy, lddy, d.M, d.O, dy_apart, w) : mdy;
+    const int arrays = d.arrays(f.dtype);
+    char *dg = w.take(arrays * d.hidden_bytes()), *du = w.take(arrays * d.hidden_bytes());
     const char *h = d.saved_h(saved);
     const size_t ldh = d.ldh * d.es;
     ops.run(c, st);
+    if constexpr (f16) halves.template run<true>(c, st);
 
     GemmProblem dh = product(mdy, md, d.M, d.H, d.O);
-    dh.epi.o0 = dg; dh.epi.o1 = du; dh.epi.parts = parts; dh.epi.part_bytes = d.hidden_bytes(); dh.epi.kept = d.kept(saved);
+    dh.epi.o0 = dg; dh.epi.o1 = du; dh.epi.arrays = arrays; dh.epi.array_bytes = d.hidden_bytes(); dh.epi.kept = d.kept(saved);
     dh.epi.ldo = d.ldh; dh.epi.N = (int)d.H;
     launch_gemm<T, false, true, EPI_DHID>(c, &dh, 1, w, st);
 
@@ -328,17 +350,21 @@ int backward(ckksmi_ctx *c, const ckksmi_gated_ff &f, const void *x, const void 
         store_to(p, dx, f.ld_dx ? f.ld_dx : d.K, f.dtype, false);
         launch_gemm<T, false, true, EPI_STORE>(c, &p, 1, w, st);
     }
-    GemmProblem dw[3] = {product(Matrix{dg, ldh}, mx, d.H, d.K, d.M), product(Matrix{du, ldh}, mx, d.H, d.K, d.M), product(mdy, Matrix{h, ldh}, d.O, d.H, d.M)};
-    for (GemmProblem &p : dw) p.nsrc = parts;
-    for (int i = 1; i < parts; i++) {
-        const size_t at = i * d.hidden_bytes();
-        dw[0].a[i] = dg + at; dw[1].a[i] = du + at; dw[2].a[i] = mdy.p;
-        dw[0].b[i] = mx.p; dw[1].b[i] = mx.p; dw[2].b[i] = h + at;
+    GemmProblem dw[3] = {product(Matrix{dg, ldh}, gx, d.H, d.K, d.M), product(Matrix{du, ldh}, gx, d.H, d.K, d.M), product(gdy, Matrix{h, ldh}, d.O, d.H, d.M)};
+    // arrays of h, dg, du and of x, dy whose products are added up (of f16 all but third part times second, 2^-24 of the whole)
+    static const struct { int hidden, other; } bf16_sources[3] = {{0, 0}, {1, 0}, {2, 0}}, f16_sources[5] = {{1, 0}, {2, 0}, {1, 1}, {3, 0}, {2, 1}};
+    for (GemmProblem &p : dw) p.nsrc = d.sources(f.dtype);
+    for (int i = 0; d.fine() && i < dw[0].nsrc; i++) {
+        const size_t at = (f16 ? f16_sources[i] : bf16_sources[i]).hidden * d.hidden_bytes(), other = (f16 ? f16_sources[i] : bf16_sources[i]).other;
+        dw[0].a[i] = dg + at; dw[1].a[i] = du + at; dw[2].b[i] = h + at;
+        dw[0].b[i] = dw[1].b[i] = gx.p + other * x_apart;
+        dw[2].a[i] = gdy.p + other * dy_apart;
     }
     store_to(dw[0], dwg, d.K, f.grad_dtype, accumulate);
     store_to(dw[1], dwu, d.K, f.grad_dtype, accumulate);
     store_to(dw[2], dwd, d.H, f.grad_dtype, accumulate);
-    launch_gemm<T, true, true, EPI_STORE>(c, dw, 3, w, st);
+    if (split) launch_gemm<__bf16, true, true, EPI_STORE>(c, dw, 3, w, st);
+    else launch_gemm<T, true, true, EPI_STORE>(c, dw, 3, w, st);
     return guard.rc();
 }
 

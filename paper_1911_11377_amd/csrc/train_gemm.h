@@ -33,8 +33,8 @@ struct Kept {
 // What happens to 8 neighbouring results of a row
 struct EpiArgs {
     void *o0, *o1;         // GATE: h; STORE: the result; DHID: dg, du
-    int parts;             // GATE, DHID: 16-bit values that o0 and o1 are written as the sum of
-    size_t part_bytes;     // from one of them to the next
+    int arrays;            // GATE, DHID: 16-bit arrays that o0 and o1 each are (store_parts)
+    size_t array_bytes;    // from one of them to the next
     Kept kept;             // GATE: to be written (a null: nothing is kept); DHID: to be read
     size_t ldo;            // elements, all of them
     int N;                 // columns
@@ -44,7 +44,7 @@ struct EpiArgs {
     Activation act;
 };
 
-#define TG_SOURCES 3
+#define TG_SOURCES 5
 struct GemmProblem {
     const char *a[TG_SOURCES], *b[TG_SOURCES];  // STORE adds nsrc products, A0 B0 + A1 B1 + ..; GATE has two B's on one A
     size_t lda, ldb;          // bytes from one row (along k) or one k index (along rows) to the next
@@ -64,17 +64,22 @@ struct GemmArgs {
     int splits;                  // parts of the k axis, joined by gemm_join_kernel
 };
 
-// x rounded to T; more parts: what that left, rounded likewise, and so on
+// x rounded to T; with more arrays also x in three bf16 parts, each the rounding of what the ones before left: 24 bits over the whole range of
+// f32.  For bf16 the rounded x is the first part, for f16 (whose range would cut small and large parts off) it is none of them
 template <class T> __device__ __forceinline__ void store_parts(const EpiArgs &E, void *o, size_t at, const float (&x)[8]) {
     store_oct((T *)o + at, x);
     if constexpr (sizeof(T) == 2) {
         float r[8];
 #pragma unroll
         for (int e = 0; e < 8; e++) r[e] = x[e];
-        for (int p = 1; p < E.parts; p++) {
+        for (int p = 1; p < E.arrays; p++) {
+            if (p > 1 || __is_same(T, __bf16))
 #pragma unroll
-            for (int e = 0; e < 8; e++) r[e] -= (float)(T)r[e];
-            store_oct((T *)((char *)o + p * E.part_bytes) + at, r);
+                for (int e = 0; e < 8; e++) {
+                    const float part = (float)(__bf16)r[e];
+                    r[e] = fabsf(part) <= 3.4e38f ? r[e] - part : 0.0f;  // what is not finite is in its first part alone
+                }
+            store_oct((__bf16 *)((char *)o + p * E.array_bytes) + at, r);
         }
     }
 }
@@ -621,13 +626,14 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(GemmArgs G) {
 }
 
 // Copies with rows padded to whole 16-byte chunks (zeros behind the last column), for operands whose rows do not begin on them: one launch for
-// all of a call's, 5.4 us for the 2.7 MB of 333 rows of 517 -> 1021 -> 129
+// all of a call's, 5.4 us for the 2.7 MB of 333 rows of 517 -> 1021 -> 129.  SPLIT: f16 values as the sum of two bf16 ones (their 11 bits fit), the
+// second array `split` bytes behind the first
 #define TG_COPIES 5  // of one call: x, three weight matrices, dy
 struct CopyArgs {
-    struct One { const char *src; char *dst; size_t ld_src, ld_dst; int cols, chunks; size_t rows; unsigned first; } c[TG_COPIES];
+    struct One { const char *src; char *dst; size_t ld_src, ld_dst; int cols, chunks; size_t rows, split; unsigned first; } c[TG_COPIES];
     int n;
 };
-template <class T> __global__ void __launch_bounds__(256) pad_rows_kernel(CopyArgs A) {
+template <class T, bool SPLIT> __global__ void __launch_bounds__(256) pad_rows_kernel(CopyArgs A) {
     int i = 0;
     while (i + 1 < A.n && blockIdx.x >= A.c[i + 1].first) i++;
     const CopyArgs::One &C = A.c[i];
@@ -646,5 +652,17 @@ template <class T> __global__ void __launch_bounds__(256) pad_rows_kernel(CopyAr
         for (int e = 0; e < EPC; e++) v[e] = c + e < C.cols ? s[e] : (T)0.0f;
         __builtin_memcpy(&w, v, 16);
     }
-    *(u32x4 *)(C.dst + r * C.ld_dst + (size_t)c * sizeof(T)) = w;
+    char *const d = C.dst + r * C.ld_dst + (size_t)c * sizeof(T);
+    if constexpr (SPLIT) {
+        T v[EPC];
+        __builtin_memcpy(&v, &w, 16);
+        float x[EPC];
+#pragma unroll
+        for (int e = 0; e < EPC; e++) x[e] = (float)v[e];
+        store_oct((__bf16 *)d, x);
+#pragma unroll
+        for (int e = 0; e < EPC; e++) x[e] -= (float)(__bf16)x[e];
+        store_oct((__bf16 *)(d + C.split), x);
+    } else
+        *(u32x4 *)d = w;
 }

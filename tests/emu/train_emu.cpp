@@ -245,7 +245,7 @@ extern "C" size_t emu_split_need(const ckksmi_gated_ff *f, int backward) {
     if (!backward) return std::max(launch({product(none, none, d.M, d.H, d.K)}, true), launch({product(none, none, d.M, d.O, d.H)}, false));
     GemmProblem dx = product(none, none, d.M, d.K, d.H), dw = product(none, none, d.H, d.K, d.M), down = product(none, none, d.O, d.H, d.M);
     dx.nsrc = 2;
-    dw.nsrc = down.nsrc = d.parts(f->dtype);
+    dw.nsrc = down.nsrc = d.sources(f->dtype);
     return std::max(launch({dw, dw, down}, false), std::max(launch({product(none, none, d.M, d.H, d.O)}, false), launch({dx}, false)));
 }
 // ... and what the workspace has for them

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import train_emu_support as emu
+import training_range
 from paper_1911_11377_amd import training
 
 pytestmark = pytest.mark.skipif(not emu.available, reason="no host compiler with 16-bit float types")
@@ -115,3 +116,34 @@ def test_relu_of_minus_infinity_is_zero(ctx, dtype, rows):
         assert bool((y[3:] == 0).all())
     ff.backward(x, wg, wu, wd, saved, dy, dx, *dw, ws)
     assert bool((dx[0] == 0).all())  # neither the gate's derivative nor its value is anything but 0 there
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("rows", [20, 70])
+@pytest.mark.parametrize("scales", training_range.SCALES, ids=str)
+def test_f32_gradients_of_16_bit_operands_have_the_range_of_f32(ctx, scales, rows, dtype):
+    training_range.check(ctx, "cpu", ctx.guarded, rows, dtype, scales)
+    assert ctx.errors() == 0
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+def test_f32_gradients_of_infinite_products(ctx, dtype):
+    """what overflows f32 itself is not finite in the gradients, and the rest is as it was"""
+    rows = 20
+    ff = training.GatedFF(ctx, 8, 8, 8, dtype, (0.0, 0.0, 0.0, 1e38), F32)
+    x, dy = torch.zeros(rows, 8, dtype=dtype), torch.zeros(rows, 8, dtype=dtype)
+    x[3], dy[3] = 4.0, 1.0
+    x[4:, 0], dy[4:, 0] = 2.0**-10, 2.0**-10
+    wg, wu = torch.zeros(8, 8, dtype=dtype), torch.ones(8, 8, dtype=dtype)
+    wg[5] = 1.0
+    x, dy, wg, wu, wd = (ctx.guarded(t) for t in (x, dy, wg, wu, torch.ones(8, 8, dtype=dtype)))
+    y, dx, dw = ctx.guarded(torch.zeros(rows, 8, dtype=dtype)), ctx.guarded(torch.zeros(rows, 8, dtype=dtype)), [ctx.guarded(torch.zeros(8, 8)) for _ in range(3)]
+    saved, ws = (ctx.guarded(torch.full((max(16, n),), 255, dtype=torch.uint8)) for n in (ff.saved_bytes(rows), ff.workspace_bytes(rows, backward=True)))
+    ff.forward(x, wg, wu, wd, y, ws, saved=saved)
+    ff.backward(x, wg, wu, wd, saved, dy, dx, *dw, ws)
+    # unit 5 alone has a gate that is not zero: its row of dWg, dWu and its column of dWd
+    for d in (dw[0], dw[1], dw[2].t()):
+        assert not bool(torch.isfinite(d[5]).any()), d[5]
+        assert bool(torch.isfinite(d[[i for i in range(8) if i != 5]]).all())
+    if dtype == BF16:  # one value a factor: infinities stay infinities
+        assert bool(torch.isinf(dw[1][5]).all())
