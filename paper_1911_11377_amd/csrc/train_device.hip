@@ -17,18 +17,19 @@ inline size_t round_up(size_t v, size_t to) { return (v + to - 1) / to * to; }
 inline bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 inline bool dtype_ok(int d) { return d == CKKSMI_F32 || d == CKKSMI_BF16 || d == CKKSMI_F16; }
 
-int check_ff(const ckksmi_gated_ff *f) {
-    if (!f || !dtype_ok(f->dtype) || (f->grad_dtype != f->dtype && f->grad_dtype != CKKSMI_F32) || f->act < CKKSMI_ACT_POLY || f->act > CKKSMI_ACT_GELU) return CKKSMI_EINVAL;
-    if (f->rows < 0 || f->rows > kMaxRows) return CKKSMI_EINVAL;
-    const int64_t d[3] = {f->d_in, f->d_hidden, f->d_out};
+// (Entry points copy the caller's structure before they check it: what was checked is what is used)
+int check_ff(const ckksmi_gated_ff &f) {
+    if (!dtype_ok(f.dtype) || (f.grad_dtype != f.dtype && f.grad_dtype != CKKSMI_F32) || f.act < CKKSMI_ACT_POLY || f.act > CKKSMI_ACT_GELU) return CKKSMI_EINVAL;
+    if (f.rows < 0 || f.rows > kMaxRows) return CKKSMI_EINVAL;
+    const int64_t d[3] = {f.d_in, f.d_hidden, f.d_out};
     for (int64_t v : d)
         if (v < 1 || v > kMaxDim) return CKKSMI_EINVAL;
     // every grid has fewer than 2^31 workgroups: of the smallest tiles, and of 4 KB of an operand that is copied
-    const double rows = (double)f->rows, in = (double)f->d_in, hidden = (double)f->d_hidden, out = (double)f->d_out, most = 2147483647.0;
+    const double rows = (double)f.rows, in = (double)f.d_in, hidden = (double)f.d_hidden, out = (double)f.d_out, most = 2147483647.0;
     auto tiles = [](double m, double n) { return (m / 32 + 1) * (n / 64 + 1); };
     if (std::max(std::max(tiles(rows, hidden), tiles(rows, out)), std::max(tiles(rows, in), 2 * tiles(hidden, in) + tiles(out, hidden))) > most) return CKKSMI_EUNSUPPORTED;
     if (((rows + 2 * hidden) * (in + 8) + out * (hidden + 8) + rows * (out + 8)) * 4 / 4096 + 8 > most) return CKKSMI_EUNSUPPORTED;
-    const int64_t ld[4] = {f->ld_x, f->ld_y, f->ld_dy, f->ld_dx}, least[4] = {f->d_in, f->d_out, f->d_out, f->d_in};
+    const int64_t ld[4] = {f.ld_x, f.ld_y, f.ld_dy, f.ld_dx}, least[4] = {f.d_in, f.d_out, f.d_out, f.d_in};
     for (int i = 0; i < 4; i++)
         if (ld[i] != 0 && (ld[i] < least[i] || ld[i] > kMaxDim)) return CKKSMI_EINVAL;
     return CKKSMI_OK;
@@ -375,62 +376,68 @@ __global__ void __launch_bounds__(256) clear_kernel(char *p, size_t bytes) {
 
 }  // namespace
 
-extern "C" int ckksmi_gated_ff_workspace_bytes(const ckksmi_ctx *c, const ckksmi_gated_ff *f, int backward, size_t *bytes) {
-    if (!c || !bytes) return CKKSMI_EINVAL;
+extern "C" int ckksmi_gated_ff_workspace_bytes(const ckksmi_ctx *c, const ckksmi_gated_ff *ff, int backward, size_t *bytes) {
+    if (!c || !ff || !bytes) return CKKSMI_EINVAL;
+    const ckksmi_gated_ff f = *ff;
     const int rc = check_ff(f);
     if (rc) return rc;
-    *bytes = workspace_of(*f, backward != 0);
+    *bytes = workspace_of(f, backward != 0);
     return CKKSMI_OK;
 }
 
-extern "C" int ckksmi_gated_ff_saved_bytes(const ckksmi_ctx *c, const ckksmi_gated_ff *f, size_t *bytes) {
-    if (!c || !bytes) return CKKSMI_EINVAL;
+extern "C" int ckksmi_gated_ff_saved_bytes(const ckksmi_ctx *c, const ckksmi_gated_ff *ff, size_t *bytes) {
+    if (!c || !ff || !bytes) return CKKSMI_EINVAL;
+    const ckksmi_gated_ff f = *ff;
     const int rc = check_ff(f);
     if (rc) return rc;
-    *bytes = FF(*f).saved_bytes(f->dtype);
+    *bytes = FF(f).saved_bytes(f.dtype);
     return CKKSMI_OK;
 }
 
-extern "C" int ckksmi_gated_ff_forward(ckksmi_ctx *c, const ckksmi_gated_ff *f, const void *x, const void *wg, const void *wu, const void *wd, void *y, void *saved,
+extern "C" int ckksmi_gated_ff_forward(ckksmi_ctx *c, const ckksmi_gated_ff *ff, const void *x, const void *wg, const void *wu, const void *wd, void *y, void *saved,
                                        void *ws, size_t ws_bytes, void *stream) {
     if (!dev_ok(c)) return CKKSMI_EDEVICE;
+    if (!ff) return CKKSMI_EINVAL;
+    const ckksmi_gated_ff f = *ff;
     const int rc = check_ff(f);
     if (rc) return rc;
     if (!wg || !wu || !wd) return CKKSMI_EINVAL;
-    if (f->rows == 0) return CKKSMI_OK;
-    const FF d(*f);
+    if (f.rows == 0) return CKKSMI_OK;
+    const FF d(f);
     if (!x || !y || !ws || !aligned(ws, 16) || !aligned(saved, 16)) return CKKSMI_EINVAL;
     for (const void *p : {x, wg, wu, wd, (const void *)y})
         if (!aligned(p, d.es)) return CKKSMI_EINVAL;
-    const size_t ldx = ld_bytes(f->ld_x, d.K, d.es), ldy = ld_bytes(f->ld_y, d.O, d.es);
-    const size_t nx = (d.M - 1) * ldx + d.K * d.es, ny = (d.M - 1) * ldy + d.O * d.es, nw = d.H * d.K * d.es, nd = d.O * d.H * d.es, ns = saved ? d.saved_bytes(f->dtype) : 0;
+    const size_t ldx = ld_bytes(f.ld_x, d.K, d.es), ldy = ld_bytes(f.ld_y, d.O, d.es);
+    const size_t nx = (d.M - 1) * ldx + d.K * d.es, ny = (d.M - 1) * ldy + d.O * d.es, nw = d.H * d.K * d.es, nd = d.O * d.H * d.es, ns = saved ? d.saved_bytes(f.dtype) : 0;
     const void *in[4] = {x, wg, wu, wd};
     const size_t n_in[4] = {nx, nw, nw, nd};
-    const size_t need = workspace_of(*f, false);
+    const size_t need = workspace_of(f, false);
     for (int i = 0; i < 4; i++)
         if (overlap(y, ny, in[i], n_in[i]) || overlap(saved, ns, in[i], n_in[i]) || overlap(ws, need, in[i], n_in[i])) return CKKSMI_EINVAL;
     if (overlap(y, ny, saved, ns) || overlap(ws, need, y, ny) || overlap(ws, need, saved, ns)) return CKKSMI_EINVAL;
     if (ws_bytes < need) return CKKSMI_EWORKSPACE;
     const Carve w(ws, ws_bytes);
-    switch (f->dtype) {
-        case CKKSMI_F32: return forward<float>(c, *f, x, wg, wu, wd, y, saved, w, S(stream));
-        case CKKSMI_BF16: return forward<__bf16>(c, *f, x, wg, wu, wd, y, saved, w, S(stream));
-        default: return forward<_Float16>(c, *f, x, wg, wu, wd, y, saved, w, S(stream));
+    switch (f.dtype) {
+        case CKKSMI_F32: return forward<float>(c, f, x, wg, wu, wd, y, saved, w, S(stream));
+        case CKKSMI_BF16: return forward<__bf16>(c, f, x, wg, wu, wd, y, saved, w, S(stream));
+        default: return forward<_Float16>(c, f, x, wg, wu, wd, y, saved, w, S(stream));
     }
 }
 
-extern "C" int ckksmi_gated_ff_backward(ckksmi_ctx *c, const ckksmi_gated_ff *f, const void *x, const void *wg, const void *wu, const void *wd, const void *saved,
+extern "C" int ckksmi_gated_ff_backward(ckksmi_ctx *c, const ckksmi_gated_ff *ff, const void *x, const void *wg, const void *wu, const void *wd, const void *saved,
                                         const void *dy, void *dx, void *dwg, void *dwu, void *dwd, int accumulate, void *ws, size_t ws_bytes, void *stream) {
     if (!dev_ok(c)) return CKKSMI_EDEVICE;
+    if (!ff) return CKKSMI_EINVAL;
+    const ckksmi_gated_ff f = *ff;
     const int rc = check_ff(f);
     if (rc) return rc;
-    const FF d(*f);
+    const FF d(f);
     if (!wg || !wu || !wd || !dwg || !dwu || !dwd) return CKKSMI_EINVAL;
     for (const void *p : {(const void *)dwg, (const void *)dwu, (const void *)dwd})
         if (!aligned(p, d.ges)) return CKKSMI_EINVAL;
     const size_t gw = d.H * d.K * d.ges, gd = d.O * d.H * d.ges;
     if (overlap(dwg, gw, dwu, gw) || overlap(dwg, gw, dwd, gd) || overlap(dwu, gw, dwd, gd)) return CKKSMI_EINVAL;
-    if (f->rows == 0) {  // sums of nothing
+    if (f.rows == 0) {  // sums of nothing
         if (accumulate) return CKKSMI_OK;
         Guard guard(c);
         KL(c, CKKSMI_K_GEMM_COPY, 1, clear_kernel, dim3(1024), dim3(256), S(stream), (char *)dwg, gw);
@@ -443,11 +450,11 @@ extern "C" int ckksmi_gated_ff_backward(ckksmi_ctx *c, const ckksmi_gated_ff *f,
         if (!aligned(p, d.es)) return CKKSMI_EINVAL;
     const size_t nw = d.H * d.K * d.es, nd = d.O * d.H * d.es;
     auto span = [&](int64_t ld, size_t cols) { return (d.M - 1) * ld_bytes(ld, cols, d.es) + cols * d.es; };
-    const size_t need = workspace_of(*f, true);
+    const size_t need = workspace_of(f, true);
     const void *in[6] = {x, wg, wu, wd, saved, dy};
-    const size_t n_in[6] = {span(f->ld_x, d.K), nw, nw, nd, d.saved_bytes(f->dtype), span(f->ld_dy, d.O)};
+    const size_t n_in[6] = {span(f.ld_x, d.K), nw, nw, nd, d.saved_bytes(f.dtype), span(f.ld_dy, d.O)};
     const void *out[4] = {dx, dwg, dwu, dwd};
-    const size_t n_out[4] = {dx ? span(f->ld_dx, d.K) : 0, gw, gw, gd};
+    const size_t n_out[4] = {dx ? span(f.ld_dx, d.K) : 0, gw, gw, gd};
     for (int o = 0; o < 4; o++) {
         for (int i = 0; i < 6; i++)
             if (overlap(out[o], n_out[o], in[i], n_in[i])) return CKKSMI_EINVAL;
@@ -457,10 +464,10 @@ extern "C" int ckksmi_gated_ff_backward(ckksmi_ctx *c, const ckksmi_gated_ff *f,
         if (overlap(ws, need, in[i], n_in[i])) return CKKSMI_EINVAL;
     if (ws_bytes < need) return CKKSMI_EWORKSPACE;
     const Carve w(ws, ws_bytes);
-    switch (f->dtype) {
-        case CKKSMI_F32: return backward<float>(c, *f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
-        case CKKSMI_BF16: return backward<__bf16>(c, *f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
-        default: return backward<_Float16>(c, *f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
+    switch (f.dtype) {
+        case CKKSMI_F32: return backward<float>(c, f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
+        case CKKSMI_BF16: return backward<__bf16>(c, f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
+        default: return backward<_Float16>(c, f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
     }
 }
 
@@ -483,30 +490,32 @@ static void launch_adamw(ckksmi_ctx *c, const AdamwArgs &A, int grad_dtype, unsi
     }
 }
 
-extern "C" int ckksmi_adamw_step(ckksmi_ctx *c, const ckksmi_adamw *o, const ckksmi_adamw_tensor *t, int n_tensors, void *stream) {
+extern "C" int ckksmi_adamw_step(ckksmi_ctx *c, const ckksmi_adamw *opt, const ckksmi_adamw_tensor *t, int n_tensors, void *stream) {
     if (!dev_ok(c)) return CKKSMI_EDEVICE;
-    if (!o || n_tensors < 0 || (!t && n_tensors) || !dtype_ok(o->p_dtype) || !dtype_ok(o->grad_dtype) || (o->state_bits != 8 && o->state_bits != 32)) return CKKSMI_EINVAL;
-    if (o->step < 1 || !(o->beta1 >= 0 && o->beta1 < 1) || !(o->beta2 >= 0 && o->beta2 < 1) || !(o->eps >= 0) || !std::isfinite(o->eps) || !std::isfinite(o->lr) ||
-        !std::isfinite(o->weight_decay) || !std::isfinite(o->grad_scale) || !aligned(o->skip, 4))
+    if (!opt) return CKKSMI_EINVAL;
+    const ckksmi_adamw o = *opt;
+    if (n_tensors < 0 || (!t && n_tensors) || !dtype_ok(o.p_dtype) || !dtype_ok(o.grad_dtype) || (o.state_bits != 8 && o.state_bits != 32)) return CKKSMI_EINVAL;
+    if (o.step < 1 || !(o.beta1 >= 0 && o.beta1 < 1) || !(o.beta2 >= 0 && o.beta2 < 1) || !(o.eps >= 0) || !std::isfinite(o.eps) || !std::isfinite(o.lr) ||
+        !std::isfinite(o.weight_decay) || !std::isfinite(o.grad_scale) || !aligned(o.skip, 4))
         return CKKSMI_EINVAL;
     bool copies = false;
     for (int i = 0; i < n_tensors; i++) copies = copies || (t[i].n > 0 && t[i].copy);
-    if (copies && o->copy_dtype != CKKSMI_BF16 && o->copy_dtype != CKKSMI_F16) return CKKSMI_EINVAL;
-    const bool bytes = o->state_bits == 8;
+    if (copies && o.copy_dtype != CKKSMI_BF16 && o.copy_dtype != CKKSMI_F16) return CKKSMI_EINVAL;
+    const bool bytes = o.state_bits == 8;
     for (int i = 0; i < n_tensors; i++) {
-        const int rc = check_tensor(t[i], element_bytes(o->p_dtype), element_bytes(o->grad_dtype), 2, bytes);
+        const int rc = check_tensor(t[i], element_bytes(o.p_dtype), element_bytes(o.grad_dtype), 2, bytes);
         if (rc) return rc;
     }
     AdamwArgs A;
     memset(&A, 0, sizeof(A));
-    A.copy_f16 = o->copy_dtype == CKKSMI_F16;
-    A.key = adamw_mix(adamw_mix((unsigned)o->seed) + (unsigned)(o->seed >> 32));
-    A.beta1 = (float)o->beta1; A.rest1 = (float)(1.0 - o->beta1);
-    A.beta2 = (float)o->beta2; A.rest2 = (float)(1.0 - o->beta2);
-    A.decay = (float)(1.0 - o->lr * o->weight_decay);
-    A.size = (float)(o->lr / (1.0 - std::pow(o->beta1, (double)o->step)));
-    A.root = (float)(1.0 / std::sqrt(1.0 - std::pow(o->beta2, (double)o->step)));
-    A.eps = (float)o->eps; A.grad_scale = (float)o->grad_scale; A.skip = o->skip;
+    A.copy_f16 = o.copy_dtype == CKKSMI_F16;
+    A.key = adamw_mix(adamw_mix((unsigned)o.seed) + (unsigned)(o.seed >> 32));
+    A.beta1 = (float)o.beta1; A.rest1 = (float)(1.0 - o.beta1);
+    A.beta2 = (float)o.beta2; A.rest2 = (float)(1.0 - o.beta2);
+    A.decay = (float)(1.0 - o.lr * o.weight_decay);
+    A.size = (float)(o.lr / (1.0 - std::pow(o.beta1, (double)o.step)));
+    A.root = (float)(1.0 / std::sqrt(1.0 - std::pow(o.beta2, (double)o.step)));
+    A.eps = (float)o.eps; A.grad_scale = (float)o.grad_scale; A.skip = o.skip;
     Guard guard(c);
     for (int i = 0; i < n_tensors;) {
         // as many tensors as the table holds and a grid may have workgroups (one tensor's always fit: 2^40 elements are 2^28)
@@ -523,13 +532,13 @@ extern "C" int ckksmi_adamw_step(ckksmi_ctx *c, const ckksmi_adamw *o, const ckk
         }
         A.first[A.n] = (unsigned)blocks;
         if (blocks == 0) continue;
-        switch (o->p_dtype * 64 + o->state_bits) {
-            case CKKSMI_F32 * 64 + 32: launch_adamw<float, 32>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
-            case CKKSMI_F32 * 64 + 8: launch_adamw<float, 8>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
-            case CKKSMI_BF16 * 64 + 32: launch_adamw<__bf16, 32>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
-            case CKKSMI_BF16 * 64 + 8: launch_adamw<__bf16, 8>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
-            case CKKSMI_F16 * 64 + 32: launch_adamw<_Float16, 32>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
-            default: launch_adamw<_Float16, 8>(c, A, o->grad_dtype, (unsigned)blocks, S(stream)); break;
+        switch (o.p_dtype * 64 + o.state_bits) {
+            case CKKSMI_F32 * 64 + 32: launch_adamw<float, 32>(c, A, o.grad_dtype, (unsigned)blocks, S(stream)); break;
+            case CKKSMI_F32 * 64 + 8: launch_adamw<float, 8>(c, A, o.grad_dtype, (unsigned)blocks, S(stream)); break;
+            case CKKSMI_BF16 * 64 + 32: launch_adamw<__bf16, 32>(c, A, o.grad_dtype, (unsigned)blocks, S(stream)); break;
+            case CKKSMI_BF16 * 64 + 8: launch_adamw<__bf16, 8>(c, A, o.grad_dtype, (unsigned)blocks, S(stream)); break;
+            case CKKSMI_F16 * 64 + 32: launch_adamw<_Float16, 32>(c, A, o.grad_dtype, (unsigned)blocks, S(stream)); break;
+            default: launch_adamw<_Float16, 8>(c, A, o.grad_dtype, (unsigned)blocks, S(stream)); break;
         }
     }
     return guard.rc();

@@ -48,13 +48,17 @@ class GatedFF:
             if len(cubic) != 4:
                 raise ValueError("a cubic has four coefficients")
             s.act, s.c = ckksmi.ACT_POLY, (C.c_float * 4)(*cubic)
-        self._s, self._r = s, C.byref(s)
-        self._saved_of = {}  # rows of the last call: bytes they save
+        self._s, self._r = s, C.byref(s)  # what all calls have in common
+
+    def _shape(self, rows, ld_x=0, ld_y=0, ld_dy=0, ld_dx=0):
+        """a call's own sizes: calls from several threads do not meet in one structure"""
+        s = ckksmi.GatedFFShape.from_buffer_copy(self._s)
+        s.rows, s.ld_x, s.ld_y, s.ld_dy, s.ld_dx = rows, ld_x, ld_y, ld_dy, ld_dx
+        return C.byref(s)
 
     def _bytes(self, name, rows, *args):
         n = C.c_size_t(0)
-        self._s.rows, self._s.ld_x, self._s.ld_y, self._s.ld_dy, self._s.ld_dx = rows, 0, 0, 0, 0
-        self.ctx._call(name, self.ctx._h, self._r, *args, C.byref(n))
+        self.ctx._call(name, self.ctx._h, self._shape(rows), *args, C.byref(n))
         return n.value
 
     def workspace_bytes(self, rows, backward=False):
@@ -84,10 +88,9 @@ class GatedFF:
                 self._matrix(w_down, self.d_out, self.d_hidden, dtype))
 
     def _saved(self, saved, rows):
-        if self._saved_of.get(rows) is None:
-            self._saved_of = {rows: self.saved_bytes(rows)}
-        if ckksmi._nbytes(saved) < self._saved_of[rows]:
-            raise ValueError("the buffer for saved activations holds %d bytes of %d" % (ckksmi._nbytes(saved), self._saved_of[rows]))
+        need = self.saved_bytes(rows)
+        if ckksmi._nbytes(saved) < need:
+            raise ValueError("the buffer for saved activations holds %d bytes of %d" % (ckksmi._nbytes(saved), need))
         return ckksmi._ptr(saved)
 
     def forward(self, x, w_gate, w_up, w_down, y, ws, saved=None, stream=None):
@@ -96,9 +99,7 @@ class GatedFF:
         sp = self._saved(saved, rows) if saved is not None else None
         px, ld_x = self._rows_of(x, self.d_in, self.dtype)
         py, ld_y = self._rows_of(y, self.d_out, self.dtype, rows)
-        s = self._s
-        s.rows, s.ld_x, s.ld_y, s.ld_dy, s.ld_dx = rows, ld_x, ld_y, 0, 0
-        self.ctx._call("ckksmi_gated_ff_forward", self.ctx._h, self._r, px, *self._weights(w_gate, w_up, w_down, self.dtype), py, sp, ckksmi._ptr(ws),
+        self.ctx._call("ckksmi_gated_ff_forward", self.ctx._h, self._shape(rows, ld_x, ld_y), px, *self._weights(w_gate, w_up, w_down, self.dtype), py, sp, ckksmi._ptr(ws),
                        ckksmi._nbytes(ws), self.ctx._stream(stream))
 
     def backward(self, x, w_gate, w_up, w_down, saved, dy, dx, dw_gate, dw_up, dw_down, ws, accumulate=False, stream=None):
@@ -108,9 +109,7 @@ class GatedFF:
         px, ld_x = self._rows_of(x, self.d_in, self.dtype)
         pdy, ld_dy = self._rows_of(dy, self.d_out, self.dtype, rows)
         pdx, ld_dx = self._rows_of(dx, self.d_in, self.dtype, rows) if dx is not None else (None, 0)
-        s = self._s
-        s.rows, s.ld_x, s.ld_y, s.ld_dy, s.ld_dx = rows, ld_x, 0, ld_dy, ld_dx
-        self.ctx._call("ckksmi_gated_ff_backward", self.ctx._h, self._r, px, *self._weights(w_gate, w_up, w_down, self.dtype), sp, pdy, pdx,
+        self.ctx._call("ckksmi_gated_ff_backward", self.ctx._h, self._shape(rows, ld_x, 0, ld_dy, ld_dx), px, *self._weights(w_gate, w_up, w_down, self.dtype), sp, pdy, pdx,
                        *self._weights(dw_gate, dw_up, dw_down, self.grad_dtype), 1 if accumulate else 0, ckksmi._ptr(ws), ckksmi._nbytes(ws), self.ctx._stream(stream))
 
 
@@ -144,7 +143,8 @@ class AdamW:
         o.grad_dtype = _dtype_code(grads[0].dtype) if self.n else ckksmi.F32
         o.copy_dtype = _dtype_code(copies[0].dtype) if copies else ckksmi.BF16
         o.state_bits = self.bits
-        self._o = o
+        o.step = 1
+        self._o = o  # what all steps have in common
         self._t = (ckksmi.AdamWTensor * max(self.n, 1))()
         for i in range(self.n):
             t, n = self._t[i], params[i].numel()
@@ -160,7 +160,7 @@ class AdamW:
 
     def step(self, lr, betas, eps, weight_decay, step, grad_scale=1.0, seed=0, skip=None, stream=None):
         """step: 1, 2, ..; seed: another one at every step (8-bit states); skip: None or a device int32 that, if not 0, makes the step do nothing"""
-        o = self._o
+        o = ckksmi.AdamWParams.from_buffer_copy(self._o)
         o.lr, o.beta1, o.beta2, o.eps, o.weight_decay, o.grad_scale, o.step = lr, betas[0], betas[1], eps, weight_decay, grad_scale, step
         o.seed, o.skip = seed & (2**64 - 1), ckksmi._ptr(skip)
         self.ctx._call("ckksmi_adamw_step", self.ctx._h, C.byref(o), self._t, self.n, self.ctx._stream(stream))

@@ -147,3 +147,36 @@ def test_f32_gradients_of_infinite_products(ctx, dtype):
         assert bool(torch.isfinite(d[[i for i in range(8) if i != 5]]).all())
     if dtype == BF16:  # one value a factor: infinities stay infinities
         assert bool(torch.isinf(dw[1][5]).all())
+
+
+class Interrupted(Calls):
+    """a context in the midst of whose calls another thread uses the same plan"""
+
+    def __init__(self, meanwhile):
+        super().__init__()
+        self.meanwhile, self.depth, self.seen = meanwhile, 0, []
+
+    def _call(self, name, *args):
+        own = [a._obj for a in args if hasattr(a, "_obj") and isinstance(a._obj, C.Structure)]
+        before = [bytes(o) for o in own]
+        self.depth += 1
+        if self.depth == 1:
+            self.meanwhile()
+            self.seen.append((name, before == [bytes(o) for o in own]))
+        self.depth -= 1
+
+
+def test_calls_of_one_plan_do_not_share_what_they_are_given():
+    x, y, w, room = torch.zeros(9, 8), torch.zeros(9, 8), [torch.zeros(8, 8)] * 3, torch.zeros(1 << 16, dtype=torch.uint8)
+    dw = [torch.zeros(8, 8) for _ in range(3)]
+    c = Interrupted(lambda: (ff.workspace_bytes(5), ff.saved_bytes(4), ff.forward(x[:3], *w, y[:3], room), ff.backward(x[:2], *w, room, y[:2], None, *dw, room)))
+    ff = training.GatedFF(c, 8, 8, 8, F32, "square")
+    ff.forward(x, *w, y, room, saved=room)
+    ff.backward(x, *w, room, y, x, *dw, room)
+    ff.workspace_bytes(9)
+    z = [torch.zeros(7)]
+    c.meanwhile = lambda: opt.step(2e-3, (0.8, 0.9), 1e-7, 0.2, 9, seed=9)
+    opt = training.AdamW(c, z, z, z, z)
+    opt.step(1e-3, (0.9, 0.99), 1e-8, 0.1, 4, seed=3)
+    assert {"ckksmi_gated_ff_forward", "ckksmi_gated_ff_backward", "ckksmi_gated_ff_workspace_bytes", "ckksmi_adamw_step"} <= {n for n, _ in c.seen}
+    assert all(same for _, same in c.seen), c.seen
