@@ -8,6 +8,7 @@ plain features (training.py: one forward and one backward call and one optimiser
   product : the other outputs dropped to that level, ciphertext x ciphertext, rescale        one level
   fc      : Wd, then a rescale                                                               one level
 """
+import contextlib
 from dataclasses import dataclass
 
 import numpy as np
@@ -18,7 +19,8 @@ from . import activation, ckksmi, training
 class GatedHead:
     """Training state of a head on up to `rows` rows a step.  weights: float32 device tensors [d_hidden][d_in] (twice) and
     [d_out][d_hidden], updated in place; dtype: the type the products run in (bfloat16 and float16: copies of the weights,
-    renewed by each step); state_bits: 8 or 32.  empty(shape, dtype) allocates zeros on the device."""
+    renewed by each step); state_bits: 8 or 32.  empty(shape, dtype) allocates zeros on the device.  The constructor waits for
+    what it enqueues: answers and steps may use any stream."""
 
     def __init__(self, ctx, rows, weights, act, dtype, empty, state_bits=8):
         import torch
@@ -40,16 +42,23 @@ class GatedHead:
         self.ws = empty((max(16, self.ff.workspace_bytes(rows, backward=True)),), torch.uint8)
         self.saved = empty((max(16, self.ff.saved_bytes(rows)),), torch.uint8)
         self.y, self.dy = [empty((rows, weights[2].shape[0]), dtype) for _ in range(2)]
+        if weights[0].is_cuda:
+            torch.cuda.current_stream(weights[0].device).synchronize()
 
     def answer(self, x, y, stream=None):
         self.ff.forward(x, *self.used, y, self.ws, stream=stream)
 
     def step(self, x, loss, lr, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.0, stream=None):
-        """One step on rows x.  loss(y, dy) writes the loss's gradient by the answers y into dy; what it returns is returned."""
+        """One step on rows x.  loss(y, dy) writes the loss's gradient by the answers y into dy; what it returns is returned.  All of the step is
+        enqueued on `stream`: loss is called with it as torch's current stream (x and what loss reads have to be ordered before it,
+        and what loss returns is ready when it has come that far)."""
+        import torch
+
         rows = x.shape[0]
         y, dy = self.y[:rows], self.dy[:rows]
         self.ff.forward(x, *self.used, y, self.ws, saved=self.saved, stream=stream)
-        out = loss(y, dy)
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(torch.cuda.ExternalStream(stream)):
+            out = loss(y, dy)
         self.ff.backward(x, *self.used, self.saved, dy, None, *self.grads, self.ws, stream=stream)
         self.steps += 1
         self.opt.step(lr, betas, eps, weight_decay, self.steps, seed=self.steps, stream=stream)

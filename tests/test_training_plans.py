@@ -180,3 +180,35 @@ def test_calls_of_one_plan_do_not_share_what_they_are_given():
     opt.step(1e-3, (0.9, 0.99), 1e-8, 0.1, 4, seed=3)
     assert {"ckksmi_gated_ff_forward", "ckksmi_gated_ff_backward", "ckksmi_gated_ff_workspace_bytes", "ckksmi_adamw_step"} <= {n for n, _ in c.seen}
     assert all(same for _, same in c.seen), c.seen
+
+
+@pytest.mark.parametrize("stream", [None, 4096])
+def test_the_loss_of_a_step_is_on_the_stream_of_the_step(ctx, monkeypatch, stream):
+    """forward, loss, backward and optimiser step of a stream's step are all on that stream, without one on the current one"""
+    import contextlib
+
+    from paper_1911_11377_amd import head
+
+    current, used = ["current"], []
+
+    @contextlib.contextmanager
+    def on(s):
+        current.append(s)
+        yield
+        current.pop()
+
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, **kw: handle)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    weights = [ctx.guarded(torch.ones(s)) for s in ((4, 8), (4, 8), (2, 4))]
+    h = head.GatedHead(ctx, 6, weights, "square", F32, lambda shape, t: ctx.guarded(torch.zeros(shape, dtype=t)))
+    monkeypatch.setattr(ctx, "_stream", lambda s: used.append(current[-1] if s is None else s))
+    want = "current" if stream is None else stream
+
+    def loss(y, dy):
+        used.append(current[-1])
+        dy.copy_(y)
+        return 7
+
+    assert h.step(ctx.guarded(torch.ones(5, 8)), loss, 1e-3, stream=stream) == 7
+    assert used == [want] * 4, used
+    assert current == ["current"]
