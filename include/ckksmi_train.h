@@ -36,8 +36,8 @@ extern "C" {
  * x: [rows][d_in], Wg, Wu: [d_hidden][d_in], Wd: [d_out][d_hidden], y: [rows][d_out].  Elements are of `dtype`; sums,
  * activations and their derivatives are formed in 32 bits, and h is rounded to `dtype` before the last product.
  * Weights are dense; rows of x, y, dy, dx may lie further apart: ld_* elements, 0 = dense.  0 <= rows < 2^31 - 256,
- * every dimension and ld 1 .. 2^20; CKKSMI_EUNSUPPORTED where a product has 2^42
- * results or more, or the operands (counted as f32) 2^43 bytes. */
+ * every dimension and ld 1 .. 2^20; CKKSMI_EUNSUPPORTED where a product of the pass has more tiles than a launch holds (2^23 of 256 x 256
+ * results; f32: 2^24 of 128 x 128; of the gate's products half as many columns). */
 typedef struct {
     int dtype;      /* of x, y, the weights, dy, dx and what is saved */
     int grad_dtype; /* of the weights' gradients: dtype or CKKSMI_F32 */
@@ -90,7 +90,7 @@ typedef struct {
     void *m, *v;       /* float [n], or bytes [n] */
     float *m_unit, *v_unit; /* state_bits 8: float [ceil(n/256)] each; else unused */
     void *copy;        /* NULL, or n elements of copy_dtype: p after the step, for the next forward pass */
-    int64_t n;         /* 0 <= n < 2^40 */
+    int64_t n;         /* 0 <= n <= (2^24 - 1) * 4096 */
 } ckksmi_adamw_tensor;
 typedef struct {
     int p_dtype, grad_dtype, copy_dtype, state_bits;

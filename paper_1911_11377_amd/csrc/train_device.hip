@@ -11,7 +11,12 @@
 namespace {
 
 constexpr int64_t kMaxDim = 1 << 20, kMaxRows = 0x7fffffff - 256;
-constexpr int64_t kMaxNumel = (int64_t)1 << 40;
+constexpr double kMaxThreads = 4294967295.0;  // of a launch, along x
+constexpr int kMaxBlocks = (1 << 24) - 1;      // workgroups of 256 threads
+#ifndef TG_COPY_BLOCKS
+#define TG_COPY_BLOCKS (1 << 23)  // of a launch that copies operands: beyond, each takes several pieces (the tests' stand-in sets it)
+#endif
+constexpr int64_t kMaxNumel = (int64_t)kMaxBlocks * TA_CHUNK;
 
 inline size_t round_up(size_t v, size_t to) { return (v + to - 1) / to * to; }
 inline bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -24,11 +29,6 @@ int check_ff(const ckksmi_gated_ff &f) {
     const int64_t d[3] = {f.d_in, f.d_hidden, f.d_out};
     for (int64_t v : d)
         if (v < 1 || v > kMaxDim) return CKKSMI_EINVAL;
-    // every grid has fewer than 2^31 workgroups: of the smallest tiles, and of 4 KB of an operand that is copied
-    const double rows = (double)f.rows, in = (double)f.d_in, hidden = (double)f.d_hidden, out = (double)f.d_out, most = 2147483647.0;
-    auto tiles = [](double m, double n) { return (m / 32 + 1) * (n / 64 + 1); };
-    if (std::max(std::max(tiles(rows, hidden), tiles(rows, out)), std::max(tiles(rows, in), 2 * tiles(hidden, in) + tiles(out, hidden))) > most) return CKKSMI_EUNSUPPORTED;
-    if (((rows + 2 * hidden) * (in + 8) + out * (hidden + 8) + rows * (out + 8)) * 4 / 4096 + 8 > most) return CKKSMI_EUNSUPPORTED;
     const int64_t ld[4] = {f.ld_x, f.ld_y, f.ld_dy, f.ld_dx}, least[4] = {f.d_in, f.d_out, f.d_out, f.d_in};
     for (int i = 0; i < 4; i++)
         if (ld[i] != 0 && (ld[i] < least[i] || ld[i] > kMaxDim)) return CKKSMI_EINVAL;
@@ -103,11 +103,11 @@ constexpr double kMuchWork = 4e9;  // operations
 #define TG_ENOUGH_TILES 192  // three quarters of the compute units (the tests' stand-in sets it)
 #endif
 
-int tiles_of(const GemmProblem &p, const TileShape &t, bool gate, GemmProblem *out) {
+long long tiles_of(const GemmProblem &p, const TileShape &t, bool gate, GemmProblem *out) {
     const int cols = gate ? t.bn / 2 : t.bn;
     const int tm = (p.M + t.bm - 1) / t.bm, tn = (p.N + cols - 1) / cols;
     if (out) { out->tiles_m = tm; out->tiles_n = tn; }
-    return tm * tn;  // check_ff() has bounded it
+    return (long long)tm * tn;
 }
 
 inline int k_steps(const GemmProblem &p, size_t es) { return (int)(((size_t)p.K * es + 127) / 128) * p.nsrc; }  // of 128 bytes
@@ -153,6 +153,15 @@ size_t part_bytes_up_to(const GemmProblem &p, bool gate, size_t es) {
     return std::max(much ? most(1) : 0, most(2));
 }
 
+// Workgroups of a product's launch, 0 where it would have more threads than a launch holds (256 a workgroup, 512 for tiles of 256 x 256;
+// groups of 1024 only up to 256 workgroups)
+long long workgroups_of(const GemmProblem *p, int n, bool gate, size_t es) {
+    const Shape s = choose(p, n, gate, es);
+    long long total = 0;
+    for (int i = 0; i < n; i++) total += tiles_of(p[i], kTiles[s.tile], gate, nullptr);
+    return (double)total * (s.tile == 0 ? 512 : 256) > kMaxThreads ? 0 : total;
+}
+
 // Up to TG_PROBLEMS products of one kind in a launch; `w` gives the memory for a split k axis
 template <class T, bool A_ROWS, bool B_ROWS, int EPI>
 void launch_gemm(ckksmi_ctx *c, GemmProblem *p, int n, Carve w, hipStream_t st) {
@@ -164,7 +173,7 @@ void launch_gemm(ckksmi_ctx *c, GemmProblem *p, int n, Carve w, hipStream_t st) 
     double flops = 0;
     for (int i = 0; i < n; i++) {
         G.first[i] = total;
-        total += tiles_of(p[i], kTiles[s.tile], gate, &p[i]);
+        total += (int)tiles_of(p[i], kTiles[s.tile], gate, &p[i]);  // (fits_grids() has bounded it)
         p[i].ld_part = round_up(p[i].N, 8);
         if (s.splits > 1) p[i].part = (float *)w.take(part_bytes(p[i], s.splits, gate));
         G.p[i] = p[i];
@@ -202,7 +211,6 @@ void store_to(GemmProblem &p, void *out, size_t ld_elements, int out_dtype, bool
 // Operands whose rows begin on 16 bytes and hold whole 16-byte chunks are used where they lie, others through a padded copy
 template <class T> struct Operands {
     CopyArgs C;
-    unsigned blocks = 0;
     Operands() { memset(&C, 0, sizeof(C)); }
     Matrix use(const void *src, size_t ld, size_t rows, size_t cols, Carve &w) {
         constexpr size_t es = sizeof(T);
@@ -223,10 +231,17 @@ template <class T> struct Operands {
     void copy(const void *src, size_t ld, size_t rows, size_t cols, char *dst, size_t ld_dst, size_t split) {
         CopyArgs::One &o = C.c[C.n++];
         o.src = (const char *)src; o.dst = dst; o.ld_src = ld; o.ld_dst = ld_dst; o.cols = (int)cols; o.chunks = (int)(ld_dst / 16); o.rows = rows; o.split = split;
-        o.first = blocks;
-        blocks += (unsigned)((rows * o.chunks + 255) / 256);
     }
     template <bool SPLIT = false> void run(ckksmi_ctx *c, hipStream_t st) {
+        // pieces of 256 chunks; several a workgroup where a launch would not hold as many workgroups
+        size_t pieces = 0;
+        for (int i = 0; i < C.n; i++) pieces += (C.c[i].rows * C.c[i].chunks + 255) / 256;
+        C.per = (unsigned)(1 + pieces / TG_COPY_BLOCKS);
+        unsigned blocks = 0;
+        for (int i = 0; i < C.n; i++) {
+            C.c[i].first = blocks;
+            blocks += (unsigned)(((C.c[i].rows * C.c[i].chunks + 255) / 256 + C.per - 1) / C.per);
+        }
         if (blocks) KL(c, CKKSMI_K_GEMM_COPY, blocks, (pad_rows_kernel<T, SPLIT>), dim3(blocks), dim3(256), st, C);
     }
 };
@@ -246,6 +261,20 @@ size_t split_bytes(const ckksmi_gated_ff &f, bool backward) {
     for (GemmProblem &p : dw) p.nsrc = d.sources(f.dtype);
     const int splits = choose(dw, 3, false, d.es).splits;
     return std::max(most, part_bytes(dw[0], splits, false) * 2 + part_bytes(dw[2], splits, false) + 768);
+}
+
+// Every product of the pass fits a launch: refused before anything is enqueued
+int fits_grids(const ckksmi_gated_ff &f, bool backward) {
+    const FF d(f);
+    if (d.M == 0) return CKKSMI_OK;
+    const Matrix none{nullptr, 0};
+    auto fits = [&](const GemmProblem &p, bool gate) { return workgroups_of(&p, 1, gate, d.es) != 0; };
+    bool ok = fits(product(none, none, d.M, d.H, d.K), true) && fits(product(none, none, d.M, d.O, d.H), false);
+    if (ok && backward) {
+        const GemmProblem dw[3] = {product(none, none, d.H, d.K, d.M), product(none, none, d.H, d.K, d.M), product(none, none, d.O, d.H, d.M)};
+        ok = fits(product(none, none, d.M, d.H, d.O), false) && fits(product(none, none, d.M, d.K, d.H), false) && workgroups_of(dw, 3, false, d.es) != 0;
+    }
+    return ok ? CKKSMI_OK : CKKSMI_EUNSUPPORTED;
 }
 
 size_t workspace_of(const ckksmi_gated_ff &f, bool backward) {
@@ -379,7 +408,8 @@ __global__ void __launch_bounds__(256) clear_kernel(char *p, size_t bytes) {
 extern "C" int ckksmi_gated_ff_workspace_bytes(const ckksmi_ctx *c, const ckksmi_gated_ff *ff, int backward, size_t *bytes) {
     if (!c || !ff || !bytes) return CKKSMI_EINVAL;
     const ckksmi_gated_ff f = *ff;
-    const int rc = check_ff(f);
+    int rc = check_ff(f);
+    if (!rc) rc = fits_grids(f, backward != 0);
     if (rc) return rc;
     *bytes = workspace_of(f, backward != 0);
     return CKKSMI_OK;
@@ -388,7 +418,8 @@ extern "C" int ckksmi_gated_ff_workspace_bytes(const ckksmi_ctx *c, const ckksmi
 extern "C" int ckksmi_gated_ff_saved_bytes(const ckksmi_ctx *c, const ckksmi_gated_ff *ff, size_t *bytes) {
     if (!c || !ff || !bytes) return CKKSMI_EINVAL;
     const ckksmi_gated_ff f = *ff;
-    const int rc = check_ff(f);
+    int rc = check_ff(f);
+    if (!rc) rc = fits_grids(f, false);
     if (rc) return rc;
     *bytes = FF(f).saved_bytes(f.dtype);
     return CKKSMI_OK;
@@ -399,7 +430,8 @@ extern "C" int ckksmi_gated_ff_forward(ckksmi_ctx *c, const ckksmi_gated_ff *ff,
     if (!dev_ok(c)) return CKKSMI_EDEVICE;
     if (!ff) return CKKSMI_EINVAL;
     const ckksmi_gated_ff f = *ff;
-    const int rc = check_ff(f);
+    int rc = check_ff(f);
+    if (!rc) rc = fits_grids(f, false);
     if (rc) return rc;
     if (!wg || !wu || !wd) return CKKSMI_EINVAL;
     if (f.rows == 0) return CKKSMI_OK;
@@ -429,7 +461,8 @@ extern "C" int ckksmi_gated_ff_backward(ckksmi_ctx *c, const ckksmi_gated_ff *ff
     if (!dev_ok(c)) return CKKSMI_EDEVICE;
     if (!ff) return CKKSMI_EINVAL;
     const ckksmi_gated_ff f = *ff;
-    const int rc = check_ff(f);
+    int rc = check_ff(f);
+    if (!rc) rc = fits_grids(f, true);
     if (rc) return rc;
     const FF d(f);
     if (!wg || !wu || !wd || !dwg || !dwu || !dwd) return CKKSMI_EINVAL;
@@ -473,7 +506,7 @@ extern "C" int ckksmi_gated_ff_backward(ckksmi_ctx *c, const ckksmi_gated_ff *ff
 
 // ------------------------------------------------------------------ AdamW
 static int check_tensor(const ckksmi_adamw_tensor &t, size_t p_align, size_t g_align, size_t copy_align, bool bytes) {
-    if (t.n < 0 || t.n >= kMaxNumel) return CKKSMI_EINVAL;
+    if (t.n < 0 || t.n > kMaxNumel) return CKKSMI_EINVAL;
     if (t.n == 0) return CKKSMI_OK;
     if (!t.p || !t.grad || !t.m || !t.v || !aligned(t.p, p_align) || !aligned(t.grad, g_align) || !aligned(t.copy, copy_align)) return CKKSMI_EINVAL;
     if (bytes) return t.m_unit && t.v_unit && aligned(t.m_unit, 4) && aligned(t.v_unit, 4) ? CKKSMI_OK : CKKSMI_EINVAL;
@@ -518,13 +551,13 @@ extern "C" int ckksmi_adamw_step(ckksmi_ctx *c, const ckksmi_adamw *opt, const c
     A.eps = (float)o.eps; A.grad_scale = (float)o.grad_scale; A.skip = o.skip;
     Guard guard(c);
     for (int i = 0; i < n_tensors;) {
-        // as many tensors as the table holds and a grid may have workgroups (one tensor's always fit: 2^40 elements are 2^28)
+        // as many tensors as the table holds and a grid may have workgroups (one tensor's always fit: kMaxNumel)
         size_t blocks = 0;
         A.tensor0 = i;
         A.n = 0;
         while (i < n_tensors && A.n < TA_TENSORS) {
             const size_t more = (size_t)(t[i].n + TA_CHUNK - 1) / TA_CHUNK;
-            if (A.n && blocks + more > 0x7fffffffu) break;
+            if (blocks + more > kMaxBlocks) break;
             A.t[A.n] = t[i];
             A.first[A.n++] = (unsigned)blocks;
             blocks += more;
@@ -548,7 +581,7 @@ extern "C" int ckksmi_adamw_read_states(ckksmi_ctx *c, const ckksmi_adamw_tensor
     if (!dev_ok(c)) return CKKSMI_EDEVICE;
     if (n_tensors < 0 || (!t && n_tensors) || (!m_out && !v_out)) return CKKSMI_EINVAL;
     for (int i = 0; i < n_tensors; i++) {
-        if (t[i].n < 0 || t[i].n >= kMaxNumel) return CKKSMI_EINVAL;
+        if (t[i].n < 0 || t[i].n > kMaxNumel) return CKKSMI_EINVAL;
         if (t[i].n == 0) continue;
         if (m_out && (!m_out[i] || !t[i].m || !t[i].m_unit || !aligned(m_out[i], 4) || !aligned(t[i].m_unit, 4))) return CKKSMI_EINVAL;
         if (v_out && (!v_out[i] || !t[i].v || !t[i].v_unit || !aligned(v_out[i], 4) || !aligned(t[i].v_unit, 4))) return CKKSMI_EINVAL;
@@ -561,7 +594,7 @@ extern "C" int ckksmi_adamw_read_states(ckksmi_ctx *c, const ckksmi_adamw_tensor
         A.n = 0;
         while (i < n_tensors && A.n < TA_TENSORS) {
             const size_t more = (size_t)(t[i].n + TA_CHUNK - 1) / TA_CHUNK;
-            if (A.n && blocks + more > 0x7fffffffu) break;
+            if (blocks + more > kMaxBlocks) break;
             ReadStatesArgs::One &o = A.t[A.n];
             o.m = (const unsigned char *)t[i].m; o.v = (const unsigned char *)t[i].v; o.m_unit = t[i].m_unit; o.v_unit = t[i].v_unit;
             o.m_out = m_out ? m_out[i] : nullptr; o.v_out = v_out ? v_out[i] : nullptr; o.n = t[i].n;

@@ -632,37 +632,40 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(GemmArgs G) {
 struct CopyArgs {
     struct One { const char *src; char *dst; size_t ld_src, ld_dst; int cols, chunks; size_t rows, split; unsigned first; } c[TG_COPIES];
     int n;
+    unsigned per;  // pieces of 256 chunks of 16 bytes that a workgroup takes
 };
 template <class T, bool SPLIT> __global__ void __launch_bounds__(256) pad_rows_kernel(CopyArgs A) {
     int i = 0;
     while (i + 1 < A.n && blockIdx.x >= A.c[i + 1].first) i++;
     const CopyArgs::One &C = A.c[i];
     constexpr int EPC = 16 / sizeof(T);
-    const size_t id = (size_t)(blockIdx.x - C.first) * 256 + threadIdx.x;
-    if (id >= C.rows * C.chunks) return;
-    // (most copies are small enough for a 32-bit division)
-    const size_t r = id >> 32 ? id / C.chunks : (unsigned)id / (unsigned)C.chunks;
-    const int c = (int)(id - r * C.chunks) * EPC;
-    const T *s = (const T *)(C.src + r * C.ld_src) + c;
-    u32x4 w;
-    if (c + EPC <= C.cols) __builtin_memcpy(&w, s, 16);
-    else {
-        T v[EPC];
+    for (unsigned j = 0; j < A.per; j++) {
+        const size_t id = ((size_t)(blockIdx.x - C.first) * A.per + j) * 256 + threadIdx.x;
+        if (id >= C.rows * C.chunks) return;
+        // (most copies are small enough for a 32-bit division)
+        const size_t r = id >> 32 ? id / C.chunks : (unsigned)id / (unsigned)C.chunks;
+        const int c = (int)(id - r * C.chunks) * EPC;
+        const T *s = (const T *)(C.src + r * C.ld_src) + c;
+        u32x4 w;
+        if (c + EPC <= C.cols) __builtin_memcpy(&w, s, 16);
+        else {
+            T v[EPC];
 #pragma unroll
-        for (int e = 0; e < EPC; e++) v[e] = c + e < C.cols ? s[e] : (T)0.0f;
-        __builtin_memcpy(&w, v, 16);
+            for (int e = 0; e < EPC; e++) v[e] = c + e < C.cols ? s[e] : (T)0.0f;
+            __builtin_memcpy(&w, v, 16);
+        }
+        char *const d = C.dst + r * C.ld_dst + (size_t)c * sizeof(T);
+        if constexpr (SPLIT) {
+            T v[EPC];
+            __builtin_memcpy(&v, &w, 16);
+            float x[EPC];
+#pragma unroll
+            for (int e = 0; e < EPC; e++) x[e] = (float)v[e];
+            store_oct((__bf16 *)d, x);
+#pragma unroll
+            for (int e = 0; e < EPC; e++) x[e] -= (float)(__bf16)x[e];
+            store_oct((__bf16 *)(d + C.split), x);
+        } else
+            *(u32x4 *)d = w;
     }
-    char *const d = C.dst + r * C.ld_dst + (size_t)c * sizeof(T);
-    if constexpr (SPLIT) {
-        T v[EPC];
-        __builtin_memcpy(&v, &w, 16);
-        float x[EPC];
-#pragma unroll
-        for (int e = 0; e < EPC; e++) x[e] = (float)v[e];
-        store_oct((__bf16 *)d, x);
-#pragma unroll
-        for (int e = 0; e < EPC; e++) x[e] -= (float)(__bf16)x[e];
-        store_oct((__bf16 *)(d + C.split), x);
-    } else
-        *(u32x4 *)d = w;
 }

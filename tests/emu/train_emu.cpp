@@ -222,6 +222,9 @@ extern "C" long emu_errors() { return g_errors; }
 static int g_enough = 192;
 extern "C" void emu_enough_tiles(int n) { g_enough = n; }
 #define TG_ENOUGH_TILES g_enough
+static unsigned g_copy_blocks = 1u << 23;
+extern "C" void emu_copy_blocks(unsigned n) { g_copy_blocks = n; }
+#define TG_COPY_BLOCKS g_copy_blocks
 #include "../../paper_1911_11377_amd/csrc/train_device.hip"
 
 // a context that the training operators accept: they use nothing of its ring

@@ -6,7 +6,8 @@ import torch
 
 import train_emu_support as emu
 import training_range
-from paper_1911_11377_amd import training
+import training_reference as ref
+from paper_1911_11377_amd import ckksmi, training
 
 pytestmark = pytest.mark.skipif(not emu.available, reason="no host compiler with 16-bit float types")
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -212,3 +213,65 @@ def test_the_loss_of_a_step_is_on_the_stream_of_the_step(ctx, monkeypatch, strea
     assert h.step(ctx.guarded(torch.ones(5, 8)), loss, 1e-3, stream=stream) == 7
     assert used == [want] * 4, used
     assert current == ["current"]
+
+
+@pytest.mark.parametrize("rows,widths,dtype,forward,backward", [
+    (2**31 - 257, (8, 128, 8), BF16, True, True),       # 2^23 - 1 tiles of 256 x 256, 512 threads each
+    (2**31 - 257, (8, 129, 8), BF16, False, False),     # two columns of tiles, the gate's
+    (2**30, (8, 129, 8), BF16, False, False),           # 2^23 tiles: one too many
+    (2**30 - 256, (8, 129, 8), BF16, True, True),
+    (2**30, (300, 128, 8), BF16, True, False),          # dx alone has too many
+    (2**31 - 257, (8, 64, 8), F32, True, True),         # 2^24 - 2 tiles of 128 x 128, 256 threads each
+    (2**31 - 257, (8, 65, 8), F32, False, False),
+    (64, (2**20, 2**20, 2**20), BF16, True, False),     # the weights' gradients alone
+    (0, (2**20, 2**20, 2**20), F32, True, True),
+], ids=str)
+def test_launches_that_would_have_too_many_threads_are_refused_first(ctx, rows, widths, dtype, forward, backward):
+    """a launch holds fewer than 2^32 threads along x: EUNSUPPORTED from every entry point of the pass, with nothing enqueued"""
+    ff = training.GatedFF(ctx, *widths, dtype, "square")
+    ff._s.rows = rows
+    a = 1 << 56  # addresses that nothing is done with
+    for which, fits in ((0, forward), (1, backward)):
+        n = C.c_size_t(0)
+        assert ctx._L.ckksmi_gated_ff_workspace_bytes(ctx._h, ff._r, which, C.byref(n)) == (ckksmi.OK if fits else ckksmi.EUNSUPPORTED)
+    args = [a * i for i in range(1, 5)]
+    if not forward:
+        assert ctx._L.ckksmi_gated_ff_forward(ctx._h, ff._r, *args, 5 * a, None, 6 * a, 2**60, None) == ckksmi.EUNSUPPORTED
+    if not backward:
+        assert ctx._L.ckksmi_gated_ff_backward(ctx._h, ff._r, *args, 5 * a, 6 * a, 7 * a, 8 * a, 9 * a, 10 * a, 0, 11 * a, 2**60, None) == ckksmi.EUNSUPPORTED
+
+
+def test_tensors_that_no_launch_holds_are_refused(ctx):
+    z = [torch.zeros(4)]
+    opt = training.AdamW(ctx, z, [z[0].clone()], [z[0].clone()], [z[0].clone()])
+    opt._t[0].n = (2**24 - 1) * 4096 + 1  # 2^24 workgroups of 256 threads
+    with pytest.raises(ckksmi.CkksmiError) as e:
+        opt.step(1e-3, (0.9, 0.99), 1e-8, 0.0, 1)
+    assert e.value.code == ckksmi.EINVAL
+    out = (C.c_void_p * 1)(z[0].data_ptr())
+    opt._t[0].m_unit = opt._t[0].v_unit = opt._t[0].m
+    assert ctx._L.ckksmi_adamw_read_states(ctx._h, opt._t, 1, out, out, None) == ckksmi.EINVAL
+
+
+@pytest.mark.parametrize("dtype,grads", [(BF16, None), (F16, F32)], ids=["bf16", "f16-f32"])
+def test_copies_in_several_pieces_a_workgroup(ctx, dtype, grads):
+    """operands off alignment, copied by fewer workgroups than they have pieces"""
+    ff = training.GatedFF(ctx, 19, 21, 13, dtype, "square", grads)
+    rows, g = 67, torch.Generator().manual_seed(2)
+    x, wg, wu, wd, dy = (ctx.guarded(torch.randn(s, generator=g).to(dtype)) for s in ((rows, 19), (21, 19), (21, 19), (13, 21), (rows, 13)))
+    y, dx = ctx.guarded(torch.zeros(rows, 13, dtype=dtype)), ctx.guarded(torch.zeros(rows, 19, dtype=dtype))
+    dw = [ctx.guarded(torch.zeros(w.shape, dtype=grads or dtype)) for w in (wg, wu, wd)]
+    saved, ws = (ctx.guarded(torch.full((max(16, n),), 255, dtype=torch.uint8)) for n in (ff.saved_bytes(rows), ff.workspace_bytes(rows, backward=True)))
+    results = []
+    for blocks in (1 << 23, 1, 2):
+        ctx._L.emu_copy_blocks(blocks)
+        try:
+            ff.forward(x, wg, wu, wd, y, ws, saved=saved)
+            ff.backward(x, wg, wu, wd, saved, dy, dx, *dw, ws)
+        finally:
+            ctx._L.emu_copy_blocks(1 << 23)
+        results.append([t.clone() for t in (y, dx, *dw)])
+        ws.fill_(255)
+    assert all(torch.equal(a, b) for r in results[1:] for a, b in zip(r, results[0]))
+    want = ref.block(x, wg, wu, wd, training.CUBICS["square"])["y"]
+    assert bool(((y.double() - want[0]).abs() <= want[1]).all())
