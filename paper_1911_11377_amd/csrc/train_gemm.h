@@ -184,9 +184,12 @@ static inline u32x4 lds_read16(LdsPointer p) { return *(const u32x4 *)emu_lds_ch
 static inline unsigned lds_read4(LdsPointer p) { return *(const unsigned *)emu_lds_check(p, 4); }
 static inline s16x4 lds_read_transposed(LdsPointer p) { return emu_read_transposed(emu_lds_check(p, 8)); }
 #else
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is one of the compiler's reserved registers: no value of its own lives there across the block)
 __device__ __forceinline__ void load_to_lds(unsigned lds, unsigned offset, u32x4 descriptor) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(descriptor) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 #define mfma_bf16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
 #define mfma_f16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0)
 #define mfma_f32(a, b, c) __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0)
