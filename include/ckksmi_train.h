@@ -81,7 +81,7 @@ int ckksmi_gated_ff_backward(ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, const v
  * and 0.018 / sqrt(1 - beta2^2) for v: 8 % and, with beta2 = 0.99 and 0.999, 13 % and 40 %.)  v > 0 is never rounded to 0.
  * A block whose unit would be below 1e-36 is held as zeros, one with a value that is not finite gets unit NaN.  The step
  * itself uses m and v before they are rounded.  States start as zeros (bytes and units).
- * Buffers must not overlap.  skip: NULL, or one device int; where it is not 0 when the step runs, the step leaves everything as it is (gradients
+ * No buffer that is written may overlap another (the caller's to see to: a step over many tensors does not look).  skip: NULL, or one device int; where it is not 0 when the step runs, the step leaves everything as it is (gradients
  * that overflowed). */
 #define CKKSMI_STATE_BLOCK 256
 typedef struct {

@@ -113,12 +113,22 @@ class GatedFF:
                        *self._weights(dw_gate, dw_up, dw_down, self.grad_dtype), 1 if accumulate else 0, ckksmi._ptr(ws), ckksmi._nbytes(ws), self.ctx._stream(stream))
 
 
+def _refuse_overlaps(written, read):
+    """raises ValueError where a tensor that is written shares a byte with any other one"""
+    ranges = sorted((t.data_ptr(), t.data_ptr() + ckksmi._nbytes(t), w) for ts, w in ((written, True), (read, False)) for t in ts if t.numel())
+    end = written_end = 0  # of those that begin before
+    for a, b, w in ranges:
+        if a < (end if w else written_end):
+            raise ValueError("tensors overlap or are listed twice")
+        end, written_end = max(end, b), max(written_end, b) if w else written_end
+
+
 class AdamW:
     """Plan of an optimiser step over a list of tensors.
 
     params, grads: tensors of one type each; m, v: float32 tensors, or uint8 with m_units, v_units (float32, one value per
     STATE_BLOCK elements of a tensor): 8-bit states.  copies: bfloat16 or float16 copies of the
-    parameters, renewed by the step.  The buffers are the caller's; the plan keeps them."""
+    parameters, renewed by the step.  The buffers are the caller's; the plan keeps them.  No tensor that a step writes may overlap another."""
 
     def __init__(self, ctx, params, grads, m, v, m_units=None, v_units=None, copies=None):
         import torch
@@ -138,6 +148,7 @@ class AdamW:
         for x, want in ((m, state), (v, state), (m_units, torch.float32), (v_units, torch.float32)):
             if x is not None and any(t.dtype != want for t in x):
                 raise ValueError("states are float32, or uint8 with float32 units")
+        _refuse_overlaps([t for x in (params, m, v, m_units, v_units, copies) if x is not None for t in x], grads)
         o = ckksmi.AdamWParams()
         o.p_dtype = _dtype_code(params[0].dtype) if self.n else ckksmi.F32
         o.grad_dtype = _dtype_code(grads[0].dtype) if self.n else ckksmi.F32

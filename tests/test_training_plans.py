@@ -175,9 +175,8 @@ def test_calls_of_one_plan_do_not_share_what_they_are_given():
     ff.forward(x, *w, y, room, saved=room)
     ff.backward(x, *w, room, y, x, *dw, room)
     ff.workspace_bytes(9)
-    z = [torch.zeros(7)]
     c.meanwhile = lambda: opt.step(2e-3, (0.8, 0.9), 1e-7, 0.2, 9, seed=9)
-    opt = training.AdamW(c, z, z, z, z)
+    opt = training.AdamW(c, *([torch.zeros(7)] for _ in range(4)))
     opt.step(1e-3, (0.9, 0.99), 1e-8, 0.1, 4, seed=3)
     assert {"ckksmi_gated_ff_forward", "ckksmi_gated_ff_backward", "ckksmi_gated_ff_workspace_bytes", "ckksmi_adamw_step"} <= {n for n, _ in c.seen}
     assert all(same for _, same in c.seen), c.seen
@@ -275,3 +274,30 @@ def test_copies_in_several_pieces_a_workgroup(ctx, dtype, grads):
     assert all(torch.equal(a, b) for r in results[1:] for a, b in zip(r, results[0]))
     want = ref.block(x, wg, wu, wd, training.CUBICS["square"])["y"]
     assert bool(((y.double() - want[0]).abs() <= want[1]).all())
+
+
+def test_tensors_that_overlap_are_refused():
+    """a tied weight listed twice, a tensor inside another, states or copies that share memory: two workgroups would update the same bytes.
+    Gradients are read only and may be one tensor; neighbours may touch"""
+    flat = torch.zeros(6000)
+
+    def plan(**kw):
+        d = {k: [torch.zeros(700), torch.zeros(300), torch.zeros(0)] for k in ("params", "grads", "m", "v")}
+        d.update(kw)
+        return training.AdamW(Calls(), d["params"], d["grads"], d["m"], d["v"], copies=d.get("copies"))
+
+    p = [torch.zeros(700), torch.zeros(300), torch.zeros(0)]
+    plan()
+    plan(params=[flat[:700], flat[700:1000], flat[:0]], m=[flat[1000:1700], flat[1700:2000], flat[:0]])
+    plan(grads=[flat[:700], flat[400:700], flat[:0]])
+    shared = torch.zeros(300)
+    for bad in (dict(params=[flat[:700], flat[699:999], flat[:0]]), dict(params=[flat[:700], flat[200:500], flat[:0]]), dict(params=p, grads=p), dict(params=p, m=p),
+                dict(m=[flat[:700], shared, flat[:0]], v=[torch.zeros(700), shared, flat[:0]]), dict(params=p, copies=[t.view(torch.bfloat16)[: t.numel()] for t in p]),
+                dict(grads=[flat[:700], flat[:300], flat[:0]], v=[torch.zeros(700), flat[650:950], flat[:0]])):
+        with pytest.raises(ValueError):
+            plan(**bad)
+    with pytest.raises(ValueError):
+        training.AdamW(Calls(), [shared, shared], *([torch.zeros(300), torch.zeros(300)] for _ in range(3)))
+    units = [torch.zeros(2)]
+    with pytest.raises(ValueError):
+        training.AdamW(Calls(), [torch.zeros(300)], [torch.zeros(300)], *([torch.zeros(300, dtype=torch.uint8)] for _ in range(2)), units, units)
