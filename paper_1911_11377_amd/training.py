@@ -171,6 +171,11 @@ class AdamW:
 
     def step(self, lr, betas, eps, weight_decay, step, grad_scale=1.0, seed=0, skip=None, stream=None):
         """step: 1, 2, ..; seed: another one at every step (8-bit states); skip: None or a device int32 that, if not 0, makes the step do nothing"""
+        if skip is not None and not isinstance(skip, int):
+            import torch
+
+            if skip.dtype != torch.int32 or skip.numel() < 1:  # four bytes are read there
+                raise ValueError("skip is an int32 on the device, got %s of %s" % (tuple(skip.shape), skip.dtype))
         o = ckksmi.AdamWParams.from_buffer_copy(self._o)
         o.lr, o.beta1, o.beta2, o.eps, o.weight_decay, o.grad_scale, o.step = lr, betas[0], betas[1], eps, weight_decay, grad_scale, step
         o.seed, o.skip = seed & (2**64 - 1), ckksmi._ptr(skip)

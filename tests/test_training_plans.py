@@ -301,3 +301,16 @@ def test_tensors_that_overlap_are_refused():
     units = [torch.zeros(2)]
     with pytest.raises(ValueError):
         training.AdamW(Calls(), [torch.zeros(300)], [torch.zeros(300)], *([torch.zeros(300, dtype=torch.uint8)] for _ in range(2)), units, units)
+
+
+def test_skip_is_one_int32():
+    """the step reads four bytes: a truth value or an empty tensor has fewer, and the lower half of other numbers says something else"""
+    c = Calls()
+    opt = training.AdamW(c, *([torch.zeros(7)] for _ in range(4)))
+    for bad in (torch.ones(1, dtype=torch.bool), torch.ones(1, dtype=torch.int64), torch.ones(1), torch.ones(0, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            opt.step(1e-3, (0.9, 0.99), 1e-8, 0.1, 4, skip=bad)
+    assert not c.made
+    opt.step(1e-3, (0.9, 0.99), 1e-8, 0.1, 4, skip=torch.zeros(1, dtype=torch.int32))
+    opt.step(1e-3, (0.9, 0.99), 1e-8, 0.1, 4)
+    assert c.made == ["ckksmi_adamw_step"] * 2
