@@ -181,13 +181,18 @@ class AdamW:
         o.seed, o.skip = seed & (2**64 - 1), ckksmi._ptr(skip)
         self.ctx._call("ckksmi_adamw_step", self.ctx._h, C.byref(o), self._t, self.n, self.ctx._stream(stream))
 
-    def read_states(self, m_out, v_out, stream=None):
-        """8-bit states as the float32 values they stand for, into lists of tensors"""
+    def read_states(self, m_out=None, v_out=None, stream=None):
+        """8-bit states as the float32 values they stand for, into lists of tensors (either may be left out)"""
+        import torch
+
         if self.bits != 8:
             raise ValueError("32-bit states are their own values")
         arrays = []
         for x in (m_out, v_out):
-            if len(x) != self.n or any(t.numel() != self._t[i].n or t.element_size() != 4 for i, t in enumerate(x)):
+            if x is None:
+                arrays.append(None)
+                continue
+            if len(x) != self.n or any(t.numel() != self._t[i].n or t.dtype != torch.float32 for i, t in enumerate(x)):
                 raise ValueError("expected float32 tensors of the parameters' sizes")
             arrays.append((C.c_void_p * max(self.n, 1))(*[ckksmi._ptr(t) for t in x]))
         self.ctx._call("ckksmi_adamw_read_states", self.ctx._h, self._t, self.n, *arrays, self.ctx._stream(stream))

@@ -314,3 +314,21 @@ def test_skip_is_one_int32():
     opt.step(1e-3, (0.9, 0.99), 1e-8, 0.1, 4, skip=torch.zeros(1, dtype=torch.int32))
     opt.step(1e-3, (0.9, 0.99), 1e-8, 0.1, 4)
     assert c.made == ["ckksmi_adamw_step"] * 2
+
+
+def test_one_kind_of_states_is_read_back(ctx):
+    """m or v alone, as the library's call allows; both are what they are together.  Only float32 is written"""
+    n = 700
+    codes = ctx.guarded(torch.arange(n).to(torch.uint8)), ctx.guarded((torch.arange(n) * 3).to(torch.uint8))
+    units = ctx.guarded(torch.tensor([1.0, 0.25, 3.0])), ctx.guarded(torch.tensor([2.0, 1e-3, 0.5]))
+    opt = training.AdamW(ctx, [ctx.guarded(torch.zeros(n))], [ctx.guarded(torch.zeros(n))], [codes[0]], [codes[1]], [units[0]], [units[1]])
+    both, one = [[[ctx.guarded(torch.zeros(n))] for _ in range(2)] for _ in range(2)]
+    opt.read_states(*both)
+    opt.read_states(m_out=one[0])
+    opt.read_states(None, one[1])
+    assert all(torch.equal(a[0], b[0]) and bool(a[0].any()) for a, b in zip(both, one))
+    for bad in ([torch.zeros(n, dtype=torch.int32)], [torch.zeros(n - 1)], []):
+        with pytest.raises(ValueError):
+            opt.read_states(bad, None)
+    with pytest.raises(ckksmi.CkksmiError):
+        opt.read_states()
