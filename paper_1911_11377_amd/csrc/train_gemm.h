@@ -93,8 +93,14 @@ template <class T> __device__ __forceinline__ void load_kept(const char *p, cons
 }
 
 template <class T, int EPI>
-__device__ __forceinline__ void epilogue8(const EpiArgs &E, size_t m, int n, const float (&v0)[8], const float (&v1)[8]) {
+__device__ __forceinline__ void epilogue8(const EpiArgs &E, size_t m, int n, float (&v0)[8], float (&v1)[8]) {
     const size_t at = m * E.ldo + n;
+    // columns that pad a row are zeros: they meet the zeros that pad the next product's other operand, and what an infinite row gives there is NaN
+    if constexpr (EPI != EPI_STORE)
+        if (n + 8 > E.N)
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (n + e >= E.N) v0[e] = v1[e] = 0.0f;
     if constexpr (EPI == EPI_GATE) {
         float h[8];
         if (E.kept.a) {

@@ -117,10 +117,5 @@ __global__ void __launch_bounds__(64 * WAVES) rows_kernel(RowsArgs R) {
 #pragma unroll
             for (int j = 0; j < 4; j++) v[a][4 * e + j] = s[j];
         }
-    // columns beyond the end are kept as zeros in padded rows
-    if constexpr (EPI == EPI_GATE)
-#pragma unroll
-        for (int j = 0; j < 8; j++)
-            if (n + j >= R.N) v[0][j] = v[1][j] = 0.0f;
     epilogue8<T, EPI>(R.epi, m, n, v[0], v[MATS - 1]);
 }

@@ -332,3 +332,28 @@ def test_one_kind_of_states_is_read_back(ctx):
             opt.read_states(bad, None)
     with pytest.raises(ckksmi.CkksmiError):
         opt.read_states()
+
+
+@pytest.mark.parametrize("grads", [None, F32], ids=["16", "fine"])
+@pytest.mark.parametrize("rows,split", [(3, False), (70, False), (260, True)], ids=["few", "tiles", "parts"])
+def test_infinities_are_not_joined_by_what_pads_a_row(ctx, rows, split, grads):
+    """5 hidden units lie in rows of 8: an infinite x or dy (positive weights, all of the row's sums infinite) gives infinite answers and
+    gradients, no NaN out of infinity times the zeros behind the weights' ends"""
+    d_in = 600 if split else 9
+    ff = training.GatedFF(ctx, d_in, 5, 600 if split else 7, BF16, "relu", grads)
+    x, dy = torch.ones(rows, d_in, dtype=BF16), torch.ones(rows, ff.d_out, dtype=BF16)
+    w = [torch.full(s, 0.5, dtype=BF16) for s in ((5, d_in), (5, d_in), (ff.d_out, 5))]
+    x[1, 2], dy[0, 1] = float("inf"), float("inf")
+    x, dy, wg, wu, wd = (ctx.guarded(t) for t in (x, dy, *w))
+    y, dx = ctx.guarded(torch.zeros(rows, ff.d_out, dtype=BF16)), ctx.guarded(torch.zeros(rows, d_in, dtype=BF16))
+    dw = [ctx.guarded(torch.zeros(t.shape, dtype=grads or BF16)) for t in w]
+    saved, ws = (ctx.guarded(torch.full((max(16, n),), 255, dtype=torch.uint8)) for n in (ff.saved_bytes(rows), ff.workspace_bytes(rows, backward=True)))
+    for keep in (saved, None):
+        ff.forward(x, wg, wu, wd, y, ws, saved=keep)
+        assert bool((y[1] == float("inf")).all()) and bool(torch.isfinite(y[torch.arange(rows) != 1]).all())
+    ff.backward(x, wg, wu, wd, saved, dy, dx, *dw, ws)
+    inf_rows = torch.arange(rows) < 2
+    assert bool((dx[inf_rows] == float("inf")).all()) and bool(torch.isfinite(dx[~inf_rows]).all())
+    # (f32 gradients take dg and du in parts, the later ones of an infinite value zeros: NaN where they meet the infinite x)
+    keep = torch.arange(d_in) != 2
+    assert all(bool((d[:, keep] == float("inf")).all()) and not bool(torch.isfinite(d).any()) for d in (dw[0], dw[1]))
