@@ -49,11 +49,14 @@ class GatedFF:
                 raise ValueError("a cubic has four coefficients")
             s.act, s.c = ckksmi.ACT_POLY, (C.c_float * 4)(*cubic)
         self._s, self._r = s, C.byref(s)  # what all calls have in common
+        self._saved_of = (0, 0)  # rows of some call and what they save: replaced as a whole
 
     def _shape(self, rows, ld_x=0, ld_y=0, ld_dy=0, ld_dx=0):
         """a call's own sizes: calls from several threads do not meet in one structure"""
         s = ckksmi.GatedFFShape.from_buffer_copy(self._s)
-        s.rows, s.ld_x, s.ld_y, s.ld_dy, s.ld_dx = rows, ld_x, ld_y, ld_dy, ld_dx
+        s.rows, s.ld_x, s.ld_y = rows, ld_x, ld_y
+        if ld_dy:
+            s.ld_dy, s.ld_dx = ld_dy, ld_dx
         return C.byref(s)
 
     def _bytes(self, name, rows, *args):
@@ -88,9 +91,11 @@ class GatedFF:
                 self._matrix(w_down, self.d_out, self.d_hidden, dtype))
 
     def _saved(self, saved, rows):
-        need = self.saved_bytes(rows)
-        if ckksmi._nbytes(saved) < need:
-            raise ValueError("the buffer for saved activations holds %d bytes of %d" % (ckksmi._nbytes(saved), need))
+        of = self._saved_of
+        if of[0] != rows:
+            of = self._saved_of = (rows, self.saved_bytes(rows))
+        if ckksmi._nbytes(saved) < of[1]:
+            raise ValueError("the buffer for saved activations holds %d bytes of %d" % (ckksmi._nbytes(saved), of[1]))
         return ckksmi._ptr(saved)
 
     def forward(self, x, w_gate, w_up, w_down, y, ws, saved=None, stream=None):
