@@ -42,17 +42,16 @@ inline bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     return x < y + nb && y < x + na;
 }
 
-// A workspace handed out piece by piece; with base == nullptr it only counts
+// A workspace handed out piece by piece (workspace_of() has counted the pieces)
 struct Carve {
     char *base;
-    size_t size, used = 0;
-    Carve(void *p, size_t n) : base((char *)p), size(n) {}
+    size_t used = 0;
+    explicit Carve(void *p) : base((char *)p) {}
     char *take(size_t bytes) {
-        char *p = base ? base + used : nullptr;
+        char *p = base + used;
         used += round_up(bytes, 256);
         return p;
     }
-    bool fits() const { return used <= size; }
 };
 
 // one operand of a product: rows of `cols` elements, `ld` bytes apart
@@ -116,7 +115,9 @@ inline int k_steps(const GemmProblem &p, size_t es) { return (int)(((size_t)p.K 
 //   enough 256 x 256 tiles for three quarters of the compute units: those
 //       (gate, 2048 rows, 1024 -> 4096: 256 x 256 0, 128 x 128 +0.5, 32 x 128 +16)
 //   enough 128 x 128 tiles likewise: those, the k axis whole (dx, 16384 rows, 500 -> 200: whole 0, two parts +7); f32, which the matrix cores
-//       bound rather than the operands' bytes, from two a compute unit on (weights' gradients, 500 rows of 2000 x 1000, 304 tiles: 32 x 128 -17 of 137)
+//       bound rather than the operands' bytes, from two a compute unit on (weights' gradients, 500 rows of 2000 x 1000, 304 tiles: 32 x 128 -17 of 137;
+//       whole passes, 32 x 128 first: 1500 rows of 1500 -> 1500 -> 1500 forward 209 and 265, backward 428 and 420; 512 rows of 2048 -> 2048 -> 2048 114
+//       and 126, 227 and 235; 2048 rows of 1024 -> 4096 -> 1024 398 and 393, 838 and 797; 3000 rows of 512 -> 512 -> 512 52 and 63, 130 and 122)
 //   few tiles of much work: 128 x 128 with the k axis in parts (2048 x 1024 from 4096: 4 parts 0, 2 parts +3, 32 x 128 whole +4, 256 x 256 in 4 parts +9)
 //   else 32 x 128, in parts where that leaves compute units idle
 //       (f32 gate, 1024 rows, 3136 -> 256: 2 parts 0, 4 and 8 parts +2; 128 x 128 in 8 parts +5, in 16 +11)
@@ -287,7 +288,7 @@ size_t workspace_of(const ckksmi_gated_ff &f, bool backward) {
     return (backward ? std::max(forward, back) : forward) + split_bytes(f, backward);
 }
 
-// Few rows: products straight from the operands where they lie.  Up to 64 (64 f32 rows of 3136 -> 256: 20 us, by tiles in 24 parts and
+// Few rows: products straight from the operands where they lie.  Up to 64 (64 f32 rows of 3136 -> 256: 22 us, by tiles in 24 parts and
 // their join 29; one bf16 row of 1024 -> 4096 -> 1024: 14 us, by tiles 21)
 constexpr int kFewRows = 64;
 template <class T, int EPI>
@@ -448,7 +449,7 @@ extern "C" int ckksmi_gated_ff_forward(ckksmi_ctx *c, const ckksmi_gated_ff *ff,
         if (overlap(y, ny, in[i], n_in[i]) || overlap(saved, ns, in[i], n_in[i]) || overlap(ws, need, in[i], n_in[i])) return CKKSMI_EINVAL;
     if (overlap(y, ny, saved, ns) || overlap(ws, need, y, ny) || overlap(ws, need, saved, ns)) return CKKSMI_EINVAL;
     if (ws_bytes < need) return CKKSMI_EWORKSPACE;
-    const Carve w(ws, ws_bytes);
+    const Carve w(ws);
     switch (f.dtype) {
         case CKKSMI_F32: return forward<float>(c, f, x, wg, wu, wd, y, saved, w, S(stream));
         case CKKSMI_BF16: return forward<__bf16>(c, f, x, wg, wu, wd, y, saved, w, S(stream));
@@ -496,7 +497,7 @@ extern "C" int ckksmi_gated_ff_backward(ckksmi_ctx *c, const ckksmi_gated_ff *ff
     for (int i = 0; i < 6; i++)
         if (overlap(ws, need, in[i], n_in[i])) return CKKSMI_EINVAL;
     if (ws_bytes < need) return CKKSMI_EWORKSPACE;
-    const Carve w(ws, ws_bytes);
+    const Carve w(ws);
     switch (f.dtype) {
         case CKKSMI_F32: return backward<float>(c, f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));
         case CKKSMI_BF16: return backward<__bf16>(c, f, x, wg, wu, wd, saved, dy, dx, dwg, dwu, dwd, accumulate != 0, w, S(stream));

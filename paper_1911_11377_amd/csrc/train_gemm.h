@@ -426,10 +426,10 @@ __device__ __forceinline__ void write_tile(const GemmArgs &G, const GemmProblem 
 // The requests stand between that quarter's products, not at once: a load instruction keeps the memory path busy for 16 cycles.
 // Rows of 128 bytes a stage: with four stages of 64 bytes a row the loads reach half the rate (68 GB/s a compute unit against 128) and the
 // forward product of 4096 rows, columns and indices took 147 us instead of 126.
-// Bound by the matrix cores and what keeps them waiting at the barrier: 65 % of the cycles busy there (a library's product: 86 %).
-// Measured, bf16, 16384 rows, 2048 -> 8192 -> 2048: gate with what is kept 1.25 ms (0.88 PFLOP/s; 1.07 GB written after the products,
-// a quarter of the time), down 0.47 ms (1.17), dh 0.80 ms (0.69; 0.8 GB read and 0.54 GB written after the products), dx 0.84 ms
-// (1.30), weights' gradients 1.29 ms (1.28); both products of 4096^3 330 us (1.25).
+// Bound by the matrix cores and what keeps them waiting at the barrier: 59 - 64 % of the cycles busy there (a library's product: 86 %).
+// Measured, bf16, 16384 rows, 2048 -> 8192 -> 2048: gate with what is kept 1.26 ms (0.87 PFLOP/s; 1.07 GB written after the products,
+// a quarter of the time), down 0.48 ms (1.15), dh 0.80 ms (0.69; 0.8 GB read and 0.54 GB written after the products), dx 0.86 ms
+// (1.28), weights' gradients 1.31 ms (1.26); both products of 4096^3 330 - 337 us (1.23).
 template <class T, int BM, int BN, int WM, int WN, bool A_ROWS, bool B_ROWS, int EPI>
 __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) gemm_kernel(GemmArgs G) {
     constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32, SB = 128, HALF = FM / 2;
@@ -542,8 +542,8 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) gemm_kernel(Gem
 // Small tiles, for products that are bound by latency: KG groups of waves share the k axis step by step, each with two LDS
 // stages of 128 bytes of k of its own; group 0 adds up the groups' sums in their order.  One group where there are more tiles
 // than compute units (three or four workgroups share one then) or no more than two steps.
-// Measured: bf16, 333 rows of 517 -> 1021, gate 12 us (176 tiles, four groups; 128 x 128 in two parts and their join 18), weights'
-// gradients of three parts each 17 us (360 tiles, one group; four groups 22); f32, 64 rows, 3136 x 256: 6.8 us (402 tiles; 11.7).
+// Measured: bf16, 333 rows of 517 -> 1021, gate 11 us (176 tiles, four groups; 128 x 128 in two parts and their join 18), weights'
+// gradients of three parts each 17 us (360 tiles, one group; four groups 22); f32, 64 rows, 3136 x 256: 7.7 us (402 tiles; 11.7).
 template <class T, int BM, int BN, int WM, int WN, int KG, bool A_ROWS, bool B_ROWS, int EPI>
 __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_small_kernel(GemmArgs G) {
     constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32, SB = 128;
@@ -635,8 +635,8 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(GemmArgs G) {
 }
 
 // Copies with rows padded to whole 16-byte chunks (zeros behind the last column), for operands whose rows do not begin on them: one launch for
-// all of a call's, 5.4 us for the 2.7 MB of 333 rows of 517 -> 1021 -> 129.  SPLIT: f16 values as the sum of two bf16 ones (their 11 bits fit), the
-// second array `split` bytes behind the first
+// all of a call's, 5.5 us for the 2.7 MB of 333 rows of 517 -> 1021 -> 129.  SPLIT: f16 values as the sum of two bf16 ones (their 11 bits fit), the
+// second array `split` bytes behind the first: 8.8 us for 2048 rows of 1024 and 1024
 #define TG_COPIES 5  // of one call: x, three weight matrices, dy
 struct CopyArgs {
     struct One { const char *src; char *dst; size_t ld_src, ld_dst; int cols, chunks; size_t rows, split; unsigned first; } c[TG_COPIES];

@@ -5,9 +5,9 @@
 // bytes a row.  Both operands come from memory as the fragments that the matrix cores take, 16 bytes a lane (row l % 16, chunk
 // l / 16); the waves' sums meet in LDS and are added in their order.
 // Bound by the weights' bytes and, at these sizes, by the latency of one trip to memory: hence many waves, each with all its
-// loads of two or four runs in flight.  (Four runs of both matrices take the registers of a wave in four: 28 us instead of 20 for
+// loads of two or four runs in flight.  (Four runs of both matrices take the registers of a wave in four: 28 us instead of 24 for
 // 64 f32 rows of 3136 -> 256.)
-// Measured: bf16, one row of 1024 -> 4096 -> 1024: gate 7.3 us (16.8 MB), down 7.0 us (8.4 MB in 64 workgroups), of which a launch
+// Measured: bf16, one row of 1024 -> 4096 -> 1024: gate 7.4 us (16.8 MB), down 6.9 us (8.4 MB in 64 workgroups), of which a launch
 // of this kernel takes 4 us with next to nothing to read; 7 rows of 999 -> 2731 -> 501 (f16, 2-byte alignment) 11 and 10 us.
 #pragma once
 #include "train_gemm.h"
