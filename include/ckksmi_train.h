@@ -36,8 +36,8 @@ extern "C" {
  * x: [rows][d_in], Wg, Wu: [d_hidden][d_in], Wd: [d_out][d_hidden], y: [rows][d_out].  Elements are of `dtype`; sums,
  * activations and their derivatives are formed in 32 bits, and h is rounded to `dtype` before the last product.
  * Weights are dense; rows of x, y, dy, dx may lie further apart: ld_* elements, 0 = dense.  0 <= rows < 2^31 - 256,
- * every dimension and ld 1 .. 2^20; CKKSMI_EUNSUPPORTED where a product of the pass has more tiles than a launch holds (2^23 of 256 x 256
- * results; f32: 2^24 of 128 x 128; of the gate's products half as many columns). */
+ * every dimension and ld 1 .. 2^20; CKKSMI_EUNSUPPORTED where a product of the pass has 2^23 tiles of 256 x 256 results or more (f32: 2^24 of
+ * 128 x 128; of the gate's products half as many columns). */
 typedef struct {
     int dtype;      /* of x, y, the weights, dy, dx and what is saved */
     int grad_dtype; /* of the weights' gradients: dtype or CKKSMI_F32 */
@@ -100,7 +100,8 @@ typedef struct {
     const int *skip;
 } ckksmi_adamw;
 int ckksmi_adamw_step(ckksmi_ctx *ctx, const ckksmi_adamw *opt, const ckksmi_adamw_tensor *tensors /* host */, int n_tensors, void *stream);
-/* What 8-bit states stand for: m_out[i], v_out[i] (host arrays of device pointers, float [n]; either array may be NULL) of tensor i. */
+/* What 8-bit states stand for: m_out[i], v_out[i] (host arrays of device pointers, float [n]; either array may be NULL) of tensor i,
+ * which must not overlap the states or each other. */
 int ckksmi_adamw_read_states(ckksmi_ctx *ctx, const ckksmi_adamw_tensor *tensors /* host */, int n_tensors, float *const *m_out, float *const *v_out, void *stream);
 
 #ifdef __cplusplus
