@@ -63,7 +63,10 @@ extern "C" {
 #define CKKSMI_K_ADAMW 40         /* optimiser step (units: elements, to whole workgroups) */
 #define CKKSMI_K_ADAMW_READ 41    /* 8-bit states read back (the same) */
 #define CKKSMI_K_GEMM_ROWS 42     /* products of few rows with a weight matrix (units: operations) */
-#define CKKSMI_K_COUNT 43
+#define CKKSMI_K_NORM_FORWARD 43  /* norms around a block, forward (units: elements) */
+#define CKKSMI_K_NORM_BACKWARD 44 /* ... backward, with the column sums of long rows (the same) */
+#define CKKSMI_K_NORM_JOIN 45     /* groups' column sums added up (units: columns) */
+#define CKKSMI_K_COUNT 46
 int ckksmi_profile_enable(ckksmi_ctx *ctx, int on);
 int ckksmi_profile_read(ckksmi_ctx *ctx, int kernel_class, double *total_ms, long long *launches, double *units);
 /* name of the kernel that class runs as in this context (the transforms have size-specific kernels; a fused kernel's variants for

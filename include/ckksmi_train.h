@@ -3,7 +3,8 @@
  *
  * What it is for: the weights of an encrypted network are trained on plain data, with the polynomials that the encrypted
  * schedules can evaluate in place of the activation (section 2.2; the paper trains such networks on a GPU, section 3.2).
- * Two operators: a gated feed-forward block with its backward pass, and an AdamW step over many tensors at once.
+ * Operators: a gated feed-forward block and the norms around it, with their backward passes; AdamW steps and steps along
+ * orthogonalised momentum over many tensors at once; the block's answers from 4-bit weights.
  *
  * Conventions are those of ckksmi.h (int return codes, device pointers, caller's memory, stream argument, nothing
  * allocated, nothing synchronised, nothing enqueued by a failed call), with these differences: the operands are
@@ -65,6 +66,45 @@ int ckksmi_gated_ff_forward(ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, const vo
 int ckksmi_gated_ff_backward(ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, const void *x, const void *w_gate, const void *w_up, const void *w_down,
                              const void *saved, const void *dy, void *dx, void *dw_gate, void *dw_up, void *dw_down, int accumulate,
                              void *ws, size_t ws_bytes, void *stream);
+
+/* Norms before and after a block, its gate and the residual sum, on `rows` rows of d elements: with f a block's results,
+ *     r = residual_scale * x + block_scale * gate * N_post(f)        what goes on to the next block's sum,
+ *     n = N_pre(r)                                                   what the next block reads.
+ * N(v) = (v - mean) / sqrt(mean of (v - mean)^2 + eps) * w + b, the mean taken as 0 for CKKSMI_NORM_RMS (which has no b), N(v) = v for
+ * CKKSMI_NORM_NONE.  f may be NULL (in front of the first block): n = N_pre(x); then r, gate and post's weights have to be NULL.
+ * x, f, r, n and an element gate are of `dtype`, rows ld_* elements apart (0 = dense); w, b [d] and a channel gate [d] of
+ * weight_dtype; a NULL w is ones, a NULL b zeros.  Everything is formed in 32 bits (n from r before it is rounded) and rounded once.
+ * 0 <= rows < 2^31 - 256, d and every ld 1 .. 2^20.  eps >= 0 and the scales finite. */
+#define CKKSMI_NORM_NONE 0
+#define CKKSMI_NORM_RMS 1
+#define CKKSMI_NORM_LAYER 2
+#define CKKSMI_GATE_NONE 0
+#define CKKSMI_GATE_CHANNEL 1 /* one value a column */
+#define CKKSMI_GATE_ELEMENT 2 /* one value an element */
+typedef struct {
+    int dtype, weight_dtype; /* weight_dtype: dtype or CKKSMI_F32 */
+    int pre, post;           /* CKKSMI_NORM_* */
+    int gate;                /* CKKSMI_GATE_* */
+    float eps, residual_scale, block_scale;
+    int64_t rows, d;
+    int64_t ld_x, ld_f, ld_gate, ld_r, ld_n;            /* ld_gate: an element gate's */
+    int64_t ld_dr, ld_dn, ld_dx, ld_df, ld_dgate;
+} ckksmi_residual_norm;
+
+/* of the backward pass on up to `rows` rows; of what a forward pass saves for it (four floats a row) */
+int ckksmi_residual_norm_workspace_bytes(const ckksmi_ctx *ctx, const ckksmi_residual_norm *rn, size_t *bytes);
+int ckksmi_residual_norm_saved_bytes(const ckksmi_ctx *ctx, const ckksmi_residual_norm *rn, size_t *bytes);
+/* r may be NULL (nobody reads it) unless pre is NONE; n is NULL if and only if pre is NONE.  r may be x itself (same address and ld);
+ * otherwise outputs must not overlap inputs or each other.  saved: NULL or a buffer for the backward pass. */
+int ckksmi_residual_norm_forward(ckksmi_ctx *ctx, const ckksmi_residual_norm *rn, const void *x, const void *f, const void *gate, const void *post_w, const void *post_b,
+                                 const void *pre_w, const void *pre_b, void *r, void *n, void *saved, void *stream);
+/* Gradients from dr (of r; NULL: zeros) and dn (of n; NULL: zeros): of x, f and an element gate (each may be NULL: not wanted), and, summed
+ * over the rows, of the weights, biases and a channel gate (weight_dtype; each may be NULL; accumulate != 0: added to what the buffer holds).
+ * x, f, gate, weights and `saved` as in the forward pass.  A gradient of something that the forward pass does not have must be NULL.
+ * Outputs must not overlap inputs or each other.  The sums' order depends on the sizes alone. */
+int ckksmi_residual_norm_backward(ckksmi_ctx *ctx, const ckksmi_residual_norm *rn, const void *x, const void *f, const void *gate, const void *post_w, const void *post_b,
+                                  const void *pre_w, const void *saved, const void *dr, const void *dn, void *dx, void *df, void *dgate, void *dpost_w, void *dpost_b,
+                                  void *dpre_w, void *dpre_b, int accumulate, void *ws, size_t ws_bytes, void *stream);
 
 /* AdamW step (decoupled weight decay) over n_tensors tensors, element by element, with g = grad_scale * grad:
  *     m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2

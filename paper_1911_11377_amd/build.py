@@ -5,7 +5,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libckksmi.so")
-SOURCES = ["ckksmi_device.hip", "train_device.hip", "host_math.cpp", "host_crypto.cpp"]
+SOURCES = ["ckksmi_device.hip", "train_device.hip", "norm_device.hip", "host_math.cpp", "host_crypto.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -27,7 +27,7 @@ def build(force=True):
     objects = ["%s.%d.o" % (tmp, i) for i in range(len(srcs))]
     compile_flags = [f for f in FLAGS if f != "-shared"]
     try:
-        # the two device sources take minutes and half a minute: side by side
+        # the device sources take up to minutes: side by side
         running = [subprocess.Popen([HIPCC] + compile_flags + ["-c", "-x", "hip", s, "-o", o]) for s, o in zip(srcs, objects)]
         failed = [s for s, p in zip(srcs, running) if p.wait() != 0]
         if failed:

@@ -37,6 +37,8 @@ class Params(C.Structure):
 F32, BF16, F16 = 0, 1, 2
 ACT_POLY, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 STATE_BLOCK = 256
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+GATE_NONE, GATE_CHANNEL, GATE_ELEMENT = 0, 1, 2
 
 
 class GatedFFShape(C.Structure):  # ckksmi_gated_ff
@@ -52,6 +54,12 @@ class AdamWParams(C.Structure):  # ckksmi_adamw
     _fields_ = [("p_dtype", C.c_int), ("grad_dtype", C.c_int), ("copy_dtype", C.c_int), ("state_bits", C.c_int), ("lr", C.c_double), ("beta1", C.c_double),
                 ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double), ("grad_scale", C.c_double), ("step", C.c_int64),
                 ("seed", C.c_uint64), ("skip", VP)]
+
+
+class ResidualNormShape(C.Structure):  # ckksmi_residual_norm
+    _fields_ = [("dtype", C.c_int), ("weight_dtype", C.c_int), ("pre", C.c_int), ("post", C.c_int), ("gate", C.c_int), ("eps", C.c_float),
+                ("residual_scale", C.c_float), ("block_scale", C.c_float), ("rows", C.c_int64), ("d", C.c_int64)] + [
+                    ("ld_" + k, C.c_int64) for k in ("x", "f", "gate", "r", "n", "dr", "dn", "dx", "df", "dgate")]
 
 
 class CkksmiError(RuntimeError):
@@ -113,14 +121,18 @@ SIGNATURES = {
     "ckksmi_gated_ff_backward": [VP, C.POINTER(GatedFFShape)] + [VP] * 10 + [C.c_int, VP, C.c_size_t, VP],
     "ckksmi_adamw_step": [VP, C.POINTER(AdamWParams), C.POINTER(AdamWTensor), C.c_int, VP],
     "ckksmi_adamw_read_states": [VP, C.POINTER(AdamWTensor), C.c_int, C.POINTER(VP), C.POINTER(VP), VP],
+    "ckksmi_residual_norm_workspace_bytes": [VP, C.POINTER(ResidualNormShape), C.POINTER(C.c_size_t)],
+    "ckksmi_residual_norm_saved_bytes": [VP, C.POINTER(ResidualNormShape), C.POINTER(C.c_size_t)],
+    "ckksmi_residual_norm_forward": [VP, C.POINTER(ResidualNormShape)] + [VP] * 11,
+    "ckksmi_residual_norm_backward": [VP, C.POINTER(ResidualNormShape)] + [VP] * 16 + [C.c_int, VP, C.c_size_t, VP],
     "ckksmi_profile_enable": [VP, C.c_int],
     "ckksmi_profile_read": [VP, C.c_int, f64p, C.POINTER(C.c_longlong), f64p],
     "ckksmi_kernel_class_name": [VP, C.c_int],
     "ckksmi_tune": [VP, C.c_int, C.c_int],
 }
 _RESTYPES = {"ckksmi_ctx_destroy": None, "ckksmi_strerror": C.c_char_p, "ckksmi_kernel_class_name": C.c_char_p}
-TRAINING = ("ckksmi_gated_ff_", "ckksmi_adamw_")  # entry points of csrc/train_device.hip
-K_COUNT = 43
+TRAINING = ("ckksmi_gated_ff_", "ckksmi_adamw_", "ckksmi_residual_norm_")  # entry points of include/ckksmi_train.h
+K_COUNT = 46
 
 _LIBS = {}
 

@@ -1,9 +1,10 @@
 """Training in the clear of weights that are evaluated under encryption (argument marshalling only).
 
-The paper trains its network on plain data with the polynomials that replace the activations (sections 2.2, 3.2).  Two
+The paper trains its network on plain data with the polynomials that replace the activations (sections 2.2, 3.2).  The
 operators, plans over the entry points of include/ckksmi_train.h:
-  GatedFF : y = (act(x Wg^T) * (x Wu^T)) Wd^T, forward and backward; act a cubic of the encrypted schedules or what they replace
-  AdamW   : one optimiser step over many tensors, states in 32 or 8 bits
+  GatedFF      : y = (act(x Wg^T) * (x Wu^T)) Wd^T, forward and backward; act a cubic of the encrypted schedules or what they replace
+  ResidualNorm : the norms before and after a block with its gate and residual sum, forward and backward
+  AdamW        : one optimiser step over many tensors, states in 32 or 8 bits
 Device buffers are torch tensors on the context's GPU and stay the caller's; calls enqueue on torch's current stream unless
 told otherwise and allocate nothing.
 """
@@ -28,6 +29,17 @@ def _dtype_code(dtype):
     if dtype not in codes:
         raise ValueError("expected float32, bfloat16 or float16, got %r" % (dtype,))
     return codes[dtype]
+
+
+def _rows_of(x, width, dtype, rows=None):
+    """a [rows][width] tensor whose rows are contiguous: address and distance of its rows"""
+    if x.dim() != 2 or x.shape[1] != width or (rows is not None and x.shape[0] != rows) or x.dtype != dtype:
+        raise ValueError("expected [%s][%d] of %s, got %s of %s" % ("rows" if rows is None else rows, width, dtype, tuple(x.shape), x.dtype))
+    if x.stride(1) != 1 and width > 1:
+        raise ValueError("rows must be contiguous")
+    if x.shape[0] > 1 and x.stride(0) < width:  # (0, a row repeated by expand(), would be taken for dense rows)
+        raise ValueError("rows must not overlap: %d elements apart, %d wide" % (x.stride(0), width))
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else width
 
 
 class GatedFF:
@@ -71,16 +83,6 @@ class GatedFF:
     def saved_bytes(self, rows):
         return self._bytes("ckksmi_gated_ff_saved_bytes", rows)
 
-    def _rows_of(self, x, width, dtype, rows=None):
-        """a [rows][width] tensor whose rows are contiguous: address and distance of its rows"""
-        if x.dim() != 2 or x.shape[1] != width or (rows is not None and x.shape[0] != rows) or x.dtype != dtype:
-            raise ValueError("expected [%s][%d] of %s, got %s of %s" % ("rows" if rows is None else rows, width, dtype, tuple(x.shape), x.dtype))
-        if x.stride(1) != 1 and width > 1:
-            raise ValueError("rows must be contiguous")
-        if x.shape[0] > 1 and x.stride(0) < width:  # (0, a row repeated by expand(), would be taken for dense rows)
-            raise ValueError("rows must not overlap: %d elements apart, %d wide" % (x.stride(0), width))
-        return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else width
-
     def _matrix(self, w, d0, d1, dtype):
         if tuple(w.shape) != (d0, d1) or w.dtype != dtype:
             raise ValueError("expected [%d][%d] of %s, got %s of %s" % (d0, d1, dtype, tuple(w.shape), w.dtype))
@@ -102,8 +104,8 @@ class GatedFF:
         """y = (act(x Wg^T) * (x Wu^T)) Wd^T; saved: a buffer of saved_bytes(rows) for the backward pass, or None"""
         rows = x.shape[0]
         sp = self._saved(saved, rows) if saved is not None else None
-        px, ld_x = self._rows_of(x, self.d_in, self.dtype)
-        py, ld_y = self._rows_of(y, self.d_out, self.dtype, rows)
+        px, ld_x = _rows_of(x, self.d_in, self.dtype)
+        py, ld_y = _rows_of(y, self.d_out, self.dtype, rows)
         self.ctx._call("ckksmi_gated_ff_forward", self.ctx._h, self._shape(rows, ld_x, ld_y), px, *self._weights(w_gate, w_up, w_down, self.dtype), py, sp, ckksmi._ptr(ws),
                        ckksmi._nbytes(ws), self.ctx._stream(stream))
 
@@ -111,11 +113,91 @@ class GatedFF:
         """gradients of the weights (added to the buffers' contents if accumulate) and of x (dx may be None)"""
         rows = x.shape[0]
         sp = self._saved(saved, rows)
-        px, ld_x = self._rows_of(x, self.d_in, self.dtype)
-        pdy, ld_dy = self._rows_of(dy, self.d_out, self.dtype, rows)
-        pdx, ld_dx = self._rows_of(dx, self.d_in, self.dtype, rows) if dx is not None else (None, 0)
+        px, ld_x = _rows_of(x, self.d_in, self.dtype)
+        pdy, ld_dy = _rows_of(dy, self.d_out, self.dtype, rows)
+        pdx, ld_dx = _rows_of(dx, self.d_in, self.dtype, rows) if dx is not None else (None, 0)
         self.ctx._call("ckksmi_gated_ff_backward", self.ctx._h, self._shape(rows, ld_x, 0, ld_dy, ld_dx), px, *self._weights(w_gate, w_up, w_down, self.dtype), sp, pdy, pdx,
                        *self._weights(dw_gate, dw_up, dw_down, self.grad_dtype), 1 if accumulate else 0, ckksmi._ptr(ws), ckksmi._nbytes(ws), self.ctx._stream(stream))
+
+
+class ResidualNorm:
+    """Plan of what stands between two blocks, for rows of d elements; any number of rows:
+        r = residual_scale * x + block_scale * gate * N_post(f),   n = N_pre(r)
+    f: what the block gave; r: the residual stream, n: what the next block reads.  pre, post: "rms", "layer" or None; gate: None, "channel"
+    (a learned [d]) or "element" (a tensor like f).  weight_dtype: of the norms' weights, biases and a channel gate, float32 or dtype.
+    Weights that are left out are ones, biases zeros."""
+
+    def __init__(self, ctx, d, dtype, pre="rms", post="rms", gate=None, weight_dtype=None, eps=1e-5, residual_scale=1.0, block_scale=1.0):
+        kinds = {None: ckksmi.NORM_NONE, "rms": ckksmi.NORM_RMS, "layer": ckksmi.NORM_LAYER}
+        gates = {None: ckksmi.GATE_NONE, "channel": ckksmi.GATE_CHANNEL, "element": ckksmi.GATE_ELEMENT}
+        if pre not in kinds or post not in kinds or gate not in gates:
+            raise ValueError("norms are None, 'rms' or 'layer', gates None, 'channel' or 'element'; got %r, %r, %r" % (pre, post, gate))
+        self.ctx, self.d, self.dtype, self.weight_dtype, self.gate = ctx, d, dtype, weight_dtype or dtype, gate
+        s = ckksmi.ResidualNormShape()
+        s.dtype, s.weight_dtype, s.pre, s.post, s.gate = _dtype_code(dtype), _dtype_code(self.weight_dtype), kinds[pre], kinds[post], gates[gate]
+        s.eps, s.residual_scale, s.block_scale, s.d = eps, residual_scale, block_scale, d
+        self._s = s  # what all calls have in common
+
+    def _shape(self, rows):
+        s = ckksmi.ResidualNormShape.from_buffer_copy(self._s)
+        s.rows = rows
+        return s
+
+    def _bytes(self, name, rows):
+        n = C.c_size_t(0)
+        self.ctx._call(name, self.ctx._h, C.byref(self._shape(rows)), C.byref(n))
+        return n.value
+
+    def workspace_bytes(self, rows):
+        """of the backward pass on up to `rows` rows"""
+        return self._bytes("ckksmi_residual_norm_workspace_bytes", rows)
+
+    def saved_bytes(self, rows):
+        return self._bytes("ckksmi_residual_norm_saved_bytes", rows)
+
+    def _vector(self, w):
+        if w is not None and (tuple(w.shape) != (self.d,) or w.dtype != self.weight_dtype):
+            raise ValueError("expected [%d] of %s, got %s of %s" % (self.d, self.weight_dtype, tuple(w.shape), w.dtype))
+        return ckksmi._ptr(w)
+
+    def _rows(self, s, **tensors):
+        """addresses of tensors of rows (None stays None); their distances into the call's structure"""
+        out = []
+        for name, x in tensors.items():
+            p, ld = _rows_of(x, self.d, self.dtype, s.rows) if x is not None else (None, 0)
+            setattr(s, "ld_" + name, ld)
+            out.append(p)
+        return out
+
+    def _gate(self, s, name, g):
+        return self._rows(s, **{name: g})[0] if self.gate == "element" else self._vector(g)
+
+    def _saved(self, saved, rows):
+        if saved is not None and ckksmi._nbytes(saved) < 16 * rows:
+            raise ValueError("the buffer for saved statistics holds %d bytes of %d" % (ckksmi._nbytes(saved), 16 * rows))
+        return ckksmi._ptr(saved)
+
+    def forward(self, x, f, r, n, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, saved=None, stream=None):
+        """f None: n = N_pre(x), r None.  r may be x; None: not wanted.  n is None where pre is.  saved: a buffer of saved_bytes(rows) for the
+        backward pass, or None"""
+        s = self._shape(x.shape[0])
+        px, pf, pr, pn = self._rows(s, x=x, f=f, r=r, n=n)
+        w = [self._vector(v) for v in (post_weight, post_bias, pre_weight, pre_bias)]
+        self.ctx._call("ckksmi_residual_norm_forward", self.ctx._h, C.byref(s), px, pf, self._gate(s, "gate", gate), *w, pr, pn, self._saved(saved, s.rows), self.ctx._stream(stream))
+
+    def backward(self, x, f, saved, dr, dn, ws, dx=None, df=None, dgate=None, dpost_weight=None, dpost_bias=None, dpre_weight=None, dpre_bias=None, gate=None,
+                 post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, accumulate=False, stream=None):
+        """dr, dn: gradients of r and n (None: zeros).  Gradients that are None are not formed; accumulate: those of weights, biases and a channel
+        gate are added to what their buffers hold.  ws: workspace_bytes(rows), None where none of them is wanted.  (pre_bias plays no part)"""
+        s = self._shape(x.shape[0])
+        px, pf, pdr, pdn, pdx, pdf = self._rows(s, x=x, f=f, dr=dr, dn=dn, dx=dx, df=df)
+        w = [self._vector(v) for v in (post_weight, post_bias, pre_weight)]
+        self._vector(pre_bias)
+        dw = [self._vector(v) for v in (dpost_weight, dpost_bias, dpre_weight, dpre_bias)]
+        if saved is None:
+            raise ValueError("the backward pass reads what a forward pass saved")
+        self.ctx._call("ckksmi_residual_norm_backward", self.ctx._h, C.byref(s), px, pf, self._gate(s, "gate", gate), *w, self._saved(saved, s.rows), pdr, pdn, pdx, pdf,
+                       self._gate(s, "dgate", dgate), *dw, 1 if accumulate else 0, ckksmi._ptr(ws), ckksmi._nbytes(ws) if ws is not None else 0, self.ctx._stream(stream))
 
 
 def _refuse_overlaps(written, read):

@@ -214,6 +214,17 @@ unsigned emu_wave_max(unsigned v) {
     return m;
 }
 
+float emu_lanes_sum(float x, int lanes) {
+    for (int by = 1; by < lanes; by *= 2) {
+        put(x);
+        wave_sync();
+        const float y = get<float>((g_cur % 64) ^ by);
+        wave_sync();
+        x += y;
+    }
+    return x;
+}
+
 extern "C" void *emu_alloc(size_t bytes) { return emu::guarded_alloc(bytes); }
 extern "C" void emu_free(void *p) { emu::guarded_free(p); }
 extern "C" long emu_errors() { return g_errors; }
@@ -226,6 +237,7 @@ static unsigned g_copy_blocks = 1u << 23;
 extern "C" void emu_copy_blocks(unsigned n) { g_copy_blocks = n; }
 #define TG_COPY_BLOCKS g_copy_blocks
 #include "../../paper_1911_11377_amd/csrc/train_device.hip"
+#include "../../paper_1911_11377_amd/csrc/norm_device.hip"
 
 // a context that the training operators accept: they use nothing of its ring
 extern "C" ckksmi_ctx *emu_train_context() {

@@ -27,3 +27,5 @@ emu_f32x4 emu_mfma_f16(emu_f16x8 first, emu_f16x8 second, emu_f32x4 c);
 emu_f32x4 emu_mfma_f32(float first, float second, emu_f32x4 c);
 emu_s16x4 emu_read_transposed(const char *p);
 unsigned emu_wave_max(unsigned v);
+// sum over the groups of `lanes` lanes, pairs first: every lane gets the same bits
+float emu_lanes_sum(float x, int lanes);

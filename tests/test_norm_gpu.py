@@ -1,0 +1,153 @@
+"""Norms around a block on the GPU against 64 bits: the sizes, kinds, strides and values where they could go wrong."""
+import math
+
+import pytest
+import torch
+
+import norm_reference as nr
+from norm_reference import BF16, F16, F32
+from paper_1911_11377_amd import ckksmi, training
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = ckksmi.Context(4, 3, 20, 1, 21, 1, device=0)
+    yield c
+    c.close()
+
+
+def off_alignment(t):
+    """a copy that begins one element behind a whole 16 bytes, among NaN"""
+    buf = torch.full((t.numel() + 24,), math.nan, device=DEV).to(t.dtype) if t.is_floating_point() else torch.zeros(t.numel() + 24, dtype=t.dtype, device=DEV)
+    lead = 1 if t.is_floating_point() else 16
+    v = buf[lead:lead + t.numel()].view(t.shape)
+    v.copy_(t)
+    return v
+
+
+SIZES = nr.SIZES + [(300, 64), (1000, 24), (257, 513), (4097, 40), (64, 2048), (33, 4096), (9, 8192), (5, 8191), (3, 12000), (2, 16384), (3, 16385), (2, 40001), (1, 2**17)]
+
+
+@pytest.mark.parametrize("rows,d", SIZES, ids=str)
+@pytest.mark.parametrize("dtype,wt", [(F32, None), (BF16, F32), (F16, None)], ids=["f32", "bf16", "f16"])
+def test_sizes(ctx, rows, d, dtype, wt):
+    pre, post, gate = nr.KINDS[(rows + d) % 2]
+    nr.check(ctx, nr.Case(rows, d, dtype, pre, post, gate, wt, device=DEV), device=DEV)
+
+
+@pytest.mark.parametrize("pre,post,gate", nr.KINDS, ids=str)
+@pytest.mark.parametrize("dtype,wt", [(BF16, None), (F32, None), (F16, F32)], ids=["bf16", "f32", "f16"])
+@pytest.mark.parametrize("d", [75, 1021, 8200])
+def test_kinds(ctx, pre, post, gate, dtype, wt, d):
+    """strided rows among NaN, addresses off alignment, sums added to what is there"""
+    nr.check(ctx, nr.Case(37, d, dtype, pre, post, gate, wt, lead=3, device=DEV, place=off_alignment), device=DEV, accumulate=True)
+
+
+@pytest.mark.parametrize("pre", ["rms", "layer"])
+def test_the_first_norm_has_no_block_before_it(ctx, pre):
+    nr.check(ctx, nr.Case(70, 90, BF16, pre, None, None, with_f=False, device=DEV), device=DEV)
+    nr.check(ctx, nr.Case(5, 9000, F32, pre, "layer", "channel", with_f=False, weights=False, device=DEV), device=DEV)
+
+
+@pytest.mark.parametrize("dr,dn", [(False, True), (True, False)])
+def test_gradients_that_are_not_there(ctx, dr, dn):
+    nr.check(ctx, nr.Case(50, 400, F32, "rms", "rms", "channel", device=DEV), device=DEV, dr=dr, dn=dn)
+
+
+@pytest.mark.parametrize("d", [16, 600, 8200])
+def test_large_means_and_magnitudes(ctx, d):
+    c = nr.Case(4, d, F32, "layer", "layer", None, device=DEV)
+    c.x[0] += 1000.0
+    c.f[1] = c.f[1] * 1e15
+    c.x[2] = c.x[2] * 1e-12
+    c.f[2] = c.f[2] * 1e-12
+    c.f[3] = 0.0
+    nr.check(ctx, c, device=DEV)
+
+
+@pytest.mark.parametrize("d", [20, 16390])
+def test_values_that_are_not_finite_stay_in_their_row(ctx, d):
+    for kind in ("rms", "layer"):
+        c = nr.Case(3, d, BF16, kind, None, None, F32, device=DEV)
+        plan = training.ResidualNorm(ctx, d, BF16, kind, None, None, F32)
+        plan.forward(c.x, c.f, c.r, c.n, **c.w)
+        before = c.n.clone()
+        c.x[1, 3] = math.inf
+        plan.forward(c.x, c.f, c.r, c.n, **c.w)
+        assert torch.equal(c.n[0], before[0]) and torch.equal(c.n[2], before[2])
+        assert math.isinf(float(c.r[1, 3])) and bool(torch.isnan(c.n[1, 3]))
+        others = torch.cat([c.n[1, :3], c.n[1, 4:]])
+        assert bool((others == 0).all()) if kind == "rms" else bool(torch.isnan(others).all())
+
+
+@pytest.mark.parametrize("rows,d", [(3, 40), (700, 2048), (3, 16390)])
+def test_the_sum_may_overwrite_x(ctx, rows, d):
+    c = nr.Case(rows, d, BF16, "layer", "rms", "channel", F32, device=DEV)
+    plan = training.ResidualNorm(ctx, d, BF16, "layer", "rms", "channel", F32)
+    plan.forward(c.x, c.f, c.r, c.n, gate=c.gate, **c.w)
+    n = torch.empty_like(c.n)
+    plan.forward(c.x, c.f, c.x, n, gate=c.gate, **c.w)
+    assert torch.equal(c.x, c.r) and torch.equal(n, c.n)
+
+
+@pytest.mark.parametrize("d", [520, 8200])
+def test_equal_calls_give_equal_bits_on_any_stream_and_in_graphs(ctx, d):
+    c = nr.Case(333, d, BF16, "layer", "layer", "channel", F32, device=DEV)
+    plan = training.ResidualNorm(ctx, d, BF16, "layer", "layer", "channel", F32)
+    saved, ws = (torch.full((n,), 255, dtype=torch.uint8, device=DEV) for n in (plan.saved_bytes(333), plan.workspace_bytes(333)))
+    g = c.gradients()
+
+    def step():
+        plan.forward(c.x, c.f, c.r, c.n, gate=c.gate, saved=saved, **c.w)
+        plan.backward(c.x, c.f, saved, c.dr, c.dn, ws, gate=c.gate, **g, **c.w)
+
+    def results():
+        return [c.r, c.n] + list(g.values())
+
+    step()
+    first = [t.clone() for t in results()]
+    side = torch.cuda.Stream()
+    for t in results():
+        t.fill_(math.nan)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(results(), first))
+    graph = torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for _ in range(3):
+        for t in results():
+            t.fill_(math.nan)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(results(), first))
+
+
+def test_fewer_rows_in_a_larger_workspace(ctx):
+    plan = training.ResidualNorm(ctx, 24, F32, "rms", "rms")
+    ws = torch.full((plan.workspace_bytes(5000),), 255, dtype=torch.uint8, device=DEV)
+    for rows in (1, 31, 257, 4999):
+        c = nr.Case(rows, 24, F32, "rms", "rms", None, device=DEV, seed=rows)
+        saved = torch.zeros(plan.saved_bytes(rows), dtype=torch.uint8, device=DEV)
+        plan.forward(c.x, c.f, c.r, c.n, saved=saved, **c.w)
+        g = c.gradients()
+        plan.backward(c.x, c.f, saved, c.dr, c.dn, ws, **g, **c.w)
+        want = nr.residual_norm(c.x, c.f, None, c.w, "rms", "rms", float(torch.tensor(1e-5)), 1.0, 1.0, c.dr, c.dn)
+        for k, t in g.items():
+            nr.within(t, want[k], F32, k)
+
+
+def test_no_rows(ctx):
+    plan = training.ResidualNorm(ctx, 12, BF16, "layer", "rms", "channel", F32)
+    none = torch.empty(0, 12, dtype=BF16, device=DEV)
+    for accumulate in (True, False):
+        g = {k: torch.full((12,), 3.0, device=DEV) for k in ("dpost_weight", "dpre_weight", "dpre_bias", "dgate")}
+        plan.backward(none, none, torch.empty(0, dtype=torch.uint8, device=DEV), none, none, None, gate=torch.ones(12, device=DEV), accumulate=accumulate, **g)
+        assert all(bool((t == (3.0 if accumulate else 0.0)).all()) for t in g.values())
