@@ -66,7 +66,10 @@ extern "C" {
 #define CKKSMI_K_NORM_FORWARD 43  /* norms around a block, forward (units: elements) */
 #define CKKSMI_K_NORM_BACKWARD 44 /* ... backward, with the column sums of long rows (the same) */
 #define CKKSMI_K_NORM_JOIN 45     /* groups' column sums added up (units: columns) */
-#define CKKSMI_K_COUNT 46
+#define CKKSMI_K_SERIES 46        /* products of orthogonalised directions (units: operations) */
+#define CKKSMI_K_SERIES_JOIN 47   /* parts of their split k axes added up (units: operations of the products) */
+#define CKKSMI_K_SERIES_PASS 48   /* momentum, normalisation, parameters (units: workgroups) */
+#define CKKSMI_K_COUNT 49
 int ckksmi_profile_enable(ckksmi_ctx *ctx, int on);
 int ckksmi_profile_read(ckksmi_ctx *ctx, int kernel_class, double *total_ms, long long *launches, double *units);
 /* name of the kernel that class runs as in this context (the transforms have size-specific kernels; a fused kernel's variants for

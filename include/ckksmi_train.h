@@ -144,6 +144,51 @@ int ckksmi_adamw_step(ckksmi_ctx *ctx, const ckksmi_adamw *opt, const ckksmi_ada
  * which must not overlap the states or each other. */
 int ckksmi_adamw_read_states(ckksmi_ctx *ctx, const ckksmi_adamw_tensor *tensors /* host */, int n_tensors, float *const *m_out, float *const *v_out, void *stream);
 
+/* Steps along orthogonalised directions, for matrices.  The direction of a matrix u (rows x cols) is
+ *     X = u / (|u| + eps)   (|u|: root of the sum of squares),   then `steps` times   X <- a X + (b A + c A^2) X,  A = X X^T
+ * (on u^T where rows > cols): the odd polynomial a s + b s^3 + c s^5 applied to u's singular values s, which the steps drive towards one.
+ * The polynomials must keep singular values from [0, 1] below 2, and |b| s^2 + |c| s^4 below 100, at every step (CKKSMI_EINVAL).  u = 0 has direction 0.
+ * Rounding errors of X grow by up to a^steps in directions that u is weak in, as they would in any arithmetic.  X is held in two f16 parts
+ * (22 bits, scaled to the matrix), the diagonals of A and of the polynomial in f32.  Directions that end in bf16 (or move 16-bit
+ * parameters) come from products of the upper parts alone, 6e-4 of the direction's size off; others from three products of the parts, as good as
+ * f32 products.  Any finite u; an infinity or NaN makes the direction NaN (and 0).
+ * Sizes 0 .. 2^16 each (a matrix without elements is left out); numbers of any type are contiguous.  A tensor's results depend on its own
+ * numbers and on the sizes in the call alone. */
+typedef struct {
+    double a, b, c;     /* 3.4445, -4.7750, 2.0315 reach [0.7, 1.2] from most singular values in five steps */
+    double eps;         /* >= 0 */
+    int steps;          /* 1 .. 32 */
+} ckksmi_series;
+typedef struct {
+    const void *in;     /* rows x cols elements of the call's dtype */
+    void *out;          /* the direction, likewise; may be `in` */
+    int64_t rows, cols;
+} ckksmi_direction;
+/* tensors: host array; outputs must not overlap other tensors (the caller's to see to, like the workspace) */
+int ckksmi_orthogonalise_workspace_bytes(const ckksmi_ctx *ctx, const ckksmi_series *s, const ckksmi_direction *tensors /* host */, int n_tensors, int dtype, size_t *bytes);
+int ckksmi_orthogonalise(ckksmi_ctx *ctx, const ckksmi_series *s, const ckksmi_direction *tensors /* host */, int n_tensors, int dtype, void *ws, size_t ws_bytes, void *stream);
+
+/* Step over n_tensors matrices: with g = grad_scale * grad,
+ *     m <- momentum m + (1 - momentum) g,     u = nesterov ? momentum m + (1 - momentum) g : m,
+ *     p <- (1 - lr weight_decay) p - lr scale direction(u)
+ * each product and sum rounded by itself to 32 bits, p to its type at the end. */
+typedef struct {
+    void *p;            /* rows x cols elements of p_dtype */
+    const void *grad;   /* ... of grad_dtype */
+    float *m;           /* ... momentum, starts as zeros */
+    void *copy;         /* NULL, or ... of copy_dtype (bf16 or f16): p after the step */
+    int64_t rows, cols;
+    double scale;       /* of the update, e.g. sqrt(max(1, rows / cols)) */
+} ckksmi_muon_tensor;
+typedef struct {
+    int p_dtype, grad_dtype, copy_dtype, nesterov;
+    double lr, momentum, weight_decay, grad_scale;
+    const int *skip;    /* as for AdamW */
+    ckksmi_series series;
+} ckksmi_muon;
+int ckksmi_muon_workspace_bytes(const ckksmi_ctx *ctx, const ckksmi_muon *opt, const ckksmi_muon_tensor *tensors /* host */, int n_tensors, size_t *bytes);
+int ckksmi_muon_step(ckksmi_ctx *ctx, const ckksmi_muon *opt, const ckksmi_muon_tensor *tensors /* host */, int n_tensors, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -62,6 +62,23 @@ class ResidualNormShape(C.Structure):  # ckksmi_residual_norm
                     ("ld_" + k, C.c_int64) for k in ("x", "f", "gate", "r", "n", "dr", "dn", "dx", "df", "dgate")]
 
 
+class Series(C.Structure):  # ckksmi_series
+    _fields_ = [("a", C.c_double), ("b", C.c_double), ("c", C.c_double), ("eps", C.c_double), ("steps", C.c_int)]
+
+
+class DirectionTensor(C.Structure):  # ckksmi_direction
+    _fields_ = [("in_", VP), ("out", VP), ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class MuonTensor(C.Structure):  # ckksmi_muon_tensor
+    _fields_ = [("p", VP), ("grad", VP), ("m", VP), ("copy", VP), ("rows", C.c_int64), ("cols", C.c_int64), ("scale", C.c_double)]
+
+
+class MuonParams(C.Structure):  # ckksmi_muon
+    _fields_ = [("p_dtype", C.c_int), ("grad_dtype", C.c_int), ("copy_dtype", C.c_int), ("nesterov", C.c_int), ("lr", C.c_double), ("momentum", C.c_double),
+                ("weight_decay", C.c_double), ("grad_scale", C.c_double), ("skip", VP), ("series", Series)]
+
+
 class CkksmiError(RuntimeError):
     def __init__(self, code, what, detail=""):
         self.code = code
@@ -125,14 +142,18 @@ SIGNATURES = {
     "ckksmi_residual_norm_saved_bytes": [VP, C.POINTER(ResidualNormShape), C.POINTER(C.c_size_t)],
     "ckksmi_residual_norm_forward": [VP, C.POINTER(ResidualNormShape)] + [VP] * 11,
     "ckksmi_residual_norm_backward": [VP, C.POINTER(ResidualNormShape)] + [VP] * 16 + [C.c_int, VP, C.c_size_t, VP],
+    "ckksmi_orthogonalise_workspace_bytes": [VP, C.POINTER(Series), C.POINTER(DirectionTensor), C.c_int, C.c_int, C.POINTER(C.c_size_t)],
+    "ckksmi_orthogonalise": [VP, C.POINTER(Series), C.POINTER(DirectionTensor), C.c_int, C.c_int, VP, C.c_size_t, VP],
+    "ckksmi_muon_workspace_bytes": [VP, C.POINTER(MuonParams), C.POINTER(MuonTensor), C.c_int, C.POINTER(C.c_size_t)],
+    "ckksmi_muon_step": [VP, C.POINTER(MuonParams), C.POINTER(MuonTensor), C.c_int, VP, C.c_size_t, VP],
     "ckksmi_profile_enable": [VP, C.c_int],
     "ckksmi_profile_read": [VP, C.c_int, f64p, C.POINTER(C.c_longlong), f64p],
     "ckksmi_kernel_class_name": [VP, C.c_int],
     "ckksmi_tune": [VP, C.c_int, C.c_int],
 }
 _RESTYPES = {"ckksmi_ctx_destroy": None, "ckksmi_strerror": C.c_char_p, "ckksmi_kernel_class_name": C.c_char_p}
-TRAINING = ("ckksmi_gated_ff_", "ckksmi_adamw_", "ckksmi_residual_norm_")  # entry points of include/ckksmi_train.h
-K_COUNT = 46
+TRAINING = ("ckksmi_gated_ff_", "ckksmi_adamw_", "ckksmi_residual_norm_", "ckksmi_orthogonalise", "ckksmi_muon_")  # entry points of include/ckksmi_train.h
+K_COUNT = 49
 
 _LIBS = {}
 

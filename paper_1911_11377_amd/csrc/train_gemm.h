@@ -20,7 +20,9 @@
 
 #define TG_OUTSIDE 0x80000000u  // a lane offset beyond every descriptor's end
 
-enum { EPI_GATE = 0, EPI_STORE = 1, EPI_DHID = 2 };
+// GRAM, SQUARE and APPLY are train_series.h's: products of other problems than GemmProblem, with its own epilogues
+enum { EPI_GATE = 0, EPI_STORE = 1, EPI_DHID = 2, EPI_GRAM = 3, EPI_SQUARE = 4, EPI_APPLY = 5 };
+constexpr bool symmetric(int epi) { return epi == EPI_GRAM || epi == EPI_SQUARE; }  // only tiles that reach the diagonal from below
 
 // What the forward pass saves and the backward pass reads: act(g) and u act'(g), in 32 bits where the weights' gradients are f32.
 // 16-bit gradients need them in 24 bits only: their roundings to 16 bits are then dg's, du's and h's own and no others
@@ -58,6 +60,7 @@ struct GemmProblem {
 
 #define TG_PROBLEMS 3
 struct GemmArgs {
+    typedef GemmProblem Problem;
     GemmProblem p[TG_PROBLEMS];
     int first[TG_PROBLEMS + 1];  // tiles of the problems before
     int n_problems;
@@ -306,11 +309,21 @@ __device__ __forceinline__ int xcd_order(int wg, int total) {
     return x * per + (x < rest ? x : rest) + i;
 }
 
+// Tiles that reach the diagonal from below, row by row: BN / BM = R tile rows have the same number of them, the next R one more
+template <int R> __device__ __forceinline__ void triangle_tile(int tile, int &row, int &col) {
+    int g = (int)((sqrtf(8.0f * (tile / R) + 1.0f) - 1.0f) * 0.5f);  // (near enough: whole numbers decide)
+    while (R * ((long long)g * (g + 1) / 2) > tile) g--;
+    while (R * ((long long)(g + 1) * (g + 2) / 2) <= tile) g++;
+    const int rest = tile - (int)(R * ((long long)g * (g + 1) / 2));
+    row = R * g + rest / (g + 1);
+    col = rest % (g + 1);
+}
+
 // A workgroup's tile and its walk along the sources' k axes
-template <class T, int BM, int BN, bool A_ROWS, bool B_ROWS, int EPI, class LA, class LB, int EVERY>
+template <class T, int BM, int BN, bool A_ROWS, bool B_ROWS, int EPI, class LA, class LB, int EVERY, class Args>
 struct TileWalk {
     static constexpr bool GATE = EPI == EPI_GATE;
-    const GemmProblem *P;
+    const typename Args::Problem *P;
     int m0, n0;
     LA la;
     LB lb;
@@ -319,16 +332,23 @@ struct TileWalk {
     const char *pa, *pb, *pb1;
     int wave;
 
-    __device__ __forceinline__ TileWalk(const GemmArgs &G, int wave_, int lane, int group) : wave(wave_) {
+    __device__ __forceinline__ TileWalk(const Args &G, int wave_, int lane, int group) : wave(wave_) {
         int tile = xcd_order(blockIdx.x, gridDim.x), pi = 0;
         while (pi + 1 < G.n_problems && tile >= G.first[pi + 1]) pi++;
         tile -= G.first[pi];
         P = &G.p[pi];
-        constexpr int GROUP = 8;
-        const int band = tile / (GROUP * P->tiles_n), in_band = tile % (GROUP * P->tiles_n);
-        const int band_rows = min(GROUP, P->tiles_m - band * GROUP);
-        m0 = (band * GROUP + in_band % band_rows) * BM;
-        n0 = in_band / band_rows * (GATE ? BN / 2 : BN);
+        if constexpr (symmetric(EPI)) {
+            int row, col;
+            triangle_tile<BN / BM>(tile, row, col);
+            m0 = row * BM;
+            n0 = col * BN;
+        } else {
+            constexpr int GROUP = 8;
+            const int band = tile / (GROUP * P->tiles_n), in_band = tile % (GROUP * P->tiles_n);
+            const int band_rows = min(GROUP, P->tiles_m - band * GROUP);
+            m0 = (band * GROUP + in_band % band_rows) * BM;
+            n0 = in_band / band_rows * (GATE ? BN / 2 : BN);
+        }
         la.init(wave, lane, P->lda, P->M - m0);
         lb.init(wave, lane, P->ldb, P->N - n0);
         // steps s0 .. s1 - 1 of the sources', one source behind the other
@@ -363,7 +383,7 @@ struct TileWalk {
     // moves on by EVERY steps
     __device__ __forceinline__ void advance() {
         step += EVERY;
-        if (EPI == EPI_STORE && step >= per_src && src + 1 < P->nsrc) return enter();
+        if ((EPI == EPI_STORE || EPI >= EPI_GRAM) && step >= per_src && src + 1 < P->nsrc) return enter();
         pa += EVERY * a_step;
         pb += EVERY * b_step;
         if constexpr (GATE) pb1 += EVERY * b_step;
@@ -377,9 +397,11 @@ struct TileWalk {
     template <int WN> static __device__ __forceinline__ int b_row(int wn, int p) { return GATE ? p % 2 * (BN / 2) + wn * (WN / 2) + p / 2 * 32 : wn * WN + 32 * p; }
 };
 
+template <int EPI> struct SeriesEpilogue;  // (train_series.h)
+
 // A wave's results to memory, 8 neighbouring columns at a time
-template <class T, int EPI, int FM, int PAIRS, int WN>
-__device__ __forceinline__ void write_tile(const GemmArgs &G, const GemmProblem &P, int m_wave, int n0, int wn, int lane, const f32x4 (&acc)[FM][2 * PAIRS]) {
+template <class T, int EPI, int FM, int PAIRS, int WN, class Args>
+__device__ __forceinline__ void write_tile(const Args &G, const typename Args::Problem &P, int m_wave, int n0, int wn, int lane, const f32x4 (&acc)[FM][2 * PAIRS]) {
     constexpr bool GATE = EPI == EPI_GATE;
     static_assert(!GATE || PAIRS % 2 == 0, "a wave holds the same columns of both products");
     const int i = lane & 15, q = lane >> 4;
@@ -410,9 +432,10 @@ __device__ __forceinline__ void write_tile(const GemmArgs &G, const GemmProblem 
 #pragma unroll
             for (int p = 0; p < PAIRS; p++) {
                 const int n = n0 + wn * WN + 32 * p + 8 * q;
-                if (n >= P.N) continue;
+                if (n >= P.N || (symmetric(EPI) && n > m)) continue;
                 eight(p, v0);
                 if (G.splits > 1) store_oct(P.part + ((size_t)blockIdx.y * P.M + m) * P.ld_part + n, v0);
+                else if constexpr (EPI >= EPI_GRAM) SeriesEpilogue<EPI>::eight(P, m, n, v0);
                 else epilogue8<T, EPI>(P.epi, m, n, v0, v0);
             }
         }
@@ -430,12 +453,12 @@ __device__ __forceinline__ void write_tile(const GemmArgs &G, const GemmProblem 
 // Measured, bf16, 16384 rows, 2048 -> 8192 -> 2048: gate with what is kept 1.26 ms (0.87 PFLOP/s; 1.07 GB written after the products,
 // a quarter of the time), down 0.48 ms (1.15), dh 0.80 ms (0.69; 0.8 GB read and 0.54 GB written after the products), dx 0.86 ms
 // (1.28), weights' gradients 1.31 ms (1.26); both products of 4096^3 330 - 337 us (1.23).
-template <class T, int BM, int BN, int WM, int WN, bool A_ROWS, bool B_ROWS, int EPI>
-__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) gemm_kernel(GemmArgs G) {
+template <class T, int BM, int BN, int WM, int WN, bool A_ROWS, bool B_ROWS, int EPI, class Args = GemmArgs>
+__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) gemm_kernel(Args G) {
     constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32, SB = 128, HALF = FM / 2;
     typedef TileLoad<T, BM, SB, A_ROWS, false, WAVES, false> LA;
     typedef TileLoad<T, BN, SB, B_ROWS, true, WAVES, EPI == EPI_GATE> LB;
-    typedef TileWalk<T, BM, BN, A_ROWS, B_ROWS, EPI, LA, LB, 1> Walk;
+    typedef TileWalk<T, BM, BN, A_ROWS, B_ROWS, EPI, LA, LB, 1, Args> Walk;
     constexpr int STAGE = LA::BYTES + LB::BYTES, LOADS = Walk::LOADS;
     __shared__ __attribute__((aligned(1024))) char stages[2 * STAGE];
     TG_LDS(stages);
@@ -544,12 +567,12 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) gemm_kernel(Gem
 // than compute units (three or four workgroups share one then) or no more than two steps.
 // Measured: bf16, 333 rows of 517 -> 1021, gate 11 us (176 tiles, four groups; 128 x 128 in two parts and their join 18), weights'
 // gradients of three parts each 17 us (360 tiles, one group; four groups 22); f32, 64 rows, 3136 x 256: 7.7 us (402 tiles; 11.7).
-template <class T, int BM, int BN, int WM, int WN, int KG, bool A_ROWS, bool B_ROWS, int EPI>
-__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_small_kernel(GemmArgs G) {
+template <class T, int BM, int BN, int WM, int WN, int KG, bool A_ROWS, bool B_ROWS, int EPI, class Args = GemmArgs>
+__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_small_kernel(Args G) {
     constexpr int WAVES = (BM / WM) * (BN / WN), FM = WM / 16, PAIRS = WN / 32, SB = 128;
     typedef TileLoad<T, BM, SB, A_ROWS, false, WAVES, false> LA;
     typedef TileLoad<T, BN, SB, B_ROWS, true, WAVES, EPI == EPI_GATE> LB;
-    typedef TileWalk<T, BM, BN, A_ROWS, B_ROWS, EPI, LA, LB, KG> Walk;
+    typedef TileWalk<T, BM, BN, A_ROWS, B_ROWS, EPI, LA, LB, KG, Args> Walk;
     constexpr int STAGE = LA::BYTES + LB::BYTES;
     __shared__ __attribute__((aligned(1024))) char stages[KG * 2 * STAGE];
     TG_LDS(stages);

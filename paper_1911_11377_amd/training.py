@@ -5,6 +5,7 @@ operators, plans over the entry points of include/ckksmi_train.h:
   GatedFF      : y = (act(x Wg^T) * (x Wu^T)) Wd^T, forward and backward; act a cubic of the encrypted schedules or what they replace
   ResidualNorm : the norms before and after a block with its gate and residual sum, forward and backward
   AdamW        : one optimiser step over many tensors, states in 32 or 8 bits
+  Muon         : one optimiser step over many matrices along their orthogonalised momentum; Orthogonalise: such directions alone
 Device buffers are torch tensors on the context's GPU and stay the caller's; calls enqueue on torch's current stream unless
 told otherwise and allocate nothing.
 """
@@ -210,6 +211,14 @@ def _refuse_overlaps(written, read):
         end, written_end = max(end, b), max(written_end, b) if w else written_end
 
 
+def _check_skip(skip):
+    if skip is not None and not isinstance(skip, int):
+        import torch
+
+        if skip.dtype != torch.int32 or skip.numel() < 1:  # four bytes are read there
+            raise ValueError("skip is an int32 on the device, got %s of %s" % (tuple(skip.shape), skip.dtype))
+
+
 class AdamW:
     """Plan of an optimiser step over a list of tensors.
 
@@ -258,11 +267,7 @@ class AdamW:
 
     def step(self, lr, betas, eps, weight_decay, step, grad_scale=1.0, seed=0, skip=None, stream=None):
         """step: 1, 2, ..; seed: another one at every step (8-bit states); skip: None or a device int32 that, if not 0, makes the step do nothing"""
-        if skip is not None and not isinstance(skip, int):
-            import torch
-
-            if skip.dtype != torch.int32 or skip.numel() < 1:  # four bytes are read there
-                raise ValueError("skip is an int32 on the device, got %s of %s" % (tuple(skip.shape), skip.dtype))
+        _check_skip(skip)
         o = ckksmi.AdamWParams.from_buffer_copy(self._o)
         o.lr, o.beta1, o.beta2, o.eps, o.weight_decay, o.grad_scale, o.step = lr, betas[0], betas[1], eps, weight_decay, grad_scale, step
         o.seed, o.skip = seed & (2**64 - 1), ckksmi._ptr(skip)
@@ -283,3 +288,101 @@ class AdamW:
                 raise ValueError("expected float32 tensors of the parameters' sizes")
             arrays.append((C.c_void_p * max(self.n, 1))(*[ckksmi._ptr(t) for t in x]))
         self.ctx._call("ckksmi_adamw_read_states", self.ctx._h, self._t, self.n, *arrays, self.ctx._stream(stream))
+
+
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)  # of s, s^3, s^5: five steps bring most singular values to [0.7, 1.2]
+
+
+def _series(eps, steps, coefficients):
+    s = ckksmi.Series()
+    s.a, s.b, s.c = coefficients
+    s.eps, s.steps = eps, steps
+    return s
+
+
+def _matrices(lists):
+    """types of lists of matrices of equal shapes (lists that are None are left out)"""
+    first = lists[0]
+    for x in lists:
+        if x is None:
+            continue
+        if len(x) != len(first):
+            raise ValueError("lists of different lengths")
+        for t, of in zip(x, first):
+            if t.dim() != 2 or t.shape != of.shape:
+                raise ValueError("expected matrices of equal shapes, got %s and %s" % (tuple(t.shape), tuple(of.shape)))
+        if len({t.dtype for t in x}) > 1:
+            raise ValueError("tensors of one list have one type")
+
+
+class Orthogonalise:
+    """Plan of directions: outputs[i] = the odd polynomial (a s + b s^3 + c s^5, `steps` times) of inputs[i]'s singular values, in units of its
+    Frobenius norm.  Matrices of one type; outputs[i] may be inputs[i], no output may overlap anything else."""
+
+    def __init__(self, ctx, inputs, outputs):
+        self.ctx, self.n, self._keep = ctx, len(inputs), (inputs, outputs)
+        _matrices(self._keep)
+        if self.n and inputs[0].dtype != outputs[0].dtype:
+            raise ValueError("directions have their matrices' type")
+        apart = [u for u, o in zip(inputs, outputs) if u.data_ptr() != o.data_ptr()]
+        _refuse_overlaps(outputs, apart)
+        self._dtype = _dtype_code(inputs[0].dtype) if self.n else ckksmi.F32
+        self._t = (ckksmi.DirectionTensor * max(self.n, 1))()
+        for t, u, o in zip(self._t, inputs, outputs):
+            t.in_, t.out, t.rows, t.cols = ckksmi._ptr(u), ckksmi._ptr(o), u.shape[0], u.shape[1]
+
+    def workspace_bytes(self):
+        n = C.c_size_t(0)
+        self.ctx._call("ckksmi_orthogonalise_workspace_bytes", self.ctx._h, C.byref(_series(0.0, 1, (1.0, 0.0, 0.0))), self._t, self.n, self._dtype, C.byref(n))
+        return n.value
+
+    def run(self, ws, eps=1e-7, steps=5, coefficients=COEFFICIENTS, stream=None):
+        s = _series(eps, steps, coefficients)
+        self.ctx._call("ckksmi_orthogonalise", self.ctx._h, C.byref(s), self._t, self.n, self._dtype, ckksmi._ptr(ws), ckksmi._nbytes(ws), self.ctx._stream(stream))
+
+
+class Muon:
+    """Plan of a step over a list of matrices along their orthogonalised momentum: m <- momentum m + (1 - momentum) g, u = nesterov ? momentum m +
+    (1 - momentum) g : m, p <- (1 - lr weight_decay) p - lr scale direction(u).
+
+    params, grads: matrices of one type each; m: float32, starting as zeros; copies: bfloat16 or float16 copies of the parameters, renewed by the
+    step; scales: one factor a matrix, by default sqrt(max(1, rows / cols)).  The buffers are the caller's; the plan keeps them.  No
+    tensor that a step writes may overlap another."""
+
+    def __init__(self, ctx, params, grads, m, copies=None, scales=None):
+        import torch
+
+        self.ctx, self.n = ctx, len(params)
+        self._keep = (params, grads, m, copies)
+        _matrices(self._keep)
+        if any(t.dtype != torch.float32 for t in m):
+            raise ValueError("momentum is float32")
+        if scales is None:
+            scales = [max(1.0, p.shape[0] / max(p.shape[1], 1)) ** 0.5 for p in params]
+        if len(scales) != self.n:
+            raise ValueError("lists of different lengths")
+        _refuse_overlaps([t for x in (params, m, copies) if x is not None for t in x], grads)
+        o = ckksmi.MuonParams()
+        o.p_dtype = _dtype_code(params[0].dtype) if self.n else ckksmi.F32
+        o.grad_dtype = _dtype_code(grads[0].dtype) if self.n else ckksmi.F32
+        o.copy_dtype = _dtype_code(copies[0].dtype) if copies else ckksmi.BF16
+        o.grad_scale, o.series = 1.0, _series(0.0, 1, (1.0, 0.0, 0.0))
+        self._o = o  # what all steps have in common
+        self._t = (ckksmi.MuonTensor * max(self.n, 1))()
+        for i in range(self.n):
+            t = self._t[i]
+            t.p, t.grad, t.m, t.copy = ckksmi._ptr(params[i]), ckksmi._ptr(grads[i]), ckksmi._ptr(m[i]), ckksmi._ptr(copies[i]) if copies is not None else None
+            t.rows, t.cols, t.scale = params[i].shape[0], params[i].shape[1], scales[i]
+
+    def workspace_bytes(self):
+        n = C.c_size_t(0)
+        self.ctx._call("ckksmi_muon_workspace_bytes", self.ctx._h, C.byref(self._o), self._t, self.n, C.byref(n))
+        return n.value
+
+    def step(self, lr, momentum, ws, weight_decay=0.0, nesterov=True, eps=1e-7, steps=5, coefficients=COEFFICIENTS, grad_scale=1.0, skip=None, stream=None):
+        """skip: None or a device int32 that, if not 0, makes the step do nothing"""
+        _check_skip(skip)
+        o = ckksmi.MuonParams.from_buffer_copy(self._o)
+        o.lr, o.momentum, o.weight_decay, o.grad_scale, o.nesterov = lr, momentum, weight_decay, grad_scale, 1 if nesterov else 0
+        o.skip, o.series = ckksmi._ptr(skip), _series(eps, steps, coefficients)
+        self.ctx._call("ckksmi_muon_step", self.ctx._h, C.byref(o), self._t, self.n, ckksmi._ptr(ws), ckksmi._nbytes(ws), self.ctx._stream(stream))

@@ -238,6 +238,7 @@ extern "C" void emu_copy_blocks(unsigned n) { g_copy_blocks = n; }
 #define TG_COPY_BLOCKS g_copy_blocks
 #include "../../paper_1911_11377_amd/csrc/train_device.hip"
 #include "../../paper_1911_11377_amd/csrc/norm_device.hip"
+#include "../../paper_1911_11377_amd/csrc/muon_device.hip"
 
 // a context that the training operators accept: they use nothing of its ring
 extern "C" ckksmi_ctx *emu_train_context() {

@@ -1,0 +1,150 @@
+"""Orthogonalised directions and steps along them on the GPU, against 64 bits."""
+import math
+
+import pytest
+import torch
+
+import series_reference as sr
+from paper_1911_11377_amd import ckksmi, training
+from series_reference import BF16, F16, F32
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = ckksmi.Context(4, 3, 20, 1, 21, 1, device=0)
+    yield c
+    c.close()
+
+
+def room(n):
+    return torch.full((max(n, 16),), 255, dtype=torch.uint8, device=DEV)
+
+
+def off_alignment(t):
+    """on the GPU, one element behind a whole 16 bytes, between NaN"""
+    buf = torch.full((t.numel() + 24,), math.nan, dtype=t.dtype, device=DEV)
+    v = buf[1:1 + t.numel()].view(t.shape)
+    v.copy_(t)
+    return v
+
+
+def direct(ctx, u, **kw):
+    out = off_alignment(torch.full(u.shape, math.nan, dtype=u.dtype))
+    plan = training.Orthogonalise(ctx, [u], [out])
+    plan.run(room(plan.workspace_bytes()), **kw)
+    return out
+
+
+@pytest.mark.parametrize("rows,cols", sr.SIZES + [(1, 65536), (3, 20001), (129, 513), (256, 256), (300, 700), (513, 129), (64, 5000), (1021, 517)], ids=str)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+def test_sizes(ctx, rows, cols, dtype):
+    u = off_alignment(sr.matrix(rows, cols, rows + cols, "strong" if rows > 100 else "normal", dtype))
+    sr.check(direct(ctx, u), u, 1 if dtype == BF16 else 2)
+
+
+@pytest.mark.parametrize("kind", ["strong", "falling", "rank3"])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+def test_spectra(ctx, kind, dtype):
+    u = sr.matrix(200, 330, 3, kind, dtype).to(DEV)
+    sr.check(direct(ctx, u), u, 1 if dtype == BF16 else 2)
+
+
+@pytest.mark.parametrize("count,rows,cols", [(16, 256, 1024), (1, 1024, 1024), (5, 700, 1300), (40, 264, 520)], ids=str)
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_many_matrices(ctx, count, rows, cols, dtype):
+    """enough tiles of 128 x 128 and of 256 x 256, split k axes, more than a launch's table; every matrix has the bits that it has in a call
+    with the same sizes, the first and the last are compared with 64 bits"""
+    us = [sr.matrix(*((rows, cols) if i % 3 else (cols, rows)), i, "strong", dtype).to(DEV) for i in range(count)]
+    outs = [torch.full_like(u, math.nan) for u in us]
+    plan = training.Orthogonalise(ctx, us, outs)
+    plan.run(room(plan.workspace_bytes()))
+    for i in {0, count - 1}:
+        sr.check(outs[i], us[i], 1 if dtype == BF16 else 2)
+    first = [o.clone() for o in outs]
+    plan.run(room(plan.workspace_bytes()))
+    assert all(torch.equal(a, b) for a, b in zip(first, outs))
+
+
+def test_in_place_zeros_and_small_numbers(ctx):
+    u = sr.matrix(120, 300, 4).to(DEV)
+    want, start = direct(ctx, u), u.clone()
+    plan = training.Orthogonalise(ctx, [u], [u])
+    plan.run(room(plan.workspace_bytes()))
+    assert torch.equal(u, want)
+    z = torch.zeros(90, 20, device=DEV)
+    assert bool((direct(ctx, z) == 0).all()) and bool((direct(ctx, z, eps=0.0) == 0).all())
+    for scale in (1e-30, 1e30):
+        sr.check(direct(ctx, start * scale, eps=0.0), start * scale, 2, eps=0.0)
+
+
+def test_values_that_are_not_finite(ctx):
+    for bad in (math.nan, math.inf):
+        u, v = sr.matrix(10, 200, 6).to(DEV), sr.matrix(80, 30, 7).to(DEV)
+        u[3, 4] = bad
+        outs = [torch.zeros_like(t) for t in (u, v)]
+        plan = training.Orthogonalise(ctx, [u, v], outs)
+        plan.run(room(plan.workspace_bytes()))
+        assert bool(torch.isnan(outs[0]).any()) and not bool((outs[0][torch.isfinite(outs[0])] != 0).any())
+        sr.check(outs[1], v, 2)
+
+
+@pytest.mark.parametrize("dtype,gt,copy", [(F32, BF16, BF16), (F32, F32, None), (BF16, BF16, None), (F16, F32, F16)], ids=str)
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_steps(ctx, dtype, gt, copy, nesterov):
+    sizes = [(160, 400), (400, 160), (0, 7), (1, 9), (333, 333), (5, 0)] + [(30, 40)] * 22
+    p0 = [sr.matrix(*s, i, scale=0.1, dtype=dtype) for i, s in enumerate(sizes)]
+    g = [sr.matrix(*s, 100 + i, scale=10.0 ** (-i % 5), dtype=gt).to(DEV) for i, s in enumerate(sizes)]
+    m0 = [sr.matrix(*s, 200 + i, scale=10.0 ** (-i % 5)) for i, s in enumerate(sizes)]
+    p, m = [off_alignment(t) for t in p0], [off_alignment(t) for t in m0]
+    copies = [torch.zeros(s, dtype=copy, device=DEV) for s in sizes] if copy else None
+    opt = training.Muon(ctx, p, g, m, copies=copies)
+    opt.step(0.02, 0.9, room(opt.workspace_bytes()), weight_decay=0.1, nesterov=nesterov, grad_scale=0.5)
+    for i, (r, c) in enumerate(sizes):
+        if not r * c:
+            continue
+        wm, u = sr.momentum(m0[i], g[i], 0.9, 0.5, nesterov)
+        assert torch.equal(m[i].cpu(), wm)
+        sr.check_step(p[i], p0[i], u, 2 if dtype == F32 else 1, 0.02, max(1.0, r / c) ** 0.5, 0.1, copies[i] if copies else None)
+
+
+def test_equal_calls_give_equal_bits_on_any_stream_and_in_graphs(ctx):
+    sizes = [(160, 1100), (400, 160), (70, 70)]
+    p0 = [sr.matrix(*s, i, scale=0.1).to(DEV) for i, s in enumerate(sizes)]
+    g = [sr.matrix(*s, 100 + i).to(DEV) for i, s in enumerate(sizes)]
+    p, m = [t.clone() for t in p0], [torch.zeros_like(t) for t in p0]
+    skip = torch.zeros(1, dtype=torch.int32, device=DEV)
+    opt = training.Muon(ctx, p, g, m)
+    ws = room(opt.workspace_bytes())
+
+    def begin():
+        for t, s, z in zip(p, p0, m):
+            t.copy_(s)
+            z.zero_()
+
+    def step():
+        opt.step(0.02, 0.9, ws, weight_decay=0.1, skip=skip)
+
+    step()
+    first = [t.clone() for t in p + m]
+    side = torch.cuda.Stream()
+    begin()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(p + m, first))
+    graph = torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for i in range(4):
+        begin()
+        ws.fill_(255)
+        skip.fill_(i == 2)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = first if i != 2 else p0 + [torch.zeros_like(t) for t in p0]
+        assert all(torch.equal(a, b) for a, b in zip(p + m, want)), i
