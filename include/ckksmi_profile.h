@@ -69,7 +69,9 @@ extern "C" {
 #define CKKSMI_K_SERIES 46        /* products of orthogonalised directions (units: operations) */
 #define CKKSMI_K_SERIES_JOIN 47   /* parts of their split k axes added up (units: operations of the products) */
 #define CKKSMI_K_SERIES_PASS 48   /* momentum, normalisation, parameters (units: workgroups) */
-#define CKKSMI_K_COUNT 49
+#define CKKSMI_K_ROWS4 49         /* products of few rows with a 4-bit matrix (units: operations) */
+#define CKKSMI_K_PACK4 50         /* matrices to 4 bits and back (units: elements) */
+#define CKKSMI_K_COUNT 51
 int ckksmi_profile_enable(ckksmi_ctx *ctx, int on);
 int ckksmi_profile_read(ckksmi_ctx *ctx, int kernel_class, double *total_ms, long long *launches, double *units);
 /* name of the kernel that class runs as in this context (the transforms have size-specific kernels; a fused kernel's variants for

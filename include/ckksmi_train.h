@@ -189,6 +189,35 @@ typedef struct {
 int ckksmi_muon_workspace_bytes(const ckksmi_ctx *ctx, const ckksmi_muon *opt, const ckksmi_muon_tensor *tensors /* host */, int n_tensors, size_t *bytes);
 int ckksmi_muon_step(ckksmi_ctx *ctx, const ckksmi_muon *opt, const ckksmi_muon_tensor *tensors /* host */, int n_tensors, void *ws, size_t ws_bytes, void *stream);
 
+/* Matrices in 4 bits, for answers of a few rows: element (o, k) of d_out x d_in is scale[o][k / group] * code(o, k), a code from -8 to 7.  codes:
+ * [d_out][round_up(d_in, 32) / 2] bytes, two's complement, the even k of a pair in the lower half of its byte (what lies behind d_in may
+ * be anything), 16-byte aligned; scales: [d_out][ceil(d_in / group)] of dtype.  group: 32, 64, .. 1024; d_in, d_out, ld 1 .. 2^20.
+ * Products are formed from the codes' exact values and x (f32 x as three bf16 parts, 24 bits), summed in 32 bits over a group, and the
+ * groups' sums times their scales in 32 bits; the order depends on the sizes alone.  Any number of rows, but every 64 read the codes again. */
+typedef struct {
+    int dtype;          /* of x, y and the scales */
+    int group;
+    int64_t d_in, d_out;
+} ckksmi_matrix4;
+/* nearest codes for w (w_dtype, dense): scale = (largest magnitude of the group) / 7 rounded to dtype, code = w / scale rounded to even.  A group
+ * whose scale is not finite gets scale NaN, one whose scale is 0 codes 0.  And back: w = scale * code, rounded to w_dtype */
+int ckksmi_pack4(ckksmi_ctx *ctx, const ckksmi_matrix4 *m, int w_dtype, const void *w, void *codes, void *scales, void *stream);
+int ckksmi_unpack4(ckksmi_ctx *ctx, const ckksmi_matrix4 *m, int w_dtype, const void *codes, const void *scales, void *w, void *stream);
+/* y = x W^T; x: [rows][d_in], y: [rows][d_out], rows ld_* elements apart (0 = dense).  0 <= rows < 2^22.  y must not overlap an input. */
+int ckksmi_product4(ckksmi_ctx *ctx, const ckksmi_matrix4 *m, int64_t rows, const void *x, int64_t ld_x, const void *codes, const void *scales, void *y, int64_t ld_y,
+                    void *stream);
+/* The gated block from such matrices (all of one dtype and group): y = (act(x Wg^T) * (x Wu^T)) Wd^T.  h = act(g) u is held in two bf16 parts (16 bits;
+ * f32: three), so y is rounded once. */
+typedef struct {
+    int dtype, group, act;
+    float c[4];
+    int64_t rows, d_in, d_hidden, d_out, ld_x, ld_y;
+} ckksmi_gated_ff4;
+typedef struct { const void *codes, *scales; } ckksmi_weights4;
+int ckksmi_gated_ff4_workspace_bytes(const ckksmi_ctx *ctx, const ckksmi_gated_ff4 *ff, size_t *bytes); /* for up to ff->rows rows */
+int ckksmi_gated_ff4_forward(ckksmi_ctx *ctx, const ckksmi_gated_ff4 *ff, const void *x, const ckksmi_weights4 *gate, const ckksmi_weights4 *up, const ckksmi_weights4 *down,
+                             void *y, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

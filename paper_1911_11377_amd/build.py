@@ -5,7 +5,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libckksmi.so")
-SOURCES = ["ckksmi_device.hip", "train_device.hip", "norm_device.hip", "muon_device.hip", "host_math.cpp", "host_crypto.cpp"]
+SOURCES = ["ckksmi_device.hip", "train_device.hip", "norm_device.hip", "muon_device.hip", "low_device.hip", "host_math.cpp", "host_crypto.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -79,6 +79,19 @@ class MuonParams(C.Structure):  # ckksmi_muon
                 ("weight_decay", C.c_double), ("grad_scale", C.c_double), ("skip", VP), ("series", Series)]
 
 
+class Matrix4(C.Structure):  # ckksmi_matrix4
+    _fields_ = [("dtype", C.c_int), ("group", C.c_int), ("d_in", C.c_int64), ("d_out", C.c_int64)]
+
+
+class GatedFF4Shape(C.Structure):  # ckksmi_gated_ff4
+    _fields_ = [("dtype", C.c_int), ("group", C.c_int), ("act", C.c_int), ("c", C.c_float * 4), ("rows", C.c_int64), ("d_in", C.c_int64), ("d_hidden", C.c_int64),
+                ("d_out", C.c_int64), ("ld_x", C.c_int64), ("ld_y", C.c_int64)]
+
+
+class Weights4(C.Structure):  # ckksmi_weights4
+    _fields_ = [("codes", VP), ("scales", VP)]
+
+
 class CkksmiError(RuntimeError):
     def __init__(self, code, what, detail=""):
         self.code = code
@@ -146,14 +159,20 @@ SIGNATURES = {
     "ckksmi_orthogonalise": [VP, C.POINTER(Series), C.POINTER(DirectionTensor), C.c_int, C.c_int, VP, C.c_size_t, VP],
     "ckksmi_muon_workspace_bytes": [VP, C.POINTER(MuonParams), C.POINTER(MuonTensor), C.c_int, C.POINTER(C.c_size_t)],
     "ckksmi_muon_step": [VP, C.POINTER(MuonParams), C.POINTER(MuonTensor), C.c_int, VP, C.c_size_t, VP],
+    "ckksmi_pack4": [VP, C.POINTER(Matrix4), C.c_int] + [VP] * 4,
+    "ckksmi_unpack4": [VP, C.POINTER(Matrix4), C.c_int] + [VP] * 4,
+    "ckksmi_product4": [VP, C.POINTER(Matrix4), C.c_int64, VP, C.c_int64, VP, VP, VP, C.c_int64, VP],
+    "ckksmi_gated_ff4_workspace_bytes": [VP, C.POINTER(GatedFF4Shape), C.POINTER(C.c_size_t)],
+    "ckksmi_gated_ff4_forward": [VP, C.POINTER(GatedFF4Shape), VP] + [C.POINTER(Weights4)] * 3 + [VP, VP, C.c_size_t, VP],
     "ckksmi_profile_enable": [VP, C.c_int],
     "ckksmi_profile_read": [VP, C.c_int, f64p, C.POINTER(C.c_longlong), f64p],
     "ckksmi_kernel_class_name": [VP, C.c_int],
     "ckksmi_tune": [VP, C.c_int, C.c_int],
 }
 _RESTYPES = {"ckksmi_ctx_destroy": None, "ckksmi_strerror": C.c_char_p, "ckksmi_kernel_class_name": C.c_char_p}
-TRAINING = ("ckksmi_gated_ff_", "ckksmi_adamw_", "ckksmi_residual_norm_", "ckksmi_orthogonalise", "ckksmi_muon_")  # entry points of include/ckksmi_train.h
-K_COUNT = 49
+TRAINING = ("ckksmi_gated_ff_", "ckksmi_adamw_", "ckksmi_residual_norm_", "ckksmi_orthogonalise", "ckksmi_muon_", "ckksmi_pack4", "ckksmi_unpack4", "ckksmi_product4",
+            "ckksmi_gated_ff4_")  # entry points of include/ckksmi_train.h
+K_COUNT = 51
 
 _LIBS = {}
 

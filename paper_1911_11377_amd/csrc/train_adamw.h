@@ -63,28 +63,6 @@ template <bool WHOLE, class T> __device__ __forceinline__ void store4(T *p, int6
 }
 template <class T> __device__ __forceinline__ bool at4(const T *p) { return ((uintptr_t)p & (4 * sizeof(T) - 1)) == 0; }
 
-// largest word of a wave: rotations by 1, 2, 4, 8 within rows of 16 lanes, then the four rows' values
-#ifdef CKKSMI_EMULATE
-#define wave_max emu_wave_max
-#else
-__device__ __forceinline__ unsigned wave_max(unsigned v) {
-#define TA_ROTATED(n) \
-    { \
-        const unsigned w = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + n, 0xf, 0xf, true); \
-        v = v > w ? v : w; \
-    }
-    TA_ROTATED(1) TA_ROTATED(2) TA_ROTATED(4) TA_ROTATED(8)
-#undef TA_ROTATED
-    unsigned m = (unsigned)__builtin_amdgcn_readlane((int)v, 0);
-#pragma unroll
-    for (int l = 16; l < 64; l += 16) {
-        const unsigned w = (unsigned)__builtin_amdgcn_readlane((int)v, l);
-        m = m > w ? m : w;
-    }
-    return m;
-}
-#endif
-
 // 8-bit codes: FRACTION bits behind the leading one, 4 bits of exponent, values in units; see ckksmi_train.h.  The code is the upper
 // part of the word of a 32-bit number scaled by 2^-(126 + FRACTION): codes without an exponent are its subnormal numbers
 template <int FRACTION> __device__ __forceinline__ float code_value(unsigned c) {

@@ -33,13 +33,7 @@ struct NormArgs {
 // column sums, in the order in which they lie in NormArgs::part
 enum NormSum { SUM_POST_W = 1, SUM_POST_B = 2, SUM_PRE_W = 4, SUM_PRE_B = 8, SUM_GATE = 16, NORM_SUMS = 5 };
 
-// 8 elements from p on, of which `left` exist (the others are zeros)
-template <class T> __device__ __forceinline__ void get8(const T *p, int left, Oct<T> &o) {
-    if (left >= 8) __builtin_memcpy(&o, p, sizeof(o));
-    else
-#pragma unroll
-        for (int e = 0; e < 8; e++) o.v[e] = e < left ? p[e] : (T)0.0f;
-}
+// 8 elements to p, of which `left` exist
 template <class T> __device__ __forceinline__ void put8(T *p, int left, const float (&x)[8]) {
     Oct<T> o;
 #pragma unroll
@@ -49,10 +43,6 @@ template <class T> __device__ __forceinline__ void put8(T *p, int left, const fl
 #pragma unroll
         for (int e = 0; e < 8; e++)
             if (e < left) p[e] = o.v[e];
-}
-template <class T> __device__ __forceinline__ void floats(const Oct<T> &o, float (&x)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; e++) x[e] = (float)o.v[e];
 }
 // 8 values of a weight, a bias or a channel gate; `missing` where there is none
 template <class T> __device__ __forceinline__ void weights8(const char *w, int w_f32, int at, int left, float missing, float (&x)[8]) {

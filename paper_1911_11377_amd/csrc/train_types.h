@@ -54,6 +54,39 @@ template <class T> __device__ __forceinline__ void store_oct(T *p, const float (
     if constexpr (sizeof(T) == 4) d[1] = w[1];
 }
 
+// 8 elements from p on, of which `left` exist (the others are zeros)
+template <class T> __device__ __forceinline__ void get8(const T *p, int left, Oct<T> &o) {
+    if (left >= 8) __builtin_memcpy(&o, p, sizeof(o));
+    else
+#pragma unroll
+        for (int e = 0; e < 8; e++) o.v[e] = e < left ? p[e] : (T)0.0f;
+}
+template <class T> __device__ __forceinline__ void floats(const Oct<T> &o, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) x[e] = (float)o.v[e];
+}
+// largest word of a wave: rotations by 1, 2, 4, 8 within rows of 16 lanes, then the four rows' values
+#ifdef CKKSMI_EMULATE
+#define wave_max emu_wave_max
+#else
+__device__ __forceinline__ unsigned wave_max(unsigned v) {
+#define TA_ROTATED(n) \
+    { \
+        const unsigned w = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + n, 0xf, 0xf, true); \
+        v = v > w ? v : w; \
+    }
+    TA_ROTATED(1) TA_ROTATED(2) TA_ROTATED(4) TA_ROTATED(8)
+#undef TA_ROTATED
+    unsigned m = (unsigned)__builtin_amdgcn_readlane((int)v, 0);
+#pragma unroll
+    for (int l = 16; l < 64; l += 16) {
+        const unsigned w = (unsigned)__builtin_amdgcn_readlane((int)v, l);
+        m = m > w ? m : w;
+    }
+    return m;
+}
+#endif
+
 // 32-bit values kept in 24 bits: the upper 16 of their words in one plane, the next 8 (rounded to nearest even) in another
 __device__ __forceinline__ void store_oct24(uint16_t *hi, uint8_t *lo, const float (&x)[8]) {
     u32x4 h;

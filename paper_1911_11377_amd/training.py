@@ -32,6 +32,16 @@ def _dtype_code(dtype):
     return codes[dtype]
 
 
+def activation_code(activation):
+    """kind and coefficients of a name of CUBICS, "relu" | "silu" | "gelu", or four coefficients of a cubic"""
+    if isinstance(activation, str) and activation in _OTHERS:
+        return _OTHERS[activation], (C.c_float * 4)()
+    cubic = CUBICS[activation] if isinstance(activation, str) else tuple(activation)
+    if len(cubic) != 4:
+        raise ValueError("a cubic has four coefficients")
+    return ckksmi.ACT_POLY, (C.c_float * 4)(*cubic)
+
+
 def _rows_of(x, width, dtype, rows=None):
     """a [rows][width] tensor whose rows are contiguous: address and distance of its rows"""
     if x.dim() != 2 or x.shape[1] != width or (rows is not None and x.shape[0] != rows) or x.dtype != dtype:
@@ -54,13 +64,7 @@ class GatedFF:
         s = ckksmi.GatedFFShape()
         s.dtype, s.grad_dtype = _dtype_code(dtype), _dtype_code(self.grad_dtype)
         s.d_in, s.d_hidden, s.d_out = d_in, d_hidden, d_out
-        if isinstance(activation, str) and activation in _OTHERS:
-            s.act = _OTHERS[activation]
-        else:
-            cubic = CUBICS[activation] if isinstance(activation, str) else tuple(activation)
-            if len(cubic) != 4:
-                raise ValueError("a cubic has four coefficients")
-            s.act, s.c = ckksmi.ACT_POLY, (C.c_float * 4)(*cubic)
+        s.act, s.c = activation_code(activation)
         self._s, self._r = s, C.byref(s)  # what all calls have in common
         self._saved_of = (0, 0)  # rows of some call and what they save: replaced as a whole
 

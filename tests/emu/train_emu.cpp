@@ -225,6 +225,17 @@ float emu_lanes_sum(float x, int lanes) {
     return x;
 }
 
+float emu_code_to_float(unsigned c) { return (float)((int)(c << 28) >> 28) / 16.0f; }
+emu_u32x4 emu_exchange_words(emu_u32x4 w) {
+    put(w);
+    wave_sync();
+    const unsigned lane = g_cur % 64;
+    emu_u32x4 o;
+    for (unsigned s = 0; s < 4; s++) o[s] = get<emu_u32x4>(16 * s + lane % 16)[lane / 16];
+    wave_sync();
+    return o;
+}
+
 extern "C" void *emu_alloc(size_t bytes) { return emu::guarded_alloc(bytes); }
 extern "C" void emu_free(void *p) { emu::guarded_free(p); }
 extern "C" long emu_errors() { return g_errors; }
@@ -239,6 +250,7 @@ extern "C" void emu_copy_blocks(unsigned n) { g_copy_blocks = n; }
 #include "../../paper_1911_11377_amd/csrc/train_device.hip"
 #include "../../paper_1911_11377_amd/csrc/norm_device.hip"
 #include "../../paper_1911_11377_amd/csrc/muon_device.hip"
+#include "../../paper_1911_11377_amd/csrc/low_device.hip"
 
 // a context that the training operators accept: they use nothing of its ring
 extern "C" ckksmi_ctx *emu_train_context() {

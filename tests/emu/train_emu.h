@@ -29,3 +29,6 @@ emu_s16x4 emu_read_transposed(const char *p);
 unsigned emu_wave_max(unsigned v);
 // sum over the groups of `lanes` lanes, pairs first: every lane gets the same bits
 float emu_lanes_sum(float x, int lanes);
+// 4-bit codes in sixteenths; word s of a lane in row q of 16 lanes from word q of the lane in row s
+float emu_code_to_float(unsigned c);
+emu_u32x4 emu_exchange_words(emu_u32x4 w);

@@ -1,0 +1,115 @@
+"""Products with 4-bit matrices in 64 bits, with bounds of the kernels' rounding errors, written from the formulas."""
+import math
+
+import torch
+
+import training_reference as ref
+from paper_1911_11377_amd import lowbit, training
+
+U = 2.0**-24
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def weights(d_out, d_in, group, dtype, seed, place=lambda t: t, fill=None):
+    """codes of all 16 values (behind d_in: anything), scales over two decades and of both signs"""
+    g = torch.Generator().manual_seed(seed)
+    codes = torch.randint(0, 256, (d_out, -(-d_in // 32) * 16), generator=g, dtype=torch.uint8)
+    if fill is not None:
+        codes.fill_(fill)
+    s = torch.exp(torch.randn((d_out, -(-d_in // group)), generator=g)) * 0.3 * d_in**-0.5 * (1 - 2 * (torch.rand((d_out, -(-d_in // group)), generator=g) < 0.2).float())
+    return place(codes), place(s.to(dtype))
+
+
+def values(w, d_in, group):
+    codes, scales = (t.cpu() for t in w)
+    c = torch.stack((codes & 15, codes >> 4), 2).reshape(codes.shape[0], -1)[:, :d_in].to(torch.int64)
+    return torch.where(c > 7, c - 16, c).double(), scales.double().repeat_interleave(group, 1)[:, :d_in]
+
+
+def product(x, e_x, w, d_in, group, parts=1):
+    """x W^T and a bound: a group's codes times x are exact, their sums of `group` (times the parts of x) terms in 32 bits are not, nor are the
+    scaled sums of the groups over runs and waves"""
+    c, s = values(w, d_in, group)
+    m = c * s
+    magnitude = x.abs() @ m.abs().t()
+    n = parts * min(group, d_in) + -(-d_in // min(group, 128)) + 24
+    return x @ m.t(), e_x @ m.abs().t() + n * U * magnitude
+
+
+def block(x, gate, up, down, act, sizes, group, dtype):
+    d_in, d_hidden, d_out = sizes
+    x = x.double().cpu()
+    parts = 3 if dtype == F32 else 1
+    g, e_g = product(x, torch.zeros_like(x), gate, d_in, group, parts)
+    u, e_u = product(x, torch.zeros_like(x), up, d_in, group, parts)
+    a, d1, d2, size = ref.act_parts(g, act)
+    e_a = d1.abs() * e_g + 0.5 * e_g**2 * d2.abs() + 8 * U * size
+    h = a * u
+    held = 2.0**-24 if dtype == F32 else 2.0**-16  # three bf16 parts, or two
+    e_h = e_a * u.abs() + a.abs() * e_u + e_a * e_u + (held + U) * h.abs()
+    return product(h, e_h, down, d_hidden, group, 3 if dtype == F32 else 2)
+
+
+def within(got, want, dtype, what=""):
+    v, bound = want
+    bound = 1.25 * bound
+    bound = bound + ref.ROUND[dtype] * (v.abs() + bound) + ref.TINY[dtype]
+    off = (got.double().cpu() - v).abs()
+    assert bool((off <= bound).all()), (what, float((off - bound).max()), float((off / bound).max()))
+
+
+def check_product(ctx, rows, d_in, d_out, group, dtype, place, device="cpu", lead=0, seed=1):
+    g = torch.Generator().manual_seed(seed)
+
+    def rowed(t):
+        wide = torch.full((t.shape[0], t.shape[1] + lead), math.nan, dtype=t.dtype)
+        wide[:, :t.shape[1]] = t
+        return place(wide.to(device))[:, :t.shape[1]]
+
+    x = rowed(torch.randn((rows, d_in), generator=g).to(dtype))
+    y = rowed(torch.full((rows, d_out), math.nan, dtype=dtype))
+    w = weights(d_out, d_in, group, dtype, seed + 1, lambda t: place(t.to(device)))
+    plan = lowbit.Product4(ctx, d_in, d_out, dtype, group)
+    plan.forward(x, *w, y)
+    within(y, product(x.double().cpu(), torch.zeros(rows, d_in, dtype=torch.float64), w, d_in, group, 3 if dtype == F32 else 1), dtype)
+    return plan, x, w, y
+
+
+def check_block(ctx, rows, sizes, group, dtype, act, place, device="cpu", seed=1):
+    g = torch.Generator().manual_seed(seed)
+    d_in, d_hidden, d_out = sizes
+    x = place(torch.randn((rows, d_in), generator=g).to(dtype).to(device))
+    y = place(torch.full((rows, d_out), math.nan, dtype=dtype).to(device))
+    put = lambda t: place(t.to(device))  # noqa: E731
+    gate, up, down = weights(d_hidden, d_in, group, dtype, seed + 1, put), weights(d_hidden, d_in, group, dtype, seed + 2, put), weights(d_out, d_hidden, group, dtype, seed + 3, put)
+    plan = lowbit.GatedFF4(ctx, *sizes, dtype, act, group)
+    ws = place(torch.full((max(16, plan.workspace_bytes(rows)),), 255, dtype=torch.uint8).to(device))
+    plan.forward(x, gate, up, down, y, ws)
+    within(y, block(x, gate, up, down, training.CUBICS.get(act, act), sizes, group, dtype), dtype)
+    return plan, x, (gate, up, down), y, ws
+
+
+def nearest(w, group, dtype):
+    """codes and scales that pack gives, one 32-bit operation at a time"""
+    w = w.float().cpu()
+    rows, cols = w.shape
+    whole = torch.zeros(rows, -(-cols // group) * group)
+    whole[:, :cols] = w
+    parts = whole.view(rows, -1, group)
+    most = parts.abs().amax(2)
+    most = torch.where(torch.isnan(parts).any(2), torch.full_like(most, math.nan), most)
+    scale = (most / 7.0).to(dtype).float()
+    scale = torch.where(torch.isfinite(scale), scale, torch.full_like(scale, math.nan))
+    inverse = torch.where(scale > 0, 1.0 / scale, torch.zeros_like(scale))
+    c = torch.round(parts * inverse[..., None]).clamp(-8, 7)
+    c = torch.where((inverse > 0)[..., None], c, torch.zeros_like(c)).view(rows, -1)[:, :cols]
+    padded = torch.zeros(rows, -(-cols // 32) * 32)
+    padded[:, :cols] = c
+    n = padded.to(torch.int64) & 15
+    return (n[:, 0::2] | n[:, 1::2] << 4).to(torch.uint8), scale.to(dtype)
+
+
+# rows, d_in, d_out, group
+SIZES = [(1, 1, 1, 32), (1, 32, 16, 32), (3, 100, 17, 32), (2, 129, 33, 64), (1, 256, 8, 128), (5, 300, 40, 128), (17, 75, 20, 32), (33, 140, 9, 256), (2, 2100, 16, 512), (65, 40, 24, 64),
+         (4, 33, 31, 1024)]
+BLOCKS = [(1, (64, 32, 16), 32, "silu"), (3, (99, 70, 31), 64, "poly3"), (20, (40, 136, 9), 128, "gelu"), (7, (33, 1, 1), 32, "relu"), (40, (130, 48, 24), 256, "square")]
