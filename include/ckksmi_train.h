@@ -213,10 +213,9 @@ typedef struct {
     float c[4];
     int64_t rows, d_in, d_hidden, d_out, ld_x, ld_y;
 } ckksmi_gated_ff4;
-typedef struct { const void *codes, *scales; } ckksmi_weights4;
 int ckksmi_gated_ff4_workspace_bytes(const ckksmi_ctx *ctx, const ckksmi_gated_ff4 *ff, size_t *bytes); /* for up to ff->rows rows */
-int ckksmi_gated_ff4_forward(ckksmi_ctx *ctx, const ckksmi_gated_ff4 *ff, const void *x, const ckksmi_weights4 *gate, const ckksmi_weights4 *up, const ckksmi_weights4 *down,
-                             void *y, void *ws, size_t ws_bytes, void *stream);
+int ckksmi_gated_ff4_forward(ckksmi_ctx *ctx, const ckksmi_gated_ff4 *ff, const void *x, const void *gate_codes, const void *gate_scales, const void *up_codes,
+                             const void *up_scales, const void *down_codes, const void *down_scales, void *y, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -88,10 +88,6 @@ class GatedFF4Shape(C.Structure):  # ckksmi_gated_ff4
                 ("d_out", C.c_int64), ("ld_x", C.c_int64), ("ld_y", C.c_int64)]
 
 
-class Weights4(C.Structure):  # ckksmi_weights4
-    _fields_ = [("codes", VP), ("scales", VP)]
-
-
 class CkksmiError(RuntimeError):
     def __init__(self, code, what, detail=""):
         self.code = code
@@ -163,7 +159,7 @@ SIGNATURES = {
     "ckksmi_unpack4": [VP, C.POINTER(Matrix4), C.c_int] + [VP] * 4,
     "ckksmi_product4": [VP, C.POINTER(Matrix4), C.c_int64, VP, C.c_int64, VP, VP, VP, C.c_int64, VP],
     "ckksmi_gated_ff4_workspace_bytes": [VP, C.POINTER(GatedFF4Shape), C.POINTER(C.c_size_t)],
-    "ckksmi_gated_ff4_forward": [VP, C.POINTER(GatedFF4Shape), VP] + [C.POINTER(Weights4)] * 3 + [VP, VP, C.c_size_t, VP],
+    "ckksmi_gated_ff4_forward": [VP, C.POINTER(GatedFF4Shape)] + [VP] * 9 + [C.c_size_t, VP],
     "ckksmi_profile_enable": [VP, C.c_int],
     "ckksmi_profile_read": [VP, C.c_int, f64p, C.POINTER(C.c_longlong), f64p],
     "ckksmi_kernel_class_name": [VP, C.c_int],

@@ -10,6 +10,7 @@ int check_matrix4(const ckksmi_matrix4 &m) {
     if (!dtype_ok(m.dtype) || m.group < 32 || m.group > 1024 || (m.group & (m.group - 1))) return CKKSMI_EINVAL;
     return m.d_in < 1 || m.d_in > kMaxDim || m.d_out < 1 || m.d_out > kMaxDim ? CKKSMI_EINVAL : CKKSMI_OK;
 }
+struct Weights4 { const void *codes, *scales; };
 struct Sizes4 {  // a matrix's rows and bytes
     size_t ldc, lds, codes, scales, elements;
     explicit Sizes4(const ckksmi_matrix4 &m)
@@ -51,7 +52,7 @@ void rows4_of_h(ckksmi_ctx *c, int dtype, const Rows4Args &R, hipStream_t st) {
     }
 }
 
-Rows4Args rows4_args(const ckksmi_matrix4 &m, int64_t rows, const void *x, size_t ldx, const ckksmi_weights4 &w) {
+Rows4Args rows4_args(const ckksmi_matrix4 &m, int64_t rows, const void *x, size_t ldx, const Weights4 &w) {
     const Sizes4 s(m);
     Rows4Args R;
     memset(&R, 0, sizeof(R));
@@ -102,7 +103,7 @@ int pack4(ckksmi_ctx *c, const ckksmi_matrix4 *matrix, int w_dtype, const void *
     return guard.rc();
 }
 
-int check_weights4(const ckksmi_weights4 &w, size_t es) { return w.codes && w.scales && aligned(w.codes, 16) && aligned(w.scales, es) ? CKKSMI_OK : CKKSMI_EINVAL; }
+int check_weights4(const Weights4 &w, size_t es) { return w.codes && w.scales && aligned(w.codes, 16) && aligned(w.scales, es) ? CKKSMI_OK : CKKSMI_EINVAL; }
 
 int check_ff4(const ckksmi_gated_ff4 &f) {
     if (f.act < CKKSMI_ACT_POLY || f.act > CKKSMI_ACT_GELU || f.rows < 0 || f.rows > kMaxRows4) return CKKSMI_EINVAL;
@@ -132,7 +133,7 @@ extern "C" int ckksmi_product4(ckksmi_ctx *c, const ckksmi_matrix4 *matrix, int6
     if (rc) return rc;
     if (rows < 0 || rows > kMaxRows4 || (ld_x != 0 && (ld_x < m.d_in || ld_x > kMaxDim)) || (ld_y != 0 && (ld_y < m.d_out || ld_y > kMaxDim))) return CKKSMI_EINVAL;
     const size_t es = element_bytes(m.dtype);
-    const ckksmi_weights4 w{codes, scales};
+    const Weights4 w{codes, scales};
     if (check_weights4(w, es)) return CKKSMI_EINVAL;
     if (rows == 0) return CKKSMI_OK;
     if (!x || !y || !aligned(x, es) || !aligned(y, es)) return CKKSMI_EINVAL;
@@ -155,16 +156,16 @@ extern "C" int ckksmi_gated_ff4_workspace_bytes(const ckksmi_ctx *c, const ckksm
     return rc;
 }
 
-extern "C" int ckksmi_gated_ff4_forward(ckksmi_ctx *c, const ckksmi_gated_ff4 *ff, const void *x, const ckksmi_weights4 *gate, const ckksmi_weights4 *up, const ckksmi_weights4 *down,
-                                        void *y, void *ws, size_t ws_bytes, void *stream) {
+extern "C" int ckksmi_gated_ff4_forward(ckksmi_ctx *c, const ckksmi_gated_ff4 *ff, const void *x, const void *gate_codes, const void *gate_scales, const void *up_codes,
+                                        const void *up_scales, const void *down_codes, const void *down_scales, void *y, void *ws, size_t ws_bytes, void *stream) {
     if (!dev_ok(c)) return CKKSMI_EDEVICE;
-    if (!ff || !gate || !up || !down) return CKKSMI_EINVAL;
+    if (!ff) return CKKSMI_EINVAL;
     const ckksmi_gated_ff4 f = *ff;
     const int rc = check_ff4(f);
     if (rc) return rc;
-    const ckksmi_weights4 w[3] = {*gate, *up, *down};
+    const Weights4 w[3] = {{gate_codes, gate_scales}, {up_codes, up_scales}, {down_codes, down_scales}};
     const size_t es = element_bytes(f.dtype);
-    for (const ckksmi_weights4 &v : w)
+    for (const Weights4 &v : w)
         if (check_weights4(v, es)) return CKKSMI_EINVAL;
     if (f.rows == 0) return CKKSMI_OK;
     if (!x || !y || !ws || !aligned(x, es) || !aligned(y, es) || !aligned(ws, 16)) return CKKSMI_EINVAL;

@@ -11,27 +11,28 @@ told otherwise and allocate nothing.  Meant for up to 64 rows; each further 64 r
 import ctypes as C
 
 from . import ckksmi
-from .training import _dtype_code, _rows_of, activation_code
+from .training import _dtype_code, _rows_or_dense, activation_code
 
 
 class Product4:
     """Plan of products with a d_out x d_in matrix in 4 bits; any number of rows.  group: 32, 64, .. 1024; dtype: of x, y and the scales"""
 
     def __init__(self, ctx, d_in, d_out, dtype, group=128):
-        self.ctx, self.d_in, self.d_out, self.dtype, self.group = ctx, d_in, d_out, dtype, group
+        import torch
+
+        self.ctx, self.d_in, self.d_out, self.dtype, self.group, self._uint8 = ctx, d_in, d_out, dtype, group, torch.uint8
         self.codes_shape = (d_out, -(-d_in // 32) * 16)
         self.scales_shape = (d_out, -(-d_in // group) if group > 0 else 0)
         m = ckksmi.Matrix4()
         m.dtype, m.group, m.d_in, m.d_out = _dtype_code(dtype), group, d_in, d_out
-        self._m = m
+        self._m, self._r = m, C.byref(m)
 
     def _weights(self, codes, scales):
-        import torch
-
-        if tuple(codes.shape) != self.codes_shape or codes.dtype != torch.uint8 or tuple(scales.shape) != self.scales_shape or scales.dtype != self.dtype:
-            raise ValueError("expected codes %s and scales %s of %s, got %s of %s and %s of %s" % (
+        if (codes.shape != self.codes_shape or codes.dtype != self._uint8 or scales.shape != self.scales_shape or scales.dtype != self.dtype or not codes.is_contiguous()
+                or not scales.is_contiguous()):
+            raise ValueError("expected contiguous codes %s and scales %s of %s, got %s of %s and %s of %s" % (
                 self.codes_shape, self.scales_shape, self.dtype, tuple(codes.shape), codes.dtype, tuple(scales.shape), scales.dtype))
-        return ckksmi._ptr(codes), ckksmi._ptr(scales)
+        return codes.data_ptr(), scales.data_ptr()
 
     def _matrix(self, w):
         if tuple(w.shape) != (self.d_out, self.d_in):
@@ -41,18 +42,19 @@ class Product4:
     def pack(self, w, codes, scales, stream=None):
         """nearest codes and scales of w (float32, bfloat16 or float16): scale = largest magnitude of a group / 7"""
         code, p = self._matrix(w)
-        self.ctx._call("ckksmi_pack4", self.ctx._h, C.byref(self._m), code, p, *self._weights(codes, scales), self.ctx._stream(stream))
+        self.ctx._call("ckksmi_pack4", self.ctx._h, self._r, code, p, *self._weights(codes, scales), self.ctx._stream(stream))
 
     def unpack(self, codes, scales, w, stream=None):
         """w = scale * code, rounded to w's type"""
         code, p = self._matrix(w)
-        self.ctx._call("ckksmi_unpack4", self.ctx._h, C.byref(self._m), code, *self._weights(codes, scales), p, self.ctx._stream(stream))
+        self.ctx._call("ckksmi_unpack4", self.ctx._h, self._r, code, *self._weights(codes, scales), p, self.ctx._stream(stream))
 
     def forward(self, x, codes, scales, y, stream=None):
         """y = x W^T"""
-        px, ld_x = _rows_of(x, self.d_in, self.dtype)
-        py, ld_y = _rows_of(y, self.d_out, self.dtype, x.shape[0])
-        self.ctx._call("ckksmi_product4", self.ctx._h, C.byref(self._m), x.shape[0], px, ld_x, *self._weights(codes, scales), py, ld_y, self.ctx._stream(stream))
+        rows, ctx = x.shape[0], self.ctx
+        px, ld_x = _rows_or_dense(x, rows, self.d_in, self.dtype)
+        py, ld_y = _rows_or_dense(y, rows, self.d_out, self.dtype)
+        ctx._call("ckksmi_product4", ctx._h, self._r, rows, px, ld_x, *self._weights(codes, scales), py, ld_y, ctx._stream(stream))
 
 
 class GatedFF4:
@@ -69,7 +71,9 @@ class GatedFF4:
 
     def _shape(self, rows, ld_x=0, ld_y=0):
         s = ckksmi.GatedFF4Shape.from_buffer_copy(self._s)
-        s.rows, s.ld_x, s.ld_y = rows, ld_x, ld_y
+        s.rows = rows
+        if ld_x or ld_y:
+            s.ld_x, s.ld_y = ld_x, ld_y
         return C.byref(s)
 
     def workspace_bytes(self, rows):
@@ -80,7 +84,8 @@ class GatedFF4:
 
     def forward(self, x, gate, up, down, y, ws, stream=None):
         """gate, up, down: pairs (codes, scales)"""
-        px, ld_x = _rows_of(x, self.into.d_in, self.into.dtype)
-        py, ld_y = _rows_of(y, self.out.d_out, self.out.dtype, x.shape[0])
-        w = [C.byref(ckksmi.Weights4(*plan._weights(*pair))) for plan, pair in ((self.into, gate), (self.into, up), (self.out, down))]
-        self.ctx._call("ckksmi_gated_ff4_forward", self.ctx._h, self._shape(x.shape[0], ld_x, ld_y), px, *w, py, ckksmi._ptr(ws), ckksmi._nbytes(ws), self.ctx._stream(stream))
+        rows, ctx, into, out = x.shape[0], self.ctx, self.into, self.out
+        px, ld_x = _rows_or_dense(x, rows, into.d_in, into.dtype)
+        py, ld_y = _rows_or_dense(y, rows, out.d_out, out.dtype)
+        ctx._call("ckksmi_gated_ff4_forward", ctx._h, self._shape(rows, ld_x, ld_y), px, *into._weights(*gate), *into._weights(*up), *out._weights(*down), py, ckksmi._ptr(ws),
+                  ckksmi._nbytes(ws), ctx._stream(stream))

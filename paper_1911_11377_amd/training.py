@@ -53,6 +53,13 @@ def _rows_of(x, width, dtype, rows=None):
     return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else width
 
 
+def _rows_or_dense(x, rows, width, dtype):
+    """the same; 0 for the distance of dense rows"""
+    if x.is_contiguous() and x.shape == (rows, width) and x.dtype == dtype:
+        return x.data_ptr(), 0
+    return _rows_of(x, width, dtype, rows)
+
+
 class GatedFF:
     """Plan of a gated feed-forward block of fixed widths and types; any number of rows.
 
@@ -141,7 +148,7 @@ class ResidualNorm:
         s = ckksmi.ResidualNormShape()
         s.dtype, s.weight_dtype, s.pre, s.post, s.gate = _dtype_code(dtype), _dtype_code(self.weight_dtype), kinds[pre], kinds[post], gates[gate]
         s.eps, s.residual_scale, s.block_scale, s.d = eps, residual_scale, block_scale, d
-        self._s = s  # what all calls have in common
+        self._s, self._vector_shape = s, (d,)  # what all calls have in common
 
     def _shape(self, rows):
         s = ckksmi.ResidualNormShape.from_buffer_copy(self._s)
@@ -161,48 +168,53 @@ class ResidualNorm:
         return self._bytes("ckksmi_residual_norm_saved_bytes", rows)
 
     def _vector(self, w):
-        if w is not None and (tuple(w.shape) != (self.d,) or w.dtype != self.weight_dtype):
-            raise ValueError("expected [%d] of %s, got %s of %s" % (self.d, self.weight_dtype, tuple(w.shape), w.dtype))
-        return ckksmi._ptr(w)
+        if w is None:
+            return None
+        if w.shape != self._vector_shape or w.dtype != self.weight_dtype or not w.is_contiguous():
+            raise ValueError("expected contiguous [%d] of %s, got %s of %s" % (self.d, self.weight_dtype, tuple(w.shape), w.dtype))
+        return w.data_ptr()
 
-    def _rows(self, s, **tensors):
-        """addresses of tensors of rows (None stays None); their distances into the call's structure"""
-        out = []
-        for name, x in tensors.items():
-            p, ld = _rows_of(x, self.d, self.dtype, s.rows) if x is not None else (None, 0)
-            setattr(s, "ld_" + name, ld)
-            out.append(p)
-        return out
+    def _rows(self, s, rows, name, x):
+        """address of a tensor of rows (None stays None); the distance of its rows, if they are not dense, into the call's structure"""
+        if x is None:
+            return None
+        p, ld = _rows_or_dense(x, rows, self.d, self.dtype)
+        if ld:
+            setattr(s, name, ld)
+        return p
 
-    def _gate(self, s, name, g):
-        return self._rows(s, **{name: g})[0] if self.gate == "element" else self._vector(g)
+    def _gate(self, s, rows, name, g):
+        return self._rows(s, rows, name, g) if self.gate == "element" else self._vector(g)
 
     def _saved(self, saved, rows):
-        if saved is not None and ckksmi._nbytes(saved) < 16 * rows:
+        if saved is None:
+            return None
+        if ckksmi._nbytes(saved) < 16 * rows:
             raise ValueError("the buffer for saved statistics holds %d bytes of %d" % (ckksmi._nbytes(saved), 16 * rows))
         return ckksmi._ptr(saved)
 
     def forward(self, x, f, r, n, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, saved=None, stream=None):
         """f None: n = N_pre(x), r None.  r may be x; None: not wanted.  n is None where pre is.  saved: a buffer of saved_bytes(rows) for the
         backward pass, or None"""
-        s = self._shape(x.shape[0])
-        px, pf, pr, pn = self._rows(s, x=x, f=f, r=r, n=n)
-        w = [self._vector(v) for v in (post_weight, post_bias, pre_weight, pre_bias)]
-        self.ctx._call("ckksmi_residual_norm_forward", self.ctx._h, C.byref(s), px, pf, self._gate(s, "gate", gate), *w, pr, pn, self._saved(saved, s.rows), self.ctx._stream(stream))
+        ctx, rows, vector = self.ctx, x.shape[0], self._vector
+        s = self._shape(rows)
+        ctx._call("ckksmi_residual_norm_forward", ctx._h, C.byref(s), self._rows(s, rows, "ld_x", x), self._rows(s, rows, "ld_f", f), self._gate(s, rows, "ld_gate", gate),
+                  vector(post_weight), vector(post_bias), vector(pre_weight), vector(pre_bias), self._rows(s, rows, "ld_r", r), self._rows(s, rows, "ld_n", n),
+                  self._saved(saved, rows), ctx._stream(stream))
 
     def backward(self, x, f, saved, dr, dn, ws, dx=None, df=None, dgate=None, dpost_weight=None, dpost_bias=None, dpre_weight=None, dpre_bias=None, gate=None,
                  post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, accumulate=False, stream=None):
         """dr, dn: gradients of r and n (None: zeros).  Gradients that are None are not formed; accumulate: those of weights, biases and a channel
         gate are added to what their buffers hold.  ws: workspace_bytes(rows), None where none of them is wanted.  (pre_bias plays no part)"""
-        s = self._shape(x.shape[0])
-        px, pf, pdr, pdn, pdx, pdf = self._rows(s, x=x, f=f, dr=dr, dn=dn, dx=dx, df=df)
-        w = [self._vector(v) for v in (post_weight, post_bias, pre_weight)]
-        self._vector(pre_bias)
-        dw = [self._vector(v) for v in (dpost_weight, dpost_bias, dpre_weight, dpre_bias)]
         if saved is None:
             raise ValueError("the backward pass reads what a forward pass saved")
-        self.ctx._call("ckksmi_residual_norm_backward", self.ctx._h, C.byref(s), px, pf, self._gate(s, "gate", gate), *w, self._saved(saved, s.rows), pdr, pdn, pdx, pdf,
-                       self._gate(s, "dgate", dgate), *dw, 1 if accumulate else 0, ckksmi._ptr(ws), ckksmi._nbytes(ws) if ws is not None else 0, self.ctx._stream(stream))
+        ctx, rows, vector = self.ctx, x.shape[0], self._vector
+        s = self._shape(rows)
+        vector(pre_bias)
+        ctx._call("ckksmi_residual_norm_backward", ctx._h, C.byref(s), self._rows(s, rows, "ld_x", x), self._rows(s, rows, "ld_f", f), self._gate(s, rows, "ld_gate", gate),
+                  vector(post_weight), vector(post_bias), vector(pre_weight), self._saved(saved, rows), self._rows(s, rows, "ld_dr", dr), self._rows(s, rows, "ld_dn", dn),
+                  self._rows(s, rows, "ld_dx", dx), self._rows(s, rows, "ld_df", df), self._gate(s, rows, "ld_dgate", dgate), vector(dpost_weight), vector(dpost_bias),
+                  vector(dpre_weight), vector(dpre_bias), 1 if accumulate else 0, ckksmi._ptr(ws), ckksmi._nbytes(ws) if ws is not None else 0, ctx._stream(stream))
 
 
 def _refuse_overlaps(written, read):
