@@ -16,9 +16,9 @@ int check_norm(const ckksmi_residual_norm &c) {
     return CKKSMI_OK;
 }
 
-// Threads a row and 8-element pieces a thread.  Rows that no row of this table holds take the kernels for long rows
-struct NormRule { int most, lanes, v; };
-constexpr NormRule kNorm[] = {{64, 8, 1}, {128, 16, 1}, {256, 32, 1}, {512, 64, 1}, {1024, 64, 2}, {2048, 128, 2}, {4096, 256, 2}, {8192, 512, 2}, {16384, 1024, 2}};
+// Threads a row (8 elements each; 16 for the longest that a forward pass holds).  Rows that no row of this table holds take the kernels for long rows
+struct NormRule { int most, lanes; };
+constexpr NormRule kNorm[] = {{64, 8}, {128, 16}, {256, 32}, {512, 64}, {1024, 128}, {2048, 256}, {4096, 512}, {8192, 1024}, {16384, 1024}};
 constexpr int kForwardRules = 9, kBackwardRules = 8;
 inline int rule_of(int64_t d, int rules) {
     int i = 0;
@@ -28,24 +28,25 @@ inline int rule_of(int64_t d, int rules) {
 inline int threads_of(int lanes) { return lanes > 64 ? lanes : 256; }
 inline int groups_of(int lanes) { return threads_of(lanes) / lanes; }
 
-// Workgroups of a backward pass, each going through its rows
-int64_t backward_blocks(int64_t rows, int64_t d) {
-    const int i = rule_of(d, kBackwardRules);
-    if (i == kBackwardRules) return std::min<int64_t>(rows, 1024);
-    const int lanes = kNorm[i].lanes;
-    return std::min<int64_t>((rows + groups_of(lanes) - 1) / groups_of(lanes), 512 * 256 / threads_of(lanes));
+// Workgroups of a backward pass, each going through its rows: as many as the compute units hold at once, so that all have the same number of rows
+// (16384 rows of 2048, rms, both passes: 768 172 us, 1024 209, 512 201; layer norms with a gate's columns 512 222, 768 260, an element's gate
+// 768 211, 512 231)
+int64_t backward_blocks(const ckksmi_residual_norm &c) {
+    const int i = rule_of(c.d, kBackwardRules);
+    if (i == kBackwardRules) return std::min<int64_t>(c.rows, 1024);
+    const int lanes = kNorm[i].lanes, threads = threads_of(lanes), groups = groups_of(lanes);
+    const bool few = (c.pre == CKKSMI_NORM_LAYER || c.post == CKKSMI_NORM_LAYER) && c.gate != CKKSMI_GATE_ELEMENT;
+    const int most = lanes >= 512 ? 262144 / lanes : (few ? 512 : 768) * 256 / threads;
+    return std::min<int64_t>((c.rows + groups - 1) / groups, most);
 }
 // waves that share the rows of a column pass, in workgroups of four
 int64_t column_blocks(int64_t rows) { return std::min<int64_t>((rows + 15) / 16, 64); }
-// groups whose column sums go to memory
-int64_t column_groups(int64_t rows, int64_t d) {
-    const int i = rule_of(d, kBackwardRules);
-    return i == kBackwardRules ? 4 * column_blocks(rows) : backward_blocks(rows, d) * groups_of(kNorm[i].lanes);
-}
+// column sums of this many go to memory
+int64_t column_groups(const ckksmi_residual_norm &c) { return rule_of(c.d, kBackwardRules) == kBackwardRules ? 4 * column_blocks(c.rows) : backward_blocks(c); }
 inline size_t part_ld(int64_t d) { return round_up((size_t)d, 8); }
 // (never less for more rows)
 size_t norm_workspace(const ckksmi_residual_norm &c) {
-    const size_t part = round_up((size_t)column_groups(c.rows, c.d) * NORM_SUMS * part_ld(c.d) * sizeof(float), 256);
+    const size_t part = round_up((size_t)column_groups(c) * NORM_SUMS * part_ld(c.d) * sizeof(float), 256);
     return part + (rule_of(c.d, kBackwardRules) == kBackwardRules ? (size_t)c.rows * 16 : 0);
 }
 
@@ -96,58 +97,73 @@ NormArgs norm_args(const ckksmi_residual_norm &c, const void *x, const void *f, 
     A.ld_part = part_ld(c.d);
     A.M = (int)c.rows; A.d = (int)c.d; A.pre = c.pre; A.post = f ? c.post : CKKSMI_NORM_NONE; A.gate_kind = f ? c.gate : CKKSMI_GATE_NONE;
     A.w_f32 = c.weight_dtype == CKKSMI_F32;
-    A.eps = c.eps; A.a = c.residual_scale; A.b = c.block_scale; A.inv_d = (float)(1.0 / (double)c.d);
+    A.eps = c.eps; A.a = f ? c.residual_scale : 1.0f; A.b = f ? c.block_scale : 0.0f; A.inv_d = (float)(1.0 / (double)c.d);
     return A;
 }
 
-template <class T> void forward(ckksmi_ctx *c, const NormArgs &A, hipStream_t st) {
-    const int i = rule_of(A.d, kForwardRules);
+template <class T, bool LAYER> void norm_forward(ckksmi_ctx *c, const NormArgs &A, int rule, dim3 grid, dim3 block, hipStream_t st) {
     const double units = (double)A.M * A.d;
+    switch (rule) {
+        case 0: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 8, 1, LAYER>), grid, block, st, A); break;
+        case 1: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 16, 1, LAYER>), grid, block, st, A); break;
+        case 2: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 32, 1, LAYER>), grid, block, st, A); break;
+        case 3: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 64, 1, LAYER>), grid, block, st, A); break;
+        case 4: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 128, 1, LAYER>), grid, block, st, A); break;
+        case 5: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 256, 1, LAYER>), grid, block, st, A); break;
+        case 6: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 512, 1, LAYER>), grid, block, st, A); break;
+        case 7: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 1024, 1, LAYER>), grid, block, st, A); break;
+        default: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 1024, 2, LAYER>), grid, block, st, A); break;
+    }
+}
+inline bool has_layer(const NormArgs &A) { return A.pre == CKKSMI_NORM_LAYER || A.post == CKKSMI_NORM_LAYER; }
+template <class T> void norm_forward(ckksmi_ctx *c, const NormArgs &A, hipStream_t st) {
+    const int i = rule_of(A.d, kForwardRules);
     if (i == kForwardRules) {
-        KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_long_kernel<T>), dim3(std::min(A.M, 1024)), dim3(NORM_LONG), st, A);
+        KL(c, CKKSMI_K_NORM_FORWARD, (double)A.M * A.d, (norm_forward_long_kernel<T>), dim3(std::min(A.M, 1024)), dim3(NORM_LONG), st, A);
         return;
     }
     const int threads = threads_of(kNorm[i].lanes), groups = groups_of(kNorm[i].lanes);
-    const dim3 grid((unsigned)std::min<int64_t>(((int64_t)A.M + groups - 1) / groups, 2048 * 256 / threads)), block(threads);
-    switch (i) {
-        case 0: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 8, 1>), grid, block, st, A); break;
-        case 1: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 16, 1>), grid, block, st, A); break;
-        case 2: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 32, 1>), grid, block, st, A); break;
-        case 3: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 64, 1>), grid, block, st, A); break;
-        case 4: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 64, 2>), grid, block, st, A); break;
-        case 5: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 128, 2>), grid, block, st, A); break;
-        case 6: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 256, 2>), grid, block, st, A); break;
-        case 7: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 512, 2>), grid, block, st, A); break;
-        default: KL(c, CKKSMI_K_NORM_FORWARD, units, (norm_forward_kernel<T, 1024, 2>), grid, block, st, A); break;
+    // as for the backward pass: five workgroups of 256 a compute unit, of layer norms four, twice
+    const int most = (has_layer(A) || threads > 256 ? 2048 : 1280) * 256 / threads;
+    const dim3 grid((unsigned)std::min<int64_t>(((int64_t)A.M + groups - 1) / groups, most)), block(threads);
+    if (has_layer(A)) norm_forward<T, true>(c, A, i, grid, block, st);
+    else norm_forward<T, false>(c, A, i, grid, block, st);
+}
+
+template <class T> void norm_join(ckksmi_ctx *c, const NormJoinArgs &J, int outs, hipStream_t st) {
+    if (outs) KL(c, CKKSMI_K_NORM_JOIN, (double)outs * J.d, (norm_join_kernel<T>), dim3((J.d + 63) / 64, outs), dim3(1024), st, J);
+}
+
+template <class T, bool LAYER, bool ELEMENT> void norm_backward(ckksmi_ctx *c, const NormArgs &A, int rule, dim3 grid, dim3 block, hipStream_t st) {
+    const double units = (double)A.M * A.d;
+    switch (rule) {
+        case 0: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 8, LAYER, ELEMENT>), grid, block, st, A); break;
+        case 1: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 16, LAYER, ELEMENT>), grid, block, st, A); break;
+        case 2: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 32, LAYER, ELEMENT>), grid, block, st, A); break;
+        case 3: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 64, LAYER, ELEMENT>), grid, block, st, A); break;
+        case 4: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 128, LAYER, ELEMENT>), grid, block, st, A); break;
+        case 5: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 256, LAYER, ELEMENT>), grid, block, st, A); break;
+        case 6: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 512, LAYER, ELEMENT>), grid, block, st, A); break;
+        default: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 1024, LAYER, ELEMENT>), grid, block, st, A); break;
     }
 }
-
-template <class T> void join(ckksmi_ctx *c, const NormJoinArgs &J, hipStream_t st) {
-    if (J.vectors) KL(c, CKKSMI_K_NORM_JOIN, (double)J.vectors * J.d, (norm_join_kernel<T>), dim3((J.d + 63) / 64, J.vectors), dim3(1024), st, J);
-}
-
-template <class T> void backward(ckksmi_ctx *c, NormArgs A, NormJoinArgs J, char *coef, hipStream_t st) {
+template <class T, bool ELEMENT> void norm_backward(ckksmi_ctx *c, NormArgs A, unsigned blocks, char *coef, hipStream_t st) {
     const int i = rule_of(A.d, kBackwardRules);
     const double units = (double)A.M * A.d;
-    const unsigned blocks = (unsigned)backward_blocks(A.M, A.d);
     if (i == kBackwardRules) {
         if (A.sums) A.coef = (float *)coef;
-        KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_long_kernel<T>), dim3(blocks), dim3(NORM_LONG), st, A);
-        if (A.sums) KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_columns_kernel<T>), dim3((A.d + 511) / 512, (unsigned)column_blocks(A.M)), dim3(256), st, A);
+        KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_long_kernel<T, ELEMENT>), dim3(blocks), dim3(NORM_LONG), st, A);
+        if (A.sums) KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_columns_kernel<T, ELEMENT>), dim3((A.d + 511) / 512, (unsigned)column_blocks(A.M)), dim3(256), st, A);
     } else {
         const dim3 grid(blocks), block(threads_of(kNorm[i].lanes));
-        switch (i) {
-            case 0: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 8, 1>), grid, block, st, A); break;
-            case 1: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 16, 1>), grid, block, st, A); break;
-            case 2: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 32, 1>), grid, block, st, A); break;
-            case 3: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 64, 1>), grid, block, st, A); break;
-            case 4: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 64, 2>), grid, block, st, A); break;
-            case 5: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 128, 2>), grid, block, st, A); break;
-            case 6: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 256, 2>), grid, block, st, A); break;
-            default: KL(c, CKKSMI_K_NORM_BACKWARD, units, (norm_backward_kernel<T, 512, 2>), grid, block, st, A); break;
-        }
+        if (has_layer(A)) norm_backward<T, true, ELEMENT>(c, A, i, grid, block, st);
+        else norm_backward<T, false, ELEMENT>(c, A, i, grid, block, st);
     }
-    join<T>(c, J, st);
+}
+template <class T> void norm_backward(ckksmi_ctx *c, const NormArgs &A, const NormJoinArgs &J, int outs, unsigned blocks, char *coef, hipStream_t st) {
+    if (A.gate_kind == CKKSMI_GATE_ELEMENT) norm_backward<T, true>(c, A, blocks, coef, st);
+    else norm_backward<T, false>(c, A, blocks, coef, st);
+    norm_join<T>(c, J, outs, st);
 }
 
 }  // namespace
@@ -193,9 +209,9 @@ extern "C" int ckksmi_residual_norm_forward(ckksmi_ctx *c, const ckksmi_residual
     A.r = (char *)r; A.n = (char *)n; A.stats = (float *)saved;
     Guard guard(c);
     switch (s.dtype) {
-        case CKKSMI_F32: forward<float>(c, A, S(stream)); break;
-        case CKKSMI_BF16: forward<__bf16>(c, A, S(stream)); break;
-        default: forward<_Float16>(c, A, S(stream)); break;
+        case CKKSMI_F32: norm_forward<float>(c, A, S(stream)); break;
+        case CKKSMI_BF16: norm_forward<__bf16>(c, A, S(stream)); break;
+        default: norm_forward<_Float16>(c, A, S(stream)); break;
     }
     return guard.rc();
 }
@@ -225,23 +241,29 @@ extern "C" int ckksmi_residual_norm_backward(ckksmi_ctx *c, const ckksmi_residua
     if ((s.gate == CKKSMI_GATE_NONE && dgate) || (s.post == CKKSMI_NORM_NONE && dpost_w) || (s.post != CKKSMI_NORM_LAYER && dpost_b) ||
         (s.pre == CKKSMI_NORM_NONE && (dn || dpre_w)) || (s.pre != CKKSMI_NORM_LAYER && dpre_b))
         return CKKSMI_EINVAL;
-    const bool column_gate = s.gate == CKKSMI_GATE_CHANNEL && dgate;
+    // which column sums, and what comes of them
+    const bool column_gate = s.gate == CKKSMI_GATE_CHANNEL && dgate, gated = s.gate == CKKSMI_GATE_CHANNEL, biased = s.post == CKKSMI_NORM_LAYER;
+    const int sums = (dpost_w || column_gate ? SUM_P : 0) | (dpost_b || (column_gate && biased) ? SUM_Q : 0) | (dpre_w ? SUM_R : 0) | (dpre_b ? SUM_T : 0);
     NormJoinArgs J;
     memset(&J, 0, sizeof(J));
-    J.d = (int)s.d; J.f32_out = s.weight_dtype == CKKSMI_F32; J.accumulate = accumulate != 0; J.ld_part = part_ld(s.d);
-    int sums = 0;
-    void *const wanted[NORM_SUMS] = {dpost_w, dpost_b, dpre_w, dpre_b, column_gate ? dgate : nullptr};
-    for (int k = 0; k < NORM_SUMS; k++)
-        if (wanted[k]) {
-            J.out[J.vectors++] = (char *)wanted[k];
-            sums |= 1 << k;
-        }
+    J.d = (int)s.d; J.w_f32 = s.weight_dtype == CKKSMI_F32; J.accumulate = accumulate != 0; J.ld_part = part_ld(s.d);
+    int place[NORM_SUMS], outs = 0;
+    for (int k = 0; k < NORM_SUMS; k++) place[k] = sums >> k & 1 ? J.vectors++ : -1;
+    auto add = [&](void *o, int first, const void *by, int second, const void *second_by) {
+        if (o) J.out[outs++] = NormJoinArgs::Out{(char *)o, first, second, (const char *)by, (const char *)second_by};
+    };
+    add(dpost_w, place[0], gated ? gate : nullptr, -1, nullptr);
+    add(dpost_b, place[1], gated ? gate : nullptr, -1, nullptr);
+    add(dpre_w, place[2], nullptr, -1, nullptr);
+    add(dpre_b, place[3], nullptr, -1, nullptr);
+    if (column_gate) add(dgate, place[0], post_w, biased && post_b ? place[1] : -1, post_b);
     const size_t need = norm_workspace(s);
     Guard guard(c);
     if (none) {
         if (J.accumulate) return CKKSMI_OK;
-        const Span out[NORM_SUMS] = {at.vector(dpost_w), at.vector(dpost_b), at.vector(dpre_w), at.vector(dpre_b), at.vector(wanted[4])};
-        if (!apart(out, NORM_SUMS, nullptr, 0)) return CKKSMI_EINVAL;
+        for (NormJoinArgs::Out &o : J.out) o.by = o.second_by = nullptr;
+        const Span out[NORM_SUMS + 1] = {at.vector(dpost_w), at.vector(dpost_b), at.vector(dpre_w), at.vector(dpre_b), at.vector(column_gate ? dgate : nullptr)};
+        if (!apart(out, NORM_SUMS + 1, nullptr, 0)) return CKKSMI_EINVAL;
     } else {
         const Span in[9] = {at.rows(x, s.ld_x), at.rows(f, s.ld_f), at.gate(gate, s.ld_gate), at.vector(post_w), at.vector(post_b), at.vector(pre_w),
                             at.rows(dr, s.ld_dr), at.rows(dn, s.ld_dn), Span{saved, (size_t)s.rows * 16}};
@@ -258,13 +280,14 @@ extern "C" int ckksmi_residual_norm_backward(ckksmi_ctx *c, const ckksmi_residua
     A.dgate = column_gate ? nullptr : (char *)dgate;
     A.sums = sums; A.vectors = J.vectors; A.part = (float *)ws;
     J.part = (const float *)ws;
-    J.groups = none ? 0 : (int)column_groups(s.rows, s.d);
-    char *const coef = (char *)ws + round_up((size_t)column_groups(s.rows, s.d) * NORM_SUMS * part_ld(s.d) * sizeof(float), 256);
+    J.groups = none ? 0 : (int)column_groups(s);
+    char *const coef = (char *)ws + round_up((size_t)column_groups(s) * NORM_SUMS * part_ld(s.d) * sizeof(float), 256);
+    const unsigned blocks = (unsigned)backward_blocks(s);
     const hipStream_t st = S(stream);
     switch (s.dtype) {
-        case CKKSMI_F32: none ? join<float>(c, J, st) : backward<float>(c, A, J, coef, st); break;
-        case CKKSMI_BF16: none ? join<__bf16>(c, J, st) : backward<__bf16>(c, A, J, coef, st); break;
-        default: none ? join<_Float16>(c, J, st) : backward<_Float16>(c, A, J, coef, st); break;
+        case CKKSMI_F32: none ? norm_join<float>(c, J, outs, st) : norm_backward<float>(c, A, J, outs, blocks, coef, st); break;
+        case CKKSMI_BF16: none ? norm_join<__bf16>(c, J, outs, st) : norm_backward<__bf16>(c, A, J, outs, blocks, coef, st); break;
+        default: none ? norm_join<_Float16>(c, J, outs, st) : norm_backward<_Float16>(c, A, J, outs, blocks, coef, st); break;
     }
     return guard.rc();
 }
