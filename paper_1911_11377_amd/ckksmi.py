@@ -204,6 +204,20 @@ def _ptr(x):
     raise TypeError("expected a device buffer, got %r" % type(x))
 
 
+def _current_stream():
+    """torch's current stream on its current device, as an address"""
+    global _current_stream
+    import torch
+
+    if hasattr(torch._C, "_cuda_getCurrentRawStream"):  # 0.2 us; a Stream object takes 2.6
+        torch.cuda.current_stream()  # (initialises CUDA if nothing has yet)
+        raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        _current_stream = lambda: raw(device())  # noqa: E731
+    else:
+        _current_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    return _current_stream()
+
+
 def _nbytes(x):
     if hasattr(x, "numel"):
         return x.numel() * x.element_size()
@@ -270,11 +284,7 @@ class Context:
 
     @staticmethod
     def _stream(stream):
-        if stream is not None:
-            return stream
-        import torch
-
-        return torch.cuda.current_stream().cuda_stream
+        return stream if stream is not None else _current_stream()
 
     # ------------------------------------------------------------ host side
     def sample_ternary(self, seed):
