@@ -23,15 +23,26 @@ inline int shift_of(int group) {
     return s;
 }
 
-template <class T, class O, bool XF32, int PARTS, bool GATE> void launch_rows4(ckksmi_ctx *c, const Rows4Args &R, hipStream_t st) {
+template <class T, class O, bool XF32, int PARTS, bool GATE, int EACH> void launch_rows4(ckksmi_ctx *c, const Rows4Args &R, hipStream_t st) {
     const int blocks = (R.N + 15) / 16, tiles = (R.M + 15) / 16;
     const double flops = 2.0 * R.M * R.N * R.K * (GATE ? 2 : 1);
     const int mt = tiles <= 1 ? 1 : tiles <= 2 ? 2 : 4;
     const dim3 grid(blocks, (tiles + mt - 1) / mt);
     switch (mt) {
-        case 1: KL(c, CKKSMI_K_ROWS4, flops, (rows4_kernel<T, O, XF32, PARTS, GATE, 1, 16>), grid, dim3(1024), st, R); break;
-        case 2: KL(c, CKKSMI_K_ROWS4, flops, (rows4_kernel<T, O, XF32, PARTS, GATE, 2, 8>), grid, dim3(512), st, R); break;
-        default: KL(c, CKKSMI_K_ROWS4, flops, (rows4_kernel<T, O, XF32, PARTS, GATE, 4, 8>), grid, dim3(512), st, R); break;
+        case 1:
+            // (one row, 8192 -> 16384: 22.7 us with four waves, 24.0 with eight, 28.8 with sixteen; 4096 -> 4096 7.0, 6.6, 7.0; 16 f32 rows 12.8, 10.6, 10.7)
+            if (blocks <= 512) KL(c, CKKSMI_K_ROWS4, flops, (rows4_kernel<T, O, XF32, PARTS, GATE, 1, 8, EACH>), grid, dim3(512), st, R);
+            else KL(c, CKKSMI_K_ROWS4, flops, (rows4_kernel<T, O, XF32, PARTS, GATE, 1, 4, EACH>), grid, dim3(256), st, R);
+            break;
+        case 2: KL(c, CKKSMI_K_ROWS4, flops, (rows4_kernel<T, O, XF32, PARTS, GATE, 2, 8, EACH>), grid, dim3(512), st, R); break;
+        default: KL(c, CKKSMI_K_ROWS4, flops, (rows4_kernel<T, O, XF32, PARTS, GATE, 4, 8, EACH>), grid, dim3(512), st, R); break;
+    }
+}
+template <class T, class O, bool XF32, int PARTS, bool GATE> void launch_rows4(ckksmi_ctx *c, const Rows4Args &R, hipStream_t st) {
+    switch (R.group_shift) {
+        case 0: launch_rows4<T, O, XF32, PARTS, GATE, 1>(c, R, st); break;
+        case 1: launch_rows4<T, O, XF32, PARTS, GATE, 2>(c, R, st); break;
+        default: launch_rows4<T, O, XF32, PARTS, GATE, 4>(c, R, st); break;
     }
 }
 

@@ -236,6 +236,8 @@ emu_u32x4 emu_exchange_words(emu_u32x4 w) {
     return o;
 }
 
+void emu_wave_fence() { wave_sync(); }
+
 extern "C" void *emu_alloc(size_t bytes) { return emu::guarded_alloc(bytes); }
 extern "C" void emu_free(void *p) { emu::guarded_free(p); }
 extern "C" long emu_errors() { return g_errors; }

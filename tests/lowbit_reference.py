@@ -111,5 +111,5 @@ def nearest(w, group, dtype):
 
 # rows, d_in, d_out, group
 SIZES = [(1, 1, 1, 32), (1, 32, 16, 32), (3, 100, 17, 32), (2, 129, 33, 64), (1, 256, 8, 128), (5, 300, 40, 128), (17, 75, 20, 32), (33, 140, 9, 256), (2, 2100, 16, 512), (65, 40, 24, 64),
-         (4, 33, 31, 1024)]
+         (4, 33, 31, 1024), (2, 300, 8209, 32)]
 BLOCKS = [(1, (64, 32, 16), 32, "silu"), (3, (99, 70, 31), 64, "poly3"), (20, (40, 136, 9), 128, "gelu"), (7, (33, 1, 1), 32, "relu"), (40, (130, 48, 24), 256, "square")]
