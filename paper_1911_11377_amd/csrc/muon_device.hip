@@ -9,6 +9,10 @@ constexpr int64_t kMaxSide = 1 << 16;
 #define TG_ENOUGH_TILES 192  // three quarters of the compute units (the tests' stand-in sets it)
 #endif
 
+#ifndef TS_SMALL_MOST
+#define TS_SMALL_MOST TS_SMALL_LDS  // bytes of LDS up to which a call's matrices take one workgroup each (the tests' stand-in sets it)
+#endif
+
 // The polynomials keep singular values and entries where f16 holds them: the largest value that can stand at each step's end, on a grid
 // fine enough for a polynomial of degree five
 int check_series(const ckksmi_series &s) {
@@ -39,7 +43,7 @@ struct SeriesTensor {
 // A tensor's sizes and its pieces of the workspace
 struct SeriesPlan {
     int side, length, ld, ld_o, parts, blocks;
-    size_t numel;
+    size_t numel, per;
     float S;
     explicit SeriesPlan(const SeriesTensor &t, int parts_) : parts(parts_) {
         side = (int)std::min(t.rows, t.cols);
@@ -47,10 +51,14 @@ struct SeriesPlan {
         ld = (int)round_up(length, 8);
         ld_o = (int)round_up(side, 8);
         numel = (size_t)t.rows * t.cols;
-        blocks = (int)((numel + TS_CHUNK - 1) / TS_CHUNK);
+        // the first pass: at most 1024 workgroups' sums, which every workgroup of the second adds up
+        per = round_up((numel + 1023) / 1024, 4096);
+        blocks = (int)((numel + per - 1) / per);
         // a power of two near sqrt(numel), at most 2^14: S times a singular value below 2 stays in f16
         S = (float)std::ldexp(1.0, std::min(14, (int)std::lround(0.5 * std::log2((double)numel))));
     }
+    // everything in one workgroup's LDS
+    bool small() const { return side <= 64 && small_lds(side, length, parts) <= TS_SMALL_MOST; }
     size_t x_bytes() const { return (size_t)side * ld * 4; }  // two parts of f16, or a direction in f32
     size_t o_bytes() const { return (size_t)side * ld_o * 2 * parts; }
     // X and its successor, O, B, two diagonals, sums of squares
@@ -181,13 +189,15 @@ struct SeriesCall {
     std::vector<SeriesTensor> t;
     std::vector<SeriesPlan> plan;
     size_t need;
+    bool small = true;  // all of them are
     SeriesCall(std::vector<SeriesTensor> tensors, int parts, const ckksmi_series &s) {
         for (const SeriesTensor &x : tensors)
             if (x.rows && x.cols) {
                 t.push_back(x);
                 plan.emplace_back(x, parts);
+                small = small && plan.back().small();
             }
-        need = series_workspace(plan, s);
+        need = small ? 0 : series_workspace(plan, s);
     }
 };
 
@@ -203,8 +213,10 @@ template <class Blocks, class Launch> void for_tables(const SeriesCall &call, co
             const SeriesPlan &l = call.plan[i];
             PassTensor &t = A.t[A.n];
             t.p = (char *)s.p; t.g = (const char *)s.g; t.m = s.m; t.copy = (char *)s.copy;
-            t.sums = w[i].sums; t.x = (_Float16 *)w[i].x[0]; t.o = (_Float16 *)w[i].o; t.b = (_Float16 *)w[i].b; t.direction = (const float *)w[i].x[direction];
-            t.numel = (int64_t)l.numel; t.rows = (int)s.rows; t.cols = (int)s.cols; t.ld = l.ld; t.ld_o = l.ld_o; t.parts = l.parts;
+            if (!call.small) {
+                t.sums = w[i].sums; t.x = (_Float16 *)w[i].x[0]; t.o = (_Float16 *)w[i].o; t.b = (_Float16 *)w[i].b; t.direction = (const float *)w[i].x[direction];
+            }
+            t.numel = (int64_t)l.numel; t.per = (int64_t)l.per; t.rows = (int)s.rows; t.cols = (int)s.cols; t.ld = l.ld; t.ld_o = l.ld_o; t.parts = l.parts;
             t.S = l.S; t.scale = (float)s.scale; t.blocks = l.blocks;
             A.first[A.n++] = (unsigned)blocks;
             blocks += more;
@@ -216,7 +228,22 @@ template <class Blocks, class Launch> void for_tables(const SeriesCall &call, co
 }
 inline int64_t series_squares(const SeriesPlan &l) { return (int64_t)((l.side + 63) / 64) * ((l.ld + 63) / 64); }
 
+template <class P, class G, bool MOVE> void run_small(ckksmi_ctx *c, const SeriesCall &call, const ckksmi_series &s, const PassArgs &A, hipStream_t st) {
+    const SmallSeries S{s.steps, (float)s.a, (float)s.b, (float)s.c};
+    for_tables(call, {}, A, 0, [](const SeriesPlan &) { return (int64_t)1; }, [&](const PassArgs &a, unsigned blocks) {
+        if (call.plan[0].parts > 1) KL(c, CKKSMI_K_SERIES, blocks, (series_small_kernel<P, G, MOVE, 2>), dim3(blocks), dim3(TS_SMALL_THREADS), st, a, S);
+        else KL(c, CKKSMI_K_SERIES, blocks, (series_small_kernel<P, G, MOVE, 1>), dim3(blocks), dim3(TS_SMALL_THREADS), st, a, S);
+    });
+}
 template <class P, bool MOVE> void run_series(ckksmi_ctx *c, const SeriesCall &call, const ckksmi_series &s, const PassArgs &A, void *ws, hipStream_t st) {
+    if (call.small) {
+        switch (A.g_dtype) {
+            case CKKSMI_F32: run_small<P, float, MOVE>(c, call, s, A, st); break;
+            case CKKSMI_BF16: run_small<P, __bf16, MOVE>(c, call, s, A, st); break;
+            default: run_small<P, _Float16, MOVE>(c, call, s, A, st); break;
+        }
+        return;
+    }
     Carve carve(ws);
     std::vector<SeriesPieces> w;
     for (const SeriesPlan &l : call.plan) {
@@ -332,7 +359,7 @@ extern "C" int ckksmi_orthogonalise(ckksmi_ctx *c, const ckksmi_series *s, const
         if (call.t.empty()) return CKKSMI_OK;
         for (const SeriesTensor &x : call.t)
             if (!x.p || !x.g || !aligned(x.p, element_bytes(dtype)) || !aligned(x.g, element_bytes(dtype))) return CKKSMI_EINVAL;
-        if (!ws || !aligned(ws, 16)) return CKKSMI_EINVAL;
+        if (call.need && (!ws || !aligned(ws, 16))) return CKKSMI_EINVAL;
         for (size_t i = 0; i < call.t.size(); i++) {
             const size_t bytes = call.plan[i].numel * element_bytes(dtype);
             if (overlap(ws, call.need, call.t[i].p, bytes) || overlap(ws, call.need, call.t[i].g, bytes)) return CKKSMI_EINVAL;
@@ -376,7 +403,7 @@ extern "C" int ckksmi_muon_step(ckksmi_ctx *c, const ckksmi_muon *opt, const ckk
         const size_t ps = element_bytes(o.p_dtype), gs = element_bytes(o.grad_dtype);
         for (const SeriesTensor &x : call.t)
             if (!x.p || !x.g || !x.m || !aligned(x.p, ps) || !aligned(x.g, gs) || !aligned(x.m, 4) || !aligned(x.copy, 2)) return CKKSMI_EINVAL;
-        if (!ws || !aligned(ws, 16)) return CKKSMI_EINVAL;
+        if (call.need && (!ws || !aligned(ws, 16))) return CKKSMI_EINVAL;
         for (size_t i = 0; i < call.t.size(); i++) {
             const SeriesTensor &x = call.t[i];
             const size_t e = call.plan[i].numel;

@@ -38,31 +38,6 @@ __host__ __device__ __forceinline__ unsigned adamw_mix(unsigned h) {
     return h ^ (h >> 16);
 }
 
-// 4 elements from index i of n on; beyond the end zeros.  WHOLE: all are there, and aligned to their size
-template <bool WHOLE, class T> __device__ __forceinline__ void load4(const T *p, int64_t i, int64_t n, bool vec, T (&x)[4]) {
-    if (WHOLE || (vec && i + 4 <= n)) {
-        struct alignas(4 * sizeof(T)) V { T v[4]; } o = *(const V *)(p + i);
-#pragma unroll
-        for (int e = 0; e < 4; e++) x[e] = o.v[e];
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; e++) x[e] = i + e < n ? p[i + e] : (T)0;
-}
-template <bool WHOLE, class T> __device__ __forceinline__ void store4(T *p, int64_t i, int64_t n, bool vec, const T (&x)[4]) {
-    if (WHOLE || (vec && i + 4 <= n)) {
-        struct alignas(4 * sizeof(T)) V { T v[4]; } o;
-#pragma unroll
-        for (int e = 0; e < 4; e++) o.v[e] = x[e];
-        *(V *)(p + i) = o;
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; e++)
-        if (i + e < n) p[i + e] = x[e];
-}
-template <class T> __device__ __forceinline__ bool at4(const T *p) { return ((uintptr_t)p & (4 * sizeof(T) - 1)) == 0; }
-
 // 8-bit codes: FRACTION bits behind the leading one, 4 bits of exponent, values in units; see ckksmi_train.h.  The code is the upper
 // part of the word of a 32-bit number scaled by 2^-(126 + FRACTION): codes without an exponent are its subnormal numbers
 template <int FRACTION> __device__ __forceinline__ float code_value(unsigned c) {

@@ -136,12 +136,19 @@ template <int EPI> __global__ void __launch_bounds__(256) series_join_kernel(Ser
     const size_t m = id / octs;
     const int n = (int)(id % octs) * 8;
     if (symmetric(EPI) && n > (int)m) return;
-    float v[8];
-    for (int s = 0; s < G.splits; s++) {
-        float x[8];
-        load_oct(P.part + ((size_t)s * P.M + m) * P.ld_part + n, x);
+    const float *part = P.part + m * P.ld_part + n;
+    const size_t next = P.M * P.ld_part;
+    float v[8] = {};
+    // (four parts under way together: with one after the other 15 parts of 256 x 256 took 8.7 us)
+    for (int s = 0; s < G.splits; s += 4) {
+        float x[4][8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = s ? v[e] + x[e] : x[e];
+        for (int k = 0; k < 4; k++) load_oct(part + min(s + k, G.splits - 1) * next, x[k]);
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (s + k < G.splits) v[e] = s + k ? v[e] + x[k][e] : x[k][e];
     }
     SeriesEpilogue<EPI>::eight(P, m, n, v);
 }
@@ -156,7 +163,7 @@ struct PassTensor {
     _Float16 *x;           // two parts of [side][ld]
     _Float16 *o, *b;       // [parts][side][ld_o]: their padding is set to zeros
     const float *direction;  // [side][ld]
-    int64_t numel;
+    int64_t numel, per;    // per: elements of a workgroup of the first pass
     int rows, cols, ld, ld_o, parts;
     float S, scale;        // scale: lr times the tensor's
     int blocks;            // workgroups of the first pass
@@ -185,114 +192,411 @@ template <class G> __device__ __forceinline__ float momentum_of(const PassArgs &
 // u from the momentum after its update
 template <class G> __device__ __forceinline__ float direction_of(const PassArgs &A, float m, G g) { return A.nesterov ? m * A.momentum + (float)g * A.grad_scale * A.rest : m; }
 
-// Momentum, and the sum of squares of what is to be orthogonalised: in 64 bits (a gradient of 1e-25 has squares that f32 does not hold)
-#define TS_CHUNK 16384
-template <class G> __global__ void __launch_bounds__(256) series_momentum_kernel(PassArgs A) {
-    if (A.skip && *A.skip) return;
-    const PassTensor &t = A.t[pass_tensor(A)];
-    const unsigned block = blockIdx.x - A.first[pass_tensor(A)];
-    const int64_t begin = (int64_t)block * TS_CHUNK, end = begin + TS_CHUNK < t.numel ? begin + TS_CHUNK : t.numel;
-    const G *g = (const G *)t.g;
-    double sum = 0.0;
-    for (int64_t i = begin + threadIdx.x; i < end; i += 256) {
-        float u = (float)g[i];
-        if (t.m) {
-            const float m = momentum_of(A, t.m[i], g[i]);
-            t.m[i] = m;
-            u = direction_of(A, m, g[i]);
-        }
-        sum += (double)u * u;
+// u in units of its size: inverse as a power of two and the rest, so that neither leaves the range of f32 where inverse does
+struct Unit {
+    int exponent;
+    float rest;
+    __device__ __forceinline__ explicit Unit(double inverse) {
+        exponent = 0;
+        rest = (float)frexp(inverse, &exponent);
+        if (!(inverse <= 1.7e308)) rest = (float)inverse;
     }
-    __shared__ double sums[256];
-    sums[threadIdx.x] = sum;
+    __device__ __forceinline__ float of(float u) const { return ldexpf(u, exponent) * rest; }
+};
+__device__ __forceinline__ double series_inverse(const PassArgs &A, const PassTensor &t, double squares) {
+    const double size = sqrt(squares) + A.eps;
+    return size < 1e-300 ? 0.0 : (double)t.S / size;  // (f32 numbers that are not all zeros are larger)
+}
+// 64-bit sum over the workgroup
+template <int THREADS> __device__ __forceinline__ double block_sum(double x, double (&sums)[THREADS]) {
+    sums[threadIdx.x] = x;
     __syncthreads();
-    for (int by = 128; by; by /= 2) {
+    for (int by = THREADS / 2; by; by /= 2) {
         if ((int)threadIdx.x < by) sums[threadIdx.x] += sums[threadIdx.x + by];
         __syncthreads();
     }
-    if (threadIdx.x == 0) t.sums[block] = sums[0];
+    return sums[0];
 }
 
-// X in its two parts from the momentum; 64 x 64 elements a workgroup
+// Momentum, and the sum of squares of what is to be orthogonalised: in 64 bits (a gradient of 1e-25 has squares that f32 does not hold).
+// A workgroup takes `per` neighbouring elements, 4096 at a time
+template <class G> __global__ void __launch_bounds__(256) series_momentum_kernel(PassArgs A) {
+    if (A.skip && *A.skip) return;
+    const int i = pass_tensor(A);
+    const PassTensor &t = A.t[i];
+    const int64_t block = blockIdx.x - A.first[i], begin = block * t.per, end = begin + t.per < t.numel ? begin + t.per : t.numel;
+    const G *g = (const G *)t.g;
+    const bool g4 = at4(g), m4 = at4(t.m);
+    double sum = 0.0;
+    for (int64_t at = begin + 4 * threadIdx.x; at < end; at += 4096) {
+        G gs[4][4];
+        float ms[4][4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) load4<false>(g, at + 1024 * k, end, g4, gs[k]);
+        if (t.m)
+#pragma unroll
+            for (int k = 0; k < 4; k++) load4<false>(t.m, at + 1024 * k, end, m4, ms[k]);
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                float u = (float)gs[k][e];
+                if (t.m) {
+                    ms[k][e] = momentum_of(A, ms[k][e], gs[k][e]);
+                    u = direction_of(A, ms[k][e], gs[k][e]);
+                }
+                sum += (double)u * u;
+            }
+            if (t.m) store4<false>(t.m, at + 1024 * k, end, m4, ms[k]);
+        }
+    }
+    __shared__ double sums[256];
+    sum = block_sum<256>(sum, sums);
+    if (threadIdx.x == 0) t.sums[block] = sum;
+}
+
+// 4 elements of a row from column c on, of which `left` exist (the others are zeros)
+template <class T> __device__ __forceinline__ void get4(const T *p, int left, float (&x)[4]) {
+    T v[4];
+    if (left >= 4) __builtin_memcpy(v, p, sizeof(v));
+    else
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = e < left ? p[e] : (T)0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; e++) x[e] = (float)v[e];
+}
+template <class T> __device__ __forceinline__ void put4(T *p, int left, const float (&x)[4]) {
+    T v[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] = (T)x[e];
+    if (left >= 4) __builtin_memcpy(p, v, sizeof(v));
+    else
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (e < left) p[e] = v[e];
+}
+
+// A workgroup's 64 x 64 elements of a tensor, along its memory: rows r0 .. of memory, columns c0 ..
+struct Square {
+    int r0, c0;          // of memory
+    bool tall;           // held transposed
+    int side, length;    // as held
+    __device__ __forceinline__ Square(const PassTensor &t, int block) {
+        tall = t.rows > t.cols;
+        side = tall ? t.cols : t.rows;
+        length = tall ? t.rows : t.cols;
+        const int across = (t.ld + 63) / 64, s0 = block / across * 64, l0 = block % across * 64;
+        r0 = tall ? l0 : s0;
+        c0 = tall ? s0 : l0;
+    }
+};
+
+// X in its two parts from the momentum
 template <class G> __global__ void __launch_bounds__(256) series_begin_kernel(PassArgs A) {
     const int i = pass_tensor(A);
     const PassTensor &t = A.t[i];
+    const Square q(t, (int)(blockIdx.x - A.first[i]));
     __shared__ double sums[256];
     __shared__ float tile[64][65];
+    // four rows of a column of 4 a thread; requested before the sums are added up
+    const int r = threadIdx.x / 16, c = threadIdx.x % 16 * 4;
+    float g[4][4], m[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int row = q.r0 + r + 16 * k;
+        const size_t at = (size_t)row * t.cols + q.c0 + c;
+        get4((const G *)t.g + at, row < t.rows ? t.cols - q.c0 - c : 0, g[k]);
+        if (t.m) get4(t.m + at, row < t.rows ? t.cols - q.c0 - c : 0, m[k]);
+    }
     double sum = 0.0;
     for (int b = threadIdx.x; b < t.blocks; b += 256) sum += t.sums[b];
-    sums[threadIdx.x] = sum;
-    __syncthreads();
-    for (int by = 128; by; by /= 2) {
-        if ((int)threadIdx.x < by) sums[threadIdx.x] += sums[threadIdx.x + by];
-        __syncthreads();
-    }
-    const double size = sqrt(sums[0]) + A.eps, inverse = size == 0.0 ? 0.0 : (double)t.S / size;
-    // tiles of the held orientation: side x length
-    const bool tall = t.rows > t.cols;
-    const int side = tall ? t.cols : t.rows, length = tall ? t.rows : t.cols, across = (t.ld + 63) / 64;
-    const int block = (int)(blockIdx.x - A.first[i]), r0 = block / across * 64, c0 = block % across * 64;
-    const G *g = (const G *)t.g;
-    // what is read lies along memory: rows of the held tile, or (tall) its columns
-    for (int k = threadIdx.x; k < 4096; k += 256) {
-        const int along = k & 63, over = k >> 6, r = tall ? r0 + along : r0 + over, c = tall ? c0 + over : c0 + along;
-        float u = 0.0f;
-        if (r < side && c < length) {
-            const size_t at = tall ? (size_t)c * t.cols + r : (size_t)r * t.cols + c;
-            u = t.m ? direction_of(A, t.m[at], g[at]) : (float)g[at];
-            u = (float)((double)u * inverse);
+    const Unit unit(series_inverse(A, t, block_sum<256>(sum, sums)));
+#pragma unroll
+    for (int k = 0; k < 4; k++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const float u = unit.of(t.m ? direction_of(A, m[k][e], g[k][e]) : g[k][e]);
+            // (what lies beyond the matrix is 0 whatever the unit)
+            const bool in = q.r0 + r + 16 * k < t.rows && q.c0 + c + e < t.cols;
+            tile[q.tall ? c + e : r + 16 * k][q.tall ? r + 16 * k : c + e] = in ? u : 0.0f;
         }
-        tile[tall ? along : over][tall ? over : along] = u;
-    }
     __syncthreads();
-    const size_t apart = (size_t)side * t.ld;
-    for (int k = threadIdx.x; k < 512; k += 256) {
-        const int r = k / 8, c = k % 8 * 8;
-        if (r0 + r >= side || c0 + c >= t.ld) continue;
+    const int s0 = q.tall ? q.c0 : q.r0, l0 = q.tall ? q.r0 : q.c0;
+    const size_t apart = (size_t)q.side * t.ld;
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        const int row = threadIdx.x / 8 + 32 * k, at = threadIdx.x % 8 * 8;
+        if (s0 + row >= q.side || l0 + at >= t.ld) continue;
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = tile[r][c + e];
-        store_two(t.x + (size_t)(r0 + r) * t.ld + c0 + c, apart, v);
+        for (int e = 0; e < 8; e++) v[e] = tile[row][at + e];
+        store_two(t.x + (size_t)(s0 + row) * t.ld + l0 + at, apart, v);
     }
     // the tensor's first tiles of a row clear what pads the symmetric matrices' rows
-    if (c0 == 0 && t.ld_o > side)
+    if (l0 == 0 && t.ld_o > q.side)
         for (int k = threadIdx.x; k < 64 * t.parts; k += 256) {
-            const int r = r0 + k % 64;
-            if (r >= side) continue;
-            for (int c = side; c < t.ld_o; c++) {
-                const size_t at = ((size_t)(k / 64) * side + r) * t.ld_o + c;
+            const int row = s0 + k % 64;
+            if (row >= q.side) continue;
+            for (int col = q.side; col < t.ld_o; col++) {
+                const size_t at = ((size_t)(k / 64) * q.side + row) * t.ld_o + col;
                 t.o[at] = t.b[at] = (_Float16)0.0f;
             }
         }
 }
 
-// Parameters along the direction, or the direction itself (MOVE false); 64 x 64 elements a workgroup
+// 4 parameters along their directions, or the directions themselves (MOVE false)
+template <class P, bool MOVE> __device__ __forceinline__ void series_move(const PassArgs &A, const PassTensor &t, size_t at, int left, const float (&d)[4]) {
+    float p[4];
+    if (MOVE) {
+        get4((const P *)t.p + at, left, p);
+#pragma unroll
+        for (int e = 0; e < 4; e++) p[e] = p[e] * A.decay - d[e] * t.scale;
+    }
+    put4((P *)t.p + at, left, MOVE ? p : d);
+    if (MOVE && t.copy) {
+        if (A.copy_f16) put4((_Float16 *)t.copy + at, left, p);
+        else put4((__bf16 *)t.copy + at, left, p);
+    }
+}
 template <class P, bool MOVE> __global__ void __launch_bounds__(256) series_end_kernel(PassArgs A) {
     if (A.skip && *A.skip) return;
     const int i = pass_tensor(A);
     const PassTensor &t = A.t[i];
+    const Square q(t, (int)(blockIdx.x - A.first[i]));
     __shared__ float tile[64][65];
+    const int r = threadIdx.x / 16, c = threadIdx.x % 16 * 4, s0 = q.tall ? q.c0 : q.r0, l0 = q.tall ? q.r0 : q.c0;
+    float d[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int row = s0 + r + 16 * k;
+        get4(t.direction + (size_t)row * t.ld + l0 + c, row < q.side ? q.length - l0 - c : 0, d[k]);
+    }
+    if (q.tall) {
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) tile[c + e][r + 16 * k] = d[k][e];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) d[k][e] = tile[r + 16 * k][c + e];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int row = q.r0 + r + 16 * k;
+        if (row < t.rows && q.c0 + c < t.cols) series_move<P, MOVE>(A, t, (size_t)row * t.cols + q.c0 + c, t.cols - q.c0 - c, d[k]);
+    }
+}
+
+// ---- matrices that fit the LDS of a compute unit: everything in one workgroup and one launch
+// The same steps on 16 x 16 results a wave.  Rows and k indices (to a multiple of 32) that there are not are zeros in LDS and stay zeros; a row's
+// elements begin 16 bytes further round the banks than the row's before.  The new X takes the old one's place: a wave takes 16 columns,
+// and reads all of them before it writes.
+// Bound by latency: three barriers a step, with a few LDS reads and products between them
+#define TS_SMALL_LDS 151552
+#define TS_SMALL_THREADS 1024
+struct SmallSeries { int steps; float ca, cb, cc; };
+__host__ __device__ __forceinline__ int small_ld(int n) { return (n + 31) / 32 * 32 + 8; }
+inline size_t small_lds(int side, int length, int parts) {
+    const size_t M = (side + 15) / 16 * 16, rows = (side + 31) / 32 * 32;
+    return 4 * (rows * small_ld(length) + parts * M * small_ld((int)M));
+}
+template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bounds__(TS_SMALL_THREADS) series_small_kernel(PassArgs A, SmallSeries S) {
+    if (A.skip && *A.skip) return;
+    const PassTensor &t = A.t[blockIdx.x];
+    __shared__ __attribute__((aligned(1024))) char lds[TS_SMALL_LDS];
+    __shared__ double sums[TS_SMALL_THREADS];
+    __shared__ float d[64], e[64];
+    TG_LDS(lds);
     const bool tall = t.rows > t.cols;
-    const int side = tall ? t.cols : t.rows, length = tall ? t.rows : t.cols, across = (t.ld + 63) / 64;
-    const int block = (int)(blockIdx.x - A.first[i]), r0 = block / across * 64, c0 = block % across * 64;
-    if (tall) {
-        for (int k = threadIdx.x; k < 4096; k += 256) {
-            const int c = k & 63, r = k >> 6;
-            tile[r][c] = r0 + r < side && c0 + c < length ? t.direction[(size_t)(r0 + r) * t.ld + c0 + c] : 0.0f;
+    const int side = tall ? t.cols : t.rows, length = tall ? t.rows : t.cols, tiles = (side + 15) / 16, M = 16 * tiles, ld = small_ld(length), ld_o = small_ld(M);
+    const int x_apart = (M + 31) / 32 * 32 * ld, o_apart = M * ld_o;
+    _Float16 *const X = (_Float16 *)lds, *const O = X + 2 * x_apart, *const B = O + PARTS * o_apart;  // parts one behind the other
+    const int lane = threadIdx.x & 63, wave = TG_UNIFORM((int)(threadIdx.x >> 6)), i = lane & 15, q = lane >> 4;
+    constexpr int WAVES = TS_SMALL_THREADS / 64;
+    for (int k = threadIdx.x; k < 2 * (x_apart + PARTS * o_apart) / 8; k += TS_SMALL_THREADS) ((u32x4 *)lds)[k] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+    // u, held as its word's halves where X's parts will be; momentum and size.  Eight elements of a thread are requested together
+    const G *g = (const G *)t.g;
+    const int numel = (int)t.numel;
+    auto place = [&](int k) {
+        const int r = k / t.cols, c = k - r * t.cols;
+        return tall ? c * ld + r : r * ld + c;
+    };
+    double sum = 0.0;
+    for (int first = threadIdx.x; first < numel; first += 8 * TS_SMALL_THREADS) {
+        float u[8], m[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) u[j] = (float)g[min(first + j * TS_SMALL_THREADS, numel - 1)];
+        if (t.m) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) m[j] = t.m[min(first + j * TS_SMALL_THREADS, numel - 1)];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const int k = first + j * TS_SMALL_THREADS;
+            if (k >= numel) continue;
+            if (t.m) {
+                t.m[k] = m[j] = momentum_of(A, m[j], u[j]);
+                u[j] = direction_of(A, m[j], u[j]);
+            }
+            sum += (double)u[j] * u[j];
+            const unsigned word = __float_as_uint(u[j]);
+            const int at = place(k);
+            ((uint16_t *)X)[at] = (uint16_t)(word >> 16);
+            ((uint16_t *)X)[x_apart + at] = (uint16_t)word;
+        }
+    }
+    const Unit unit(series_inverse(A, t, block_sum<TS_SMALL_THREADS>(sum, sums)));
+    for (int k = threadIdx.x; k < numel; k += TS_SMALL_THREADS) {
+        const int at = place(k);
+        const float u = __uint_as_float((unsigned)((uint16_t *)X)[at] << 16 | ((uint16_t *)X)[x_apart + at]);
+        split16(unit.of(u), X[at], X[x_apart + at]);
+    }
+    // 16 bytes of a lane: row l % 16, k chunk l / 16 of rows along k
+    auto fragment = [&](const _Float16 *p, int row0, int stride, int k) { return lds_read16((LdsPointer)(p + (row0 + i) * stride + k + 8 * q)); };
+    // ... of rows of X as columns: column l % 16, k indices 8 (l / 16) .. + 7
+    auto column = [&](const _Float16 *p, int n0, int k) {
+        s16x4 h[2];
+#pragma unroll
+        for (int j = 0; j < 2; j++) h[j] = lds_read_transposed((LdsPointer)(p + (k + 8 * q + 4 * j + (i >> 2)) * ld + n0 + 4 * (i & 3)));
+        u32x4 f;
+        __builtin_memcpy(&f, h, 16);
+        return f;
+    };
+    // 16 x 16 results of a symmetric product of rows along k: lane l has row l % 16, columns 4 (l / 16) .. + 3
+    auto symmetric_tile = [&](const _Float16 *p, int apart, int stride, int row, int col, int K) {
+        f32x4 acc = {0, 0, 0, 0};
+        for (int k = 0; k < K; k += 32) {
+            const u32x4 a = fragment(p, col, stride, k), b = fragment(p, row, stride, k);
+            acc = mma<_Float16>(a, b, acc);
+            if constexpr (PARTS > 1) {
+                acc = mma<_Float16>(a, fragment(p + apart, row, stride, k), acc);
+                acc = mma<_Float16>(fragment(p + apart, col, stride, k), b, acc);
+            }
+        }
+        return acc;
+    };
+    // four neighbouring columns of a row of a symmetric matrix, and as a column; those that reach the diagonal one by one
+    auto put = [&](_Float16 *p, int row, int col, const float (&x)[4]) {
+        _Float16 h[4], l[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            split16(x[k], h[k], l[k]);
+            if (col + k >= row) continue;
+            p[(col + k) * ld_o + row] = h[k];
+            if (PARTS > 1) p[o_apart + (col + k) * ld_o + row] = l[k];
+            if (col + 3 >= row) {
+                p[row * ld_o + col + k] = h[k];
+                if (PARTS > 1) p[o_apart + row * ld_o + col + k] = l[k];
+            }
+        }
+        if (col + 3 < row) {
+            __builtin_memcpy(__builtin_assume_aligned(p + row * ld_o + col, 8), h, 8);
+            if (PARTS > 1) __builtin_memcpy(__builtin_assume_aligned(p + o_apart + row * ld_o + col, 8), l, 8);
+        }
+    };
+    auto four = [&](const _Float16 *p, int apart, float (&x)[4]) {
+        _Float16 h[4], l[4];
+        __builtin_memcpy(h, __builtin_assume_aligned(p, 8), 8);
+        __builtin_memcpy(l, __builtin_assume_aligned(p + apart, 8), 8);
+#pragma unroll
+        for (int k = 0; k < 4; k++) x[k] = apart ? (float)h[k] + (float)l[k] : (float)h[k];
+    };
+    const float gram = TS_SCALE / (t.S * t.S);
+    const int pairs = tiles * (tiles + 1) / 2, columns = (length + 15) / 16;
+    for (int s = 0; s < S.steps; s++) {
+        __syncthreads();
+        for (int p = wave; p < pairs; p += WAVES) {
+            int row, col;
+            triangle_tile<1>(p, row, col);
+            const f32x4 v = symmetric_tile(X, x_apart, ld, 16 * row, 16 * col, (length + 31) / 32 * 32);
+            const int m = 16 * row + i, n = 16 * col + 4 * q;
+            float x[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                x[k] = v[k] * gram;
+                if (n + k == m) d[m] = x[k] * (1.0f / TS_SCALE);
+            }
+            put(O, m, n, x);
         }
         __syncthreads();
+        for (int p = wave; p < pairs; p += WAVES) {
+            int row, col;
+            triangle_tile<1>(p, row, col);
+            const f32x4 v = symmetric_tile(O, o_apart, ld_o, 16 * row, 16 * col, (M + 31) / 32 * 32);
+            const int m = 16 * row + i, n = 16 * col + 4 * q;
+            const float dm = d[m];
+            float o[4];
+            four(O + m * ld_o + n, PARTS > 1 ? o_apart : 0, o);
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const float square = v[k] * (1.0f / TS_SCALE);
+                if (n + k == m) e[m] = S.ca + S.cb * dm + S.cc * (dm * dm + square * (1.0f / TS_SCALE));
+                o[k] = S.cb * o[k] + S.cc * ((dm + d[n + k]) * o[k] + square);
+            }
+            put(B, m, n, o);
+        }
+        __syncthreads();
+        for (int c = wave; c < columns; c += WAVES) {
+            u32x4 x[2][2];  // k steps, parts
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+                if (32 * k < M) {
+                    x[k][0] = column(X, 16 * c, 32 * k);
+                    if (PARTS > 1) x[k][1] = column(X + x_apart, 16 * c, 32 * k);
+                }
+            f32x4 acc[4];
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                acc[r] = f32x4{0, 0, 0, 0};
+                if (r >= tiles) continue;
+#pragma unroll
+                for (int k = 0; k < 2; k++)
+                    if (32 * k < M) {
+                        const u32x4 b = fragment(B, 16 * r, ld_o, 32 * k);
+                        acc[r] = mma<_Float16>(x[k][0], b, acc[r]);
+                        if constexpr (PARTS > 1) {
+                            acc[r] = mma<_Float16>(x[k][1], b, acc[r]);
+                            acc[r] = mma<_Float16>(x[k][0], fragment(B + o_apart, 16 * r, ld_o, 32 * k), acc[r]);
+                        }
+                    }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                if (r >= tiles) continue;
+                const int m = 16 * r + i;
+                _Float16 *const at = X + m * ld + 16 * c + 4 * q;
+                const float em = e[m];
+                float old[4];
+                four(at, x_apart, old);
+                _Float16 h[4], l[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++) split16(em * old[k] + acc[r][k] * (1.0f / TS_SCALE), h[k], l[k]);
+                __builtin_memcpy(__builtin_assume_aligned(at, 8), h, 8);
+                __builtin_memcpy(__builtin_assume_aligned(at + x_apart, 8), l, 8);
+            }
+        }
     }
-    for (int k = threadIdx.x; k < 4096; k += 256) {
-        const int along = k & 63, over = k >> 6, r = tall ? along : over, c = tall ? over : along;
-        if (r0 + r >= side || c0 + c >= length) continue;
-        const float d = tall ? tile[r][c] : t.direction[(size_t)(r0 + r) * t.ld + c0 + c];
-        const size_t at = tall ? (size_t)(c0 + c) * t.cols + r0 + r : (size_t)(r0 + r) * t.cols + c0 + c;
-        P *p = (P *)t.p + at;
-        const float q = MOVE ? (float)*p * A.decay - d * t.scale : d;
-        *p = (P)q;
-        if (MOVE && t.copy) {
-            if (A.copy_f16) ((_Float16 *)t.copy)[at] = (_Float16)q;
-            else ((__bf16 *)t.copy)[at] = (__bf16)q;
+    __syncthreads();
+    const float size = 1.0f / t.S;
+    for (int first = threadIdx.x; first < numel; first += 8 * TS_SMALL_THREADS) {
+        float p[8];
+        if (MOVE)
+#pragma unroll
+            for (int j = 0; j < 8; j++) p[j] = (float)((const P *)t.p)[min(first + j * TS_SMALL_THREADS, numel - 1)];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const int k = first + j * TS_SMALL_THREADS;
+            if (k >= numel) continue;
+            const int at = place(k);
+            const float v = ((float)X[at] + (float)X[x_apart + at]) * size, moved = MOVE ? p[j] * A.decay - v * t.scale : v;
+            ((P *)t.p)[k] = (P)moved;
+            if (MOVE && t.copy) {
+                if (A.copy_f16) ((_Float16 *)t.copy)[k] = (_Float16)moved;
+                else ((__bf16 *)t.copy)[k] = (__bf16)moved;
+            }
         }
     }
 }

@@ -87,6 +87,31 @@ __device__ __forceinline__ unsigned wave_max(unsigned v) {
 }
 #endif
 
+// 4 elements from index i of n on; beyond the end zeros.  WHOLE: all are there, and aligned to their size
+template <bool WHOLE, class T> __device__ __forceinline__ void load4(const T *p, int64_t i, int64_t n, bool vec, T (&x)[4]) {
+    if (WHOLE || (vec && i + 4 <= n)) {
+        struct alignas(4 * sizeof(T)) V { T v[4]; } o = *(const V *)(p + i);
+#pragma unroll
+        for (int e = 0; e < 4; e++) x[e] = o.v[e];
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; e++) x[e] = i + e < n ? p[i + e] : (T)0;
+}
+template <bool WHOLE, class T> __device__ __forceinline__ void store4(T *p, int64_t i, int64_t n, bool vec, const T (&x)[4]) {
+    if (WHOLE || (vec && i + 4 <= n)) {
+        struct alignas(4 * sizeof(T)) V { T v[4]; } o;
+#pragma unroll
+        for (int e = 0; e < 4; e++) o.v[e] = x[e];
+        *(V *)(p + i) = o;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        if (i + e < n) p[i + e] = x[e];
+}
+template <class T> __device__ __forceinline__ bool at4(const T *p) { return ((uintptr_t)p & (4 * sizeof(T) - 1)) == 0; }
+
 // 32-bit values kept in 24 bits: the upper 16 of their words in one plane, the next 8 (rounded to nearest even) in another
 __device__ __forceinline__ void store_oct24(uint16_t *hi, uint8_t *lo, const float (&x)[8]) {
     u32x4 h;

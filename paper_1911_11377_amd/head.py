@@ -7,23 +7,39 @@ plain features (training.py: one forward and one backward call and one optimiser
   act     : linear, square, poly2 or poly3 (activation.py) on the gate's outputs             level l-1 -> l-1, l-2, l-3, l-3
   product : the other outputs dropped to that level, ciphertext x ciphertext, rescale        one level
   fc      : Wd, then a rescale                                                               one level
+
+`ResidualHead` puts norms around such a block, r = a x + b gate * N_post(block(N_pre(x))): whoever encrypts the features norms them first
+and takes the norm, the gate and the sum of what was decrypted, so the block under encryption stays the same.  `LowBitHead`
+answers in the clear from the trained matrices in 4 bits.
 """
 import contextlib
 from dataclasses import dataclass
 
 import numpy as np
 
-from . import activation, ckksmi, training
+from . import activation, ckksmi, lowbit, training
+
+
+def _on_stream(stream, f, *args):
+    """f(*args) with `stream` (an address; None: as it is) as torch's current one"""
+    import torch
+
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(torch.cuda.ExternalStream(stream)):
+        return f(*args)
 
 
 class GatedHead:
     """Training state of a head on up to `rows` rows a step.  weights: float32 device tensors [d_hidden][d_in] (twice) and
     [d_out][d_hidden], updated in place; dtype: the type the products run in (bfloat16 and float16: copies of the weights,
-    renewed by each step); state_bits: 8 or 32.  empty(shape, dtype) allocates zeros on the device.  The constructor waits for
-    what it enqueues: answers and steps may use any stream."""
+    renewed by each step); state_bits: 8 or 32.  optimizer: "adamw", or "muon" (steps along orthogonalised momentum, which is held in 32
+    bits).  empty(shape, dtype) allocates zeros on the device.  The constructor waits for what it enqueues: answers and steps may
+    use any stream."""
 
-    def __init__(self, ctx, rows, weights, act, dtype, empty, state_bits=8):
+    def __init__(self, ctx, rows, weights, act, dtype, empty, state_bits=8, optimizer="adamw"):
         import torch
+
+        if optimizer not in ("adamw", "muon"):
+            raise ValueError("expected 'adamw' or 'muon', got %r" % (optimizer,))
 
         d_hidden, d_in = weights[0].shape
         self.weights, self.steps = weights, 0
@@ -35,10 +51,15 @@ class GatedHead:
                 c.copy_(w)
         self.used = copies or weights
         self.grads = [empty(tuple(w.shape), dtype) for w in weights]
-        state = torch.uint8 if state_bits == 8 else torch.float32
-        m, v = [[empty(tuple(w.shape), state) for w in weights] for _ in range(2)]
-        units = [[empty((-(-w.numel() // ckksmi.STATE_BLOCK),), torch.float32) for w in weights] for _ in range(2)] if state_bits == 8 else (None, None)
-        self.opt = training.AdamW(ctx, weights, self.grads, m, v, *units, copies=copies)
+        self.opt_ws = None
+        if optimizer == "muon":
+            self.opt = training.Muon(ctx, weights, self.grads, [empty(tuple(w.shape), torch.float32) for w in weights], copies=copies)
+            self.opt_ws = empty((max(16, self.opt.workspace_bytes()),), torch.uint8)
+        else:
+            state = torch.uint8 if state_bits == 8 else torch.float32
+            m, v = [[empty(tuple(w.shape), state) for w in weights] for _ in range(2)]
+            units = [[empty((-(-w.numel() // ckksmi.STATE_BLOCK),), torch.float32) for w in weights] for _ in range(2)] if state_bits == 8 else (None, None)
+            self.opt = training.AdamW(ctx, weights, self.grads, m, v, *units, copies=copies)
         self.ws = empty((max(16, self.ff.workspace_bytes(rows, backward=True)),), torch.uint8)
         self.saved = empty((max(16, self.ff.saved_bytes(rows)),), torch.uint8)
         self.y, self.dy = [empty((rows, weights[2].shape[0]), dtype) for _ in range(2)]
@@ -51,18 +72,103 @@ class GatedHead:
     def step(self, x, loss, lr, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.0, stream=None):
         """One step on rows x.  loss(y, dy) writes the loss's gradient by the answers y into dy; what it returns is returned.  All of the step is
         enqueued on `stream`: loss is called with it as torch's current stream (x and what loss reads have to be ordered before it,
-        and what loss returns is ready when it has come that far)."""
-        import torch
-
+        and what loss returns is ready when it has come that far).  Muon: betas[0] is its momentum; eps is AdamW's alone."""
         rows = x.shape[0]
         y, dy = self.y[:rows], self.dy[:rows]
         self.ff.forward(x, *self.used, y, self.ws, saved=self.saved, stream=stream)
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(torch.cuda.ExternalStream(stream)):
-            out = loss(y, dy)
+        out = _on_stream(stream, loss, y, dy)
         self.ff.backward(x, *self.used, self.saved, dy, None, *self.grads, self.ws, stream=stream)
-        self.steps += 1
-        self.opt.step(lr, betas, eps, weight_decay, self.steps, seed=self.steps, stream=stream)
+        self._move(lr, betas, eps, weight_decay, stream)
         return out
+
+    def _move(self, lr, betas, eps, weight_decay, stream):
+        self.steps += 1
+        if self.opt_ws is not None:
+            self.opt.step(lr, betas[0], self.opt_ws, weight_decay=weight_decay, stream=stream)
+        else:
+            self.opt.step(lr, betas, eps, weight_decay, self.steps, seed=self.steps, stream=stream)
+
+
+class ResidualHead:
+    """A gated block between norms, answers of the features' width: r = residual_scale x + block_scale gate * N_post(block(N_pre(x))), with a learned
+    gate for every channel.  `block` is the GatedHead inside (its weights, its optimizer); `vectors` are the norms' weights and the gate
+    (float32, from ones; AdamW with 32-bit states).  Arguments as for GatedHead."""
+
+    def __init__(self, ctx, rows, weights, act, dtype, empty, norm="rms", residual_scale=1.0, block_scale=1.0, eps=1e-5, optimizer="muon", state_bits=32):
+        import torch
+
+        d = weights[0].shape[1]
+        if weights[2].shape[0] != d:
+            raise ValueError("a residual block answers with as many values as it reads: %d and %d" % (weights[2].shape[0], d))
+        self.block = GatedHead(ctx, rows, weights, act, dtype, empty, state_bits=state_bits, optimizer=optimizer)
+        self.before = training.ResidualNorm(ctx, d, dtype, pre=norm, post=None, weight_dtype=torch.float32, eps=eps)
+        self.after = training.ResidualNorm(ctx, d, dtype, pre=None, post=norm, gate="channel", weight_dtype=torch.float32, eps=eps, residual_scale=residual_scale,
+                                           block_scale=block_scale)
+        names = ["pre_weight", "post_weight", "gate"] + (["pre_bias", "post_bias"] if norm == "layer" else [])
+        self.vectors = {k: empty((d,), torch.float32).fill_(0.0 if k.endswith("bias") else 1.0) for k in names}
+        self.grads = {k: empty((d,), torch.float32) for k in names}
+        states = [[empty((d,), torch.float32) for _ in names] for _ in range(2)]
+        self.opt = training.AdamW(ctx, [self.vectors[k] for k in names], [self.grads[k] for k in names], *states)
+        self.n, self.f, self.df, self.dn, self.r, self.dr = [empty((rows, d), dtype) for _ in range(6)]
+        self.saved = [empty((max(16, p.saved_bytes(rows)),), torch.uint8) for p in (self.before, self.after)]
+        self.ws = empty((max(16, self.before.workspace_bytes(rows), self.after.workspace_bytes(rows)),), torch.uint8)
+        if weights[0].is_cuda:
+            torch.cuda.current_stream(weights[0].device).synchronize()
+
+    def _of(self, side, grads=False):
+        at = self.grads if grads else self.vectors
+        return {("d" if grads else "") + k: v for k, v in at.items() if k.startswith(side) or (side == "post" and k == "gate")}
+
+    def normed(self, x, n, stream=None):
+        """n = N_pre(x): what is encrypted"""
+        self.before.forward(x, None, None, n, **self._of("pre"), stream=stream)
+
+    def joined(self, x, f, r, stream=None):
+        """r from x and the block's answers f (decrypted ones, say)"""
+        self.after.forward(x, f, r, None, **self._of("post"), stream=stream)
+
+    def answer(self, x, r, stream=None):
+        rows = x.shape[0]
+        self.normed(x, self.n[:rows], stream)
+        self.block.answer(self.n[:rows], self.f[:rows], stream)
+        self.joined(x, self.f[:rows], r, stream)
+
+    def step(self, x, loss, lr, vector_lr=1e-3, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.0, stream=None):
+        """one step on rows x, like GatedHead.step; vector_lr: of the norms' weights and the gate"""
+        rows, b = x.shape[0], self.block
+        n, f, df, dn, r, dr = (t[:rows] for t in (self.n, self.f, self.df, self.dn, self.r, self.dr))
+        self.before.forward(x, None, None, n, **self._of("pre"), saved=self.saved[0], stream=stream)
+        b.ff.forward(n, *b.used, f, b.ws, saved=b.saved, stream=stream)
+        self.after.forward(x, f, r, None, **self._of("post"), saved=self.saved[1], stream=stream)
+        out = _on_stream(stream, loss, r, dr)
+        self.after.backward(x, f, self.saved[1], dr, None, self.ws, df=df, **self._of("post", grads=True), **self._of("post"), stream=stream)
+        b.ff.backward(n, *b.used, b.saved, df, dn, *b.grads, b.ws, stream=stream)
+        self.before.backward(x, None, self.saved[0], None, dn, self.ws, **self._of("pre", grads=True), **self._of("pre"), stream=stream)
+        b._move(lr, betas, eps, weight_decay, stream)
+        self.opt.step(vector_lr, betas, eps, 0.0, b.steps, stream=stream)
+        return out
+
+
+class LowBitHead:
+    """A trained head's answers in the clear from its matrices in 4 bits, up to `rows` rows a call.  weights: device tensors as for GatedHead (read once,
+    here); empty(shape, dtype) allocates on the device.  The constructor waits for what it enqueues."""
+
+    def __init__(self, ctx, rows, weights, act, dtype, empty, group=128):
+        import torch
+
+        d_hidden, d_in = weights[0].shape
+        self.ff = lowbit.GatedFF4(ctx, d_in, d_hidden, weights[2].shape[0], dtype, act, group)
+        self.matrices = []
+        for w, plan in zip(weights, (self.ff.into, self.ff.into, self.ff.out)):
+            pair = empty(plan.codes_shape, torch.uint8), empty(plan.scales_shape, dtype)
+            plan.pack(w, *pair)
+            self.matrices.append(pair)
+        self.ws = empty((max(16, self.ff.workspace_bytes(rows)),), torch.uint8)
+        if weights[0].is_cuda:
+            torch.cuda.current_stream(weights[0].device).synchronize()
+
+    def answer(self, x, y, stream=None):
+        self.ff.forward(x, *self.matrices, y, self.ws, stream=stream)
 
 
 @dataclass

@@ -249,6 +249,9 @@ extern "C" void emu_enough_tiles(int n) { g_enough = n; }
 static unsigned g_copy_blocks = 1u << 23;
 extern "C" void emu_copy_blocks(unsigned n) { g_copy_blocks = n; }
 #define TG_COPY_BLOCKS g_copy_blocks
+static size_t g_small = (size_t)-1;  // matrices that take one workgroup: bytes of its LDS at most
+extern "C" void emu_series_small(size_t bytes) { g_small = bytes; }
+#define TS_SMALL_MOST (g_small < TS_SMALL_LDS ? g_small : (size_t)TS_SMALL_LDS)
 #include "../../paper_1911_11377_amd/csrc/train_device.hip"
 #include "../../paper_1911_11377_amd/csrc/norm_device.hip"
 #include "../../paper_1911_11377_amd/csrc/muon_device.hip"

@@ -1,4 +1,5 @@
 """Orthogonalised directions and steps along them on the CPU stand-in: small sizes of each kernel, and refusals."""
+import ctypes as C
 import math
 
 import pytest
@@ -12,10 +13,15 @@ from series_reference import BF16, F16, F32
 pytestmark = pytest.mark.skipif(not emu.available, reason="no host compiler with 16-bit float types")
 
 
-@pytest.fixture(scope="module")
-def ctx():
+@pytest.fixture(scope="module", params=["small", "tiles"])
+def ctx(request):
+    """matrices in one workgroup's LDS where they fit; and in tiles whatever their size"""
     c = emu.EmuContext()
+    c._L.emu_series_small.argtypes = [C.c_size_t]
+    c.kind = request.param
+    c._L.emu_series_small(2**63 if c.kind == "small" else 0)
     yield c
+    c._L.emu_series_small(2**63)
     assert c.errors() == 0
     c.close()
 
@@ -87,6 +93,15 @@ def test_values_that_are_not_finite(ctx):
         sr.check(outs[1], v, 2)
 
 
+@pytest.mark.parametrize("rows,cols", [(64, 380), (1050, 16), (48, 400), (17, 33), (64, 64)], ids=str)
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_the_largest_that_fit_one_workgroup(ctx, rows, cols, dtype):
+    u = ctx.guarded(sr.matrix(rows, cols, 5, "strong", dtype))
+    plan = training.Orthogonalise(ctx, [u], [ctx.guarded(torch.zeros_like(u))])
+    assert (plan.workspace_bytes() == 0) == (ctx.kind == "small")
+    sr.check(direct(ctx, u, steps=2), u, 1 if dtype == BF16 else 2, steps=2)
+
+
 def test_other_polynomials_and_numbers_of_steps(ctx):
     u = ctx.guarded(sr.matrix(9, 21, 8))
     for steps, k in ((1, sr.COEFFICIENTS), (4, sr.COEFFICIENTS), (8, (1.5, -0.5, 0.0)), (3, (2.0, -1.5, 0.5))):
@@ -146,13 +161,13 @@ def refused(code, call, *args, **kw):
 
 
 def test_polynomials_that_leave_the_range_are_refused(ctx):
-    u = sr.matrix(4, 6, 1)
+    u = sr.matrix(70, 80, 1)
     plan = training.Orthogonalise(ctx, [u], [torch.zeros_like(u)])
     ws = room(ctx, plan.workspace_bytes())
     for kw in (dict(steps=0), dict(steps=33), dict(eps=-1.0), dict(eps=math.nan), dict(coefficients=(3.0, 0.0, 0.0)), dict(coefficients=(1.0, math.inf, 0.0)),
                dict(coefficients=(0.0, 0.0, 120.0)), dict(coefficients=(1.5, 0.0, 0.0), steps=3)):
         refused(ckksmi.EINVAL, plan.run, ws, **kw)
-    plan.run(ws, steps=32)
+    plan.run(ws, steps=3)
     refused(ckksmi.EWORKSPACE, plan.run, ws[:-1])
     refused(ckksmi.EINVAL, plan.run, ctx.guarded(torch.zeros(ws.numel() + 8, dtype=torch.uint8))[8:])
 
@@ -174,7 +189,7 @@ def test_plans_that_are_refused(ctx):
 
 
 def test_steps_that_are_refused(ctx):
-    p, g, m = sr.matrix(4, 6, 1), sr.matrix(4, 6, 2), sr.matrix(4, 6, 3)
+    p, g, m = sr.matrix(70, 80, 1), sr.matrix(70, 80, 2), sr.matrix(70, 80, 3)
     opt = training.Muon(ctx, [p], [g], [m])
     ws = room(ctx, opt.workspace_bytes())
     for a, kw in (((math.nan, 0.9), {}), ((0.1, 1.0), {}), ((0.1, -0.1), {}), ((0.1, 0.9), dict(weight_decay=math.inf)), ((0.1, 0.9), dict(grad_scale=math.nan)),
@@ -186,5 +201,5 @@ def test_steps_that_are_refused(ctx):
     bad = training.Muon(ctx, [p], [g], [m], scales=[math.inf])
     refused(ckksmi.EINVAL, bad.workspace_bytes)
     both = torch.zeros(ws.numel() + 4096, dtype=torch.uint8)
-    inside = both[1024:1024 + 96].view(torch.float32).view(4, 6)
+    inside = both[1024:1024 + 4 * 5600].view(torch.float32).view(70, 80)
     refused(ckksmi.EINVAL, training.Muon(ctx, [inside], [g], [m]).step, 0.1, 0.9, both)
