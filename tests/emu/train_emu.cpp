@@ -252,6 +252,9 @@ extern "C" void emu_copy_blocks(unsigned n) { g_copy_blocks = n; }
 static size_t g_small = (size_t)-1;  // matrices that take one workgroup: bytes of its LDS at most
 extern "C" void emu_series_small(size_t bytes) { g_small = bytes; }
 #define TS_SMALL_MOST (g_small < TS_SMALL_LDS ? g_small : (size_t)TS_SMALL_LDS)
+static int g_tile = -1;  // of the large ones: 0, 1, or as the rule says
+extern "C" void emu_series_tile(int n) { g_tile = n; }
+#define TS_TILE(rule) (g_tile >= 0 ? g_tile : (rule))
 #include "../../paper_1911_11377_amd/csrc/train_device.hip"
 #include "../../paper_1911_11377_amd/csrc/norm_device.hip"
 #include "../../paper_1911_11377_amd/csrc/muon_device.hip"
