@@ -74,7 +74,7 @@ int ckksmi_gated_ff_backward(ckksmi_ctx *ctx, const ckksmi_gated_ff *ff, const v
  * CKKSMI_NORM_NONE.  f may be NULL (in front of the first block): n = N_pre(x); then r, gate and post's weights have to be NULL.
  * x, f, r, n and an element gate are of `dtype`, rows ld_* elements apart (0 = dense); w, b [d] and a channel gate [d] of
  * weight_dtype; a NULL w is ones, a NULL b zeros.  Everything is formed in 32 bits (n from r before it is rounded) and rounded once.
- * 0 <= rows < 2^31 - 256, d and every ld 1 .. 2^20.  eps >= 0 and the scales finite. */
+ * 0 <= rows <= 2^30, d and every ld 1 .. 2^20.  eps >= 0 and the scales finite. */
 #define CKKSMI_NORM_NONE 0
 #define CKKSMI_NORM_RMS 1
 #define CKKSMI_NORM_LAYER 2
@@ -203,7 +203,7 @@ typedef struct {
  * whose scale is not finite gets scale NaN, one whose scale is 0 codes 0.  And back: w = scale * code, rounded to w_dtype */
 int ckksmi_pack4(ckksmi_ctx *ctx, const ckksmi_matrix4 *m, int w_dtype, const void *w, void *codes, void *scales, void *stream);
 int ckksmi_unpack4(ckksmi_ctx *ctx, const ckksmi_matrix4 *m, int w_dtype, const void *codes, const void *scales, void *w, void *stream);
-/* y = x W^T; x: [rows][d_in], y: [rows][d_out], rows ld_* elements apart (0 = dense).  0 <= rows < 2^22.  y must not overlap an input. */
+/* y = x W^T; x: [rows][d_in], y: [rows][d_out], rows ld_* elements apart (0 = dense).  0 <= rows <= 2^21.  y must not overlap an input. */
 int ckksmi_product4(ckksmi_ctx *ctx, const ckksmi_matrix4 *m, int64_t rows, const void *x, int64_t ld_x, const void *codes, const void *scales, void *y, int64_t ld_y,
                     void *stream);
 /* The gated block from such matrices (all of one dtype and group): y = (act(x Wg^T) * (x Wu^T)) Wd^T.  h = act(g) u is held in two bf16 parts (16 bits;

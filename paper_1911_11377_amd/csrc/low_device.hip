@@ -4,7 +4,7 @@
 
 namespace {
 
-constexpr int64_t kMaxRows4 = (1 << 22) - 1;
+constexpr int64_t kMaxRows4 = 1 << 21;  // (64 rows a workgroup along y, of which a launch has 65535)
 
 int check_matrix4(const ckksmi_matrix4 &m) {
     if (!dtype_ok(m.dtype) || m.group < 32 || m.group > 1024 || (m.group & (m.group - 1))) return CKKSMI_EINVAL;

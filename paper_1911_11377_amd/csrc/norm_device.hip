@@ -4,13 +4,15 @@
 
 namespace {
 
+constexpr int64_t kMaxNormRows = 1 << 30;  // (the kernels go on by a grid's rows from there, in 32 bits)
+
 int check_norm(const ckksmi_residual_norm &c) {
     if (!dtype_ok(c.dtype) || (c.weight_dtype != c.dtype && c.weight_dtype != CKKSMI_F32)) return CKKSMI_EINVAL;
     for (int k : {c.pre, c.post})
         if (k < CKKSMI_NORM_NONE || k > CKKSMI_NORM_LAYER) return CKKSMI_EINVAL;
     if (c.gate < CKKSMI_GATE_NONE || c.gate > CKKSMI_GATE_ELEMENT) return CKKSMI_EINVAL;
     if (!(c.eps >= 0) || !std::isfinite(c.eps) || !std::isfinite(c.residual_scale) || !std::isfinite(c.block_scale)) return CKKSMI_EINVAL;
-    if (c.rows < 0 || c.rows > kMaxRows || c.d < 1 || c.d > kMaxDim) return CKKSMI_EINVAL;
+    if (c.rows < 0 || c.rows > kMaxNormRows || c.d < 1 || c.d > kMaxDim) return CKKSMI_EINVAL;
     for (int64_t ld : {c.ld_x, c.ld_f, c.ld_gate, c.ld_r, c.ld_n, c.ld_dr, c.ld_dn, c.ld_dx, c.ld_df, c.ld_dgate})
         if (ld != 0 && (ld < c.d || ld > kMaxDim)) return CKKSMI_EINVAL;
     return CKKSMI_OK;

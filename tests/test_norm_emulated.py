@@ -161,6 +161,8 @@ def test_plans_that_make_no_sense(ctx):
         d, dtype = kw.pop("d"), kw.pop("dtype")
         refused(ckksmi.EINVAL, training.ResidualNorm(ctx, d, dtype, **kw).workspace_bytes, 4)
     refused(ckksmi.EINVAL, training.ResidualNorm(ctx, 8, F32).saved_bytes, -1)
+    assert training.ResidualNorm(ctx, 8, F32).saved_bytes(2**30) == 2**34
+    refused(ckksmi.EINVAL, training.ResidualNorm(ctx, 8, F32).saved_bytes, 2**30 + 1)
 
 
 def test_forward_calls_that_are_refused(ctx):
