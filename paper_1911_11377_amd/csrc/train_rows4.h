@@ -336,7 +336,6 @@ template <class W, class O> __global__ void __launch_bounds__(256) pack4_kernel(
     float scale = (float)(O)(__uint_as_float(most) / 7.0f);
     const bool held = scale <= 3.4028234e38f;
     if (!held) scale = __uint_as_float(0x7fc00000u);
-    const float inverse = held && scale > 0.0f ? 1.0f / scale : 0.0f;
     if (lane == 0) ((O *)A.scales)[id] = (O)scale;
     // 8 codes a lane, to the end of the row's 16 bytes
     const int stop = min(k0 + A.group, (A.K + 31) / 32 * 32);
@@ -344,7 +343,7 @@ template <class W, class O> __global__ void __launch_bounds__(256) pack4_kernel(
         unsigned c = 0;
 #pragma unroll
         for (int e = 0; e < 8; e++)
-            if (k + e < A.K && inverse > 0.0f) c |= ((unsigned)(int)fminf(fmaxf(rintf((float)w[k + e] * inverse), -8.0f), 7.0f) & 15u) << (4 * e);
+            if (k + e < A.K && scale > 0.0f) c |= ((unsigned)(int)fminf(fmaxf(rintf((float)w[k + e] / scale), -8.0f), 7.0f) & 15u) << (4 * e);  // (1 / scale may be beyond f32)
         *(unsigned *)(A.codes + (size_t)row * A.ldc + k / 2) = c;
     }
 }

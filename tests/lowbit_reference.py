@@ -100,9 +100,8 @@ def nearest(w, group, dtype):
     most = torch.where(torch.isnan(parts).any(2), torch.full_like(most, math.nan), most)
     scale = (most / 7.0).to(dtype).float()
     scale = torch.where(torch.isfinite(scale), scale, torch.full_like(scale, math.nan))
-    inverse = torch.where(scale > 0, 1.0 / scale, torch.zeros_like(scale))
-    c = torch.round(parts * inverse[..., None]).clamp(-8, 7)
-    c = torch.where((inverse > 0)[..., None], c, torch.zeros_like(c)).view(rows, -1)[:, :cols]
+    c = torch.round(parts / scale[..., None]).clamp(-8, 7)
+    c = torch.where((scale > 0)[..., None], c, torch.zeros_like(c)).view(rows, -1)[:, :cols]
     padded = torch.zeros(rows, -(-cols // 32) * 32)
     padded[:, :cols] = c
     n = padded.to(torch.int64) & 15

@@ -57,6 +57,24 @@ def test_packing(ctx, rows, cols, group, dtype, wt):
     assert bool(((back.double() - w.double()).abs() <= reach).all())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_scales_whose_inverse_f32_does_not_hold(ctx, dtype):
+    """weights of 1e-39 with zeros between them: zeros stay zeros, the others within half a scale (and what the scale's rounding adds)"""
+    w = torch.zeros(2, 64)
+    w[:, ::2] = torch.linspace(-7e-39, 7e-39, 32)
+    plan = lowbit.Product4(ctx, 64, 2, dtype, 64)
+    codes, scales, back = torch.zeros(plan.codes_shape, dtype=torch.uint8), torch.zeros(plan.scales_shape, dtype=dtype), torch.ones(2, 64)
+    plan.pack(w, codes, scales)
+    plan.unpack(codes, scales, back)
+    s = scales.double().amax()
+    assert 0.9e-39 < float(s) < 1.1e-39 and bool((back[:, 1::2] == 0).all())
+    # (a bf16 denormal near 1e-39 has steps of 2^-133, 9e-41: the largest weight is seven times half of that off)
+    off = s * 0.5 + (7 * 2.0**-134 if dtype == BF16 else 7 * 2.0**-149)
+    assert bool(((back.double() - w.double()).abs() <= off).all())
+    want = lr.nearest(w, 64, dtype)
+    assert torch.equal(codes, want[0]) and torch.equal(scales, want[1])
+
+
 def test_groups_without_a_finite_scale(ctx):
     w = torch.ones(4, 64)
     w[0, 3], w[1, 40], w[2, 5] = math.inf, math.nan, 1e38
@@ -120,7 +138,7 @@ def test_plans_that_are_refused(ctx):
     for group in (0, -32):
         refused(ckksmi.EINVAL, lowbit.GatedFF4(ctx, 64, 8, 8, BF16, "silu", group).workspace_bytes, 1)
     refused(ckksmi.EINVAL, lowbit.GatedFF4(ctx, 2**20 + 1, 8, 8, BF16, "silu").workspace_bytes, 1)
-    refused(ckksmi.EINVAL, lowbit.GatedFF4(ctx, 64, 8, 8, BF16, "silu").workspace_bytes, 2**22)
+    refused(ckksmi.EINVAL, lowbit.GatedFF4(ctx, 64, 8, 8, BF16, "silu").workspace_bytes, 2**21 + 1)
     with pytest.raises(ValueError):
         lowbit.Product4(ctx, 64, 8, torch.float64)
     with pytest.raises(KeyError):
