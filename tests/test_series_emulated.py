@@ -51,13 +51,11 @@ def test_spectra(ctx, kind, dtype):
     sr.check(direct(ctx, u), u, 1 if dtype == BF16 else 2)
 
 
-@pytest.mark.parametrize("size", [(140, 70), (200, 140), (300, 290)], ids=str)
-@pytest.mark.parametrize("tile", [0, 1, -1], ids=["256", "128", "rule"])
-@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size,tile,dtype", [((140, 70), 0, F32), ((140, 70), 1, F32), ((200, 140), 0, BF16), ((200, 140), 1, F32), ((200, 140), -1, BF16), ((300, 290), 0, BF16)], ids=str)
 def test_large_tiles(ctx, size, tile, dtype):
     """tiles of 128 x 128 and 256 x 256, whole and ragged, below and on the diagonal"""
-    if size == (300, 290) and dtype == F32 and tile == -1:
-        pytest.skip("minutes, and nothing that the others do not reach")
+    if ctx.kind == "small":
+        pytest.skip("matrices that are none for one workgroup: the same kernels as the other way")
     ctx._L.emu_enough_tiles(1)
     ctx._L.emu_series_tile(tile)
     try:
