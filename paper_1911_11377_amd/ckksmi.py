@@ -209,7 +209,7 @@ def _current_stream():
     global _current_stream
     import torch
 
-    if hasattr(torch._C, "_cuda_getCurrentRawStream"):  # 0.2 us; a Stream object takes 2.6
+    if hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice"):  # 0.2 us; a Stream object takes 2.6
         torch.cuda.current_stream()  # (initialises CUDA if nothing has yet)
         raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _current_stream = lambda: raw(device())  # noqa: E731

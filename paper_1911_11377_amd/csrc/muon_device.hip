@@ -301,9 +301,9 @@ template <class P, bool MOVE> void run_series(ckksmi_ctx *c, const SeriesCall &c
 
 int check_sizes(int64_t rows, int64_t cols) { return rows < 0 || cols < 0 || rows > kMaxSide || cols > kMaxSide ? CKKSMI_EINVAL : CKKSMI_OK; }
 
-// directions that end in bf16 are formed from upper parts
+// Directions that end in bf16 are formed from upper parts alone: 6e-4 of the direction's size off, where bf16 rounds by 4e-3
 inline int parts_of_direction(int dtype) { return dtype == CKKSMI_BF16 ? 1 : 2; }
-// steps move 16-bit parameters by far less than their last place's error times ..
+// ... and so are those that move 16-bit parameters: a step is a small part of them, 6e-4 of it less than their last place (4e-3, 5e-4 of them)
 inline int parts_of_step(int p_dtype) { return p_dtype == CKKSMI_F32 ? 2 : 1; }
 
 int directions_call(const ckksmi_series *s, const ckksmi_direction *t, int n, int dtype, ckksmi_series &series, std::vector<SeriesTensor> &out) {
