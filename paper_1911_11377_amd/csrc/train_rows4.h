@@ -7,7 +7,8 @@
 // conversion gives), a group's sum stays in f32 and is scaled there: a scaled weight rounded to 16 bits would cost three decimal
 // places of four.  x: 16-bit as it is, f32 in three bf16 parts, cut as it is read; h between the block's products in two or three bf16 parts.
 // The waves' sums meet in LDS and are added in their order.
-// Bound by the codes' bytes and, for small matrices, by the latency of one trip to memory.
+// Bound by the codes' bytes (one row, 8192 -> 16384: 20 - 22.5 us, 3.1 - 3.4 TB/s), for small matrices by the latency of one trip to memory (1024 -> 4096,
+// two of them: 7.4 us), and for 64 f32 rows by cutting x, which every workgroup does (4096 -> 4096: 24 - 27 us)
 #pragma once
 #include "train_rows.h"
 
