@@ -132,3 +132,16 @@ def test_a_trained_block_in_4_bits_answers_like_itself(ctx):
     # the wide product's bound has the same terms, over d_in and d_hidden instead of groups
     wider, other = lr.ref.block(x.cpu(), *(t.cpu() for t in wide), "silu")["y"]
     assert bool(((y.double().cpu() - z.double().cpu()).abs() <= 1.25 * bound + other + lr.U * v.abs()).all()) and float((wider - v).abs().max()) < 1e-6
+
+
+def test_as_many_rows_as_a_call_takes(ctx):
+    """2^21 rows, 16-row tiles 64 rows a workgroup: every 2^17-th row is as in a call on 64 rows (the same kernel)"""
+    plan = lowbit.Product4(ctx, 40, 24, BF16, 32)
+    w = [t.to(DEV) for t in lr.weights(24, 40, 32, BF16, 1)]
+    x = torch.randn(2**21, 40, device=DEV, generator=torch.Generator(DEV).manual_seed(2)).to(BF16)
+    y = torch.full((2**21, 24), math.nan, dtype=BF16, device=DEV)
+    plan.forward(x, *w, y)
+    some = x[2**17 - 1::2**17].repeat(4, 1)
+    want = torch.empty(64, 24, dtype=BF16, device=DEV)
+    plan.forward(some, *w, want)
+    assert torch.equal(y[2**17 - 1::2**17], want[:16]) and bool(torch.isfinite(y).all())

@@ -151,3 +151,34 @@ def test_no_rows(ctx):
         g = {k: torch.full((12,), 3.0, device=DEV) for k in ("dpost_weight", "dpre_weight", "dpre_bias", "dgate")}
         plan.backward(none, none, torch.empty(0, dtype=torch.uint8, device=DEV), none, none, None, gate=torch.ones(12, device=DEV), accumulate=accumulate, **g)
         assert all(bool((t == (3.0 if accumulate else 0.0)).all()) for t in g.values())
+
+
+def test_offsets_that_32_bits_do_not_hold(ctx):
+    """2^20 + 5 rows of 4096: the last rows' results are those of a call on them alone"""
+    rows, d, last = 2**20 + 5, 4096, 9
+    c = nr.Case(last, d, BF16, "rms", "rms", "channel", F32, device=DEV)
+    plan = training.ResidualNorm(ctx, d, BF16, "rms", "rms", "channel", F32)
+
+    def run(x, f, dr, dn):
+        n = x.shape[0]
+        r, out, dx, df = (torch.empty_like(x) for _ in range(4))
+        vectors = {k: torch.empty(d, device=DEV) for k in ("dgate", "dpost_weight", "dpre_weight")}
+        saved, ws = torch.empty(plan.saved_bytes(n), dtype=torch.uint8, device=DEV), torch.empty(plan.workspace_bytes(n), dtype=torch.uint8, device=DEV)
+        plan.forward(x, f, r, out, gate=c.gate, saved=saved, **c.w)
+        plan.backward(x, f, saved, dr, dn, ws, dx=dx, df=df, gate=c.gate, **vectors, **c.w)
+        return [t[n - last:].clone() for t in (r, out, dx, df)], vectors
+
+    def behind_zeros(t):
+        whole = torch.zeros(rows, d, dtype=t.dtype, device=DEV)
+        whole[rows - last:] = t
+        return whole
+
+    want, sums = run(c.x, c.f, c.dr, c.dn)
+    got, all_sums = run(*(behind_zeros(t) for t in (c.x, c.f, c.dr, c.dn)))
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    # zeros add nothing: the same terms in another order, each sum within (last - 1) 2^-24 of its terms' sizes, at most the largest times their number
+    for k in sums:
+        terms = last * max(float(c.dr.abs().max()), float(c.dn.abs().max()), float(want[2].abs().max())) * 4 * math.sqrt(d)
+        assert float((all_sums[k] - sums[k]).abs().max()) <= 2 * (last - 1) * 2.0**-24 * terms
+    torch.cuda.empty_cache()

@@ -148,3 +148,36 @@ def test_equal_calls_give_equal_bits_on_any_stream_and_in_graphs(ctx):
         torch.cuda.synchronize()
         want = first if i != 2 else p0 + [torch.zeros_like(t) for t in p0]
         assert all(torch.equal(a, b) for a, b in zip(p + m, want)), i
+
+
+def test_offsets_that_32_bits_do_not_hold(ctx):
+    """one step on 2^31 elements of 8 strong directions, some rows against products with a vector in 32 bits.  A row of a X + (b A + c A^2) X has five
+    roundings to 11 bits on its way (X twice in A, A, the polynomial, X), each off by 2^-11 of at most (|b| + |c|) |x| as |X| <= 1, and one to bf16"""
+    m, n, many = 32768, 65536, 4096
+    g = torch.Generator(DEV).manual_seed(5)
+    left, right = torch.randn(m, 8, device=DEV, generator=g), torch.randn(8, n, device=DEV, generator=g)
+    u = torch.empty(m, n, dtype=BF16, device=DEV)
+    for i in range(0, m, many):
+        u[i:i + many] = left[i:i + many] @ right + 0.1 * torch.randn(many, n, device=DEV, generator=g)
+    out = torch.full_like(u, math.nan)
+    plan = training.Orthogonalise(ctx, [u], [out])
+    plan.run(room(plan.workspace_bytes()), steps=1)
+    size = math.sqrt(sum(float((u[i:i + many].float() ** 2).sum(dtype=torch.float64)) for i in range(0, m, many)))
+    rows = torch.tensor([0, 1, 127, 128, 16383, 20001, m - 257, m - 1], device=DEV)
+    x = u[rows].float() / size
+
+    def squared(v):  # v X^T X
+        total = torch.zeros_like(v)
+        for i in range(0, m, many):
+            part = u[i:i + many].float() / size
+            total += (v @ part.t().contiguous()) @ part
+        return total
+
+    a, b, c = training.COEFFICIENTS
+    once = squared(x)
+    want = a * x + b * once + c * squared(once)
+    off = (out[rows].float() - want).norm(dim=1)
+    assert bool((off <= 2.0**-8 * want.norm(dim=1) + 5 * 2.0**-11 * (abs(b) + abs(c)) * x.norm(dim=1)).all()), off / want.norm(dim=1)
+    assert bool(torch.isfinite(out).all())
+    del u, out
+    torch.cuda.empty_cache()
