@@ -52,7 +52,7 @@ def test_spectra(ctx, kind, dtype):
     sr.check(direct(ctx, u), u, 1 if dtype == BF16 else 2)
 
 
-@pytest.mark.parametrize("count,rows,cols", [(16, 256, 1024), (1, 1024, 1024), (5, 700, 1300), (40, 264, 520)], ids=str)
+@pytest.mark.parametrize("count,rows,cols", [(16, 256, 1024), (1, 1024, 1024), (5, 700, 1300), (40, 264, 520), (16, 1024, 1030), (15, 1030, 900)], ids=str)
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_many_matrices(ctx, count, rows, cols, dtype):
     """enough tiles of 128 x 128 and of 256 x 256, split k axes, more than a launch's table; every matrix has the bits that it has in a call
