@@ -18,12 +18,15 @@ constexpr int64_t kMaxSide = 1 << 16;
 #endif
 
 // The polynomials keep singular values and entries where f16 holds them: the largest value that can stand at each step's end, on a grid
-// fine enough for a polynomial of degree five
-int check_series(const ckksmi_series &s) {
+// fine enough for a polynomial of degree five.  of_b: the power of two that takes the entries of b A + c A^2 near f16's end
+int check_series(const ckksmi_series &s, float *of_b = nullptr) {
+    double entries = 1.0;
     if (s.steps < 1 || s.steps > 32 || !(s.eps >= 0) || !std::isfinite(s.eps) || !std::isfinite(s.a) || !std::isfinite(s.b) || !std::isfinite(s.c)) return CKKSMI_EINVAL;
     double most = 1.0;
     for (int k = 0; k < s.steps; k++) {
-        if (!(std::fabs(s.b) * most * most + std::fabs(s.c) * most * most * most * most < 100.0)) return CKKSMI_EINVAL;
+        const double entry = std::fabs(s.b) * most * most + std::fabs(s.c) * most * most * most * most;
+        if (!(entry < 100.0)) return CKKSMI_EINVAL;
+        entries = std::max(entries, entry);
         double next = 0.0;
         for (int i = 0; i <= 1024; i++) {
             const double v = most * i / 1024.0, w = v * v;
@@ -32,6 +35,7 @@ int check_series(const ckksmi_series &s) {
         if (!(next < 2.0)) return CKKSMI_EINVAL;
         most = std::max(most, next);
     }
+    if (of_b) *of_b = (float)std::ldexp(1.0, (int)std::floor(std::log2(52000.0 / entries)));
     return CKKSMI_OK;
 }
 
@@ -46,10 +50,9 @@ struct SeriesTensor {
 
 // A tensor's sizes and its pieces of the workspace
 struct SeriesPlan {
-    int side, length, ld, ld_o, parts, blocks;
+    int side, length, ld, ld_o, blocks;
     size_t numel, per;
-    float S;
-    explicit SeriesPlan(const SeriesTensor &t, int parts_) : parts(parts_) {
+    explicit SeriesPlan(const SeriesTensor &t) {
         side = (int)std::min(t.rows, t.cols);
         length = (int)std::max(t.rows, t.cols);
         ld = (int)round_up(length, 8);
@@ -58,13 +61,11 @@ struct SeriesPlan {
         // the first pass: at most 1024 workgroups' sums, which every workgroup of the second adds up
         per = round_up((numel + 1023) / 1024, 4096);
         blocks = (int)((numel + per - 1) / per);
-        // a power of two near sqrt(numel), at most 2^14: S times a singular value below 2 stays in f16
-        S = (float)std::ldexp(1.0, std::min(14, (int)std::lround(0.5 * std::log2((double)numel))));
     }
     // everything in one workgroup's LDS
-    bool small() const { return side <= 64 && small_lds(side, length, parts) <= TS_SMALL_MOST; }
+    bool small() const { return side <= 64 && small_lds(side, length) <= TS_SMALL_MOST; }
     size_t x_bytes() const { return (size_t)side * ld * 4; }  // two parts of f16, or a direction in f32
-    size_t o_bytes() const { return (size_t)side * ld_o * 2 * parts; }
+    size_t o_bytes() const { return (size_t)side * ld_o * 4; }  // two parts
     // X and its successor, O, B, two diagonals, sums of squares
     size_t bytes() const {
         return 2 * round_up(x_bytes(), 256) + 2 * round_up(o_bytes(), 256) + 2 * round_up((size_t)side * 4, 256) + round_up((size_t)blocks * 8, 256);
@@ -141,37 +142,33 @@ template <int EPI> void launch_series(ckksmi_ctx *c, SeriesProblem *p, int n, ch
 }
 
 // A tensor's products of a step; pieces null: their sizes alone
-SeriesProblem series_problem(const SeriesPlan &t, const SeriesPieces &w, const ckksmi_series &s, int epi, int from, bool last) {
+SeriesProblem series_problem(const SeriesPlan &t, const SeriesPieces &w, const ckksmi_series &s, float of_b, int epi, int from, bool last) {
     SeriesProblem p;
     memset(&p, 0, sizeof(p));
     const size_t x_part = (size_t)t.side * t.ld * 2, o_part = (size_t)t.side * t.ld_o * 2;
     const char *a = epi == EPI_GRAM ? w.x[from] : epi == EPI_SQUARE ? w.o : w.b, *b = epi == EPI_SQUARE ? w.o : w.x[from];
     const size_t a_part = epi == EPI_GRAM ? x_part : o_part, b_part = epi == EPI_SQUARE ? o_part : x_part;
-    p.nsrc = t.parts > 1 ? 3 : 1;
-    for (int i = 0; i < p.nsrc; i++) {  // upper times upper, upper times lower, lower times upper
-        p.a[i] = a + (i == 2 ? a_part : 0);
-        p.b[i] = b + (i == 1 ? b_part : 0);
+    p.nsrc = 3;
+    for (int i = 0; i < 3; i++) {  // upper times lower, lower times upper, upper times upper
+        p.a[i] = a + (i == 1 ? a_part : 0);
+        p.b[i] = b + (i == 0 ? b_part : 0);
     }
     p.lda = (epi == EPI_GRAM ? t.ld : t.ld_o) * 2;
     p.ldb = (epi == EPI_SQUARE ? t.ld_o : t.ld) * 2;
     p.M = t.side;
     p.N = epi == EPI_APPLY ? t.length : t.side;
     p.K = epi == EPI_GRAM ? t.length : t.side;
-    p.parts = t.parts;
-    p.ca = (float)s.a; p.cb = (float)s.b; p.cc = (float)s.c;
-    p.o_apart = p.in_apart = (epi == EPI_APPLY ? x_part : o_part) / 2;
+    p.ca = (float)s.a; p.cb = (float)s.b; p.cc = (float)s.c; p.of_b = of_b;
+    p.apart = (epi == EPI_APPLY ? x_part : o_part) / 2;
     p.ldo = epi == EPI_APPLY ? t.ld : t.ld_o;
     if (epi == EPI_GRAM) {
-        p.o = (_Float16 *)w.o; p.diag_out = w.d; p.scale = TS_SCALE / (t.S * t.S);
+        p.o = (_Float16 *)w.o; p.diag_out = w.d;
     } else if (epi == EPI_SQUARE) {
         p.o = (_Float16 *)w.b; p.in = (const _Float16 *)w.o; p.diag = w.d; p.diag_out = w.e;
     } else {
         p.in = (const _Float16 *)w.x[from]; p.diag = w.e;
-        if (last) {
-            p.last = (float *)w.x[1 - from];
-            p.scale = 1.0f / t.S;
-        } else
-            p.o = (_Float16 *)w.x[1 - from];
+        if (last) p.last = (float *)w.x[1 - from];
+        else p.o = (_Float16 *)w.x[1 - from];
     }
     return p;
 }
@@ -185,7 +182,7 @@ size_t series_workspace(const std::vector<SeriesPlan> &plans, const ckksmi_serie
         const int n = (int)std::min<size_t>(TS_PROBLEMS, plans.size() - i);
         for (int epi : {EPI_GRAM, EPI_SQUARE, EPI_APPLY}) {
             SeriesProblem p[TS_PROBLEMS];
-            for (int k = 0; k < n; k++) p[k] = series_problem(plans[i + k], none, s, epi, 0, false);
+            for (int k = 0; k < n; k++) p[k] = series_problem(plans[i + k], none, s, 1.0f, epi, 0, false);
             const int splits = series_choose(p, n, symmetric(epi)).splits;
             size_t need = 0;
             for (int k = 0; k < n; k++) need += series_part_bytes(p[k], splits);
@@ -200,12 +197,14 @@ struct SeriesCall {
     std::vector<SeriesTensor> t;
     std::vector<SeriesPlan> plan;
     size_t need;
+    float of_b = 1.0f;
     bool small = true;  // all of them are
-    SeriesCall(std::vector<SeriesTensor> tensors, int parts, const ckksmi_series &s) {
+    SeriesCall(std::vector<SeriesTensor> tensors, const ckksmi_series &s) {
+        (void)check_series(s, &of_b);  // (it has passed)
         for (const SeriesTensor &x : tensors)
             if (x.rows && x.cols) {
                 t.push_back(x);
-                plan.emplace_back(x, parts);
+                plan.emplace_back(x);
                 small = small && plan.back().small();
             }
         need = small ? 0 : series_workspace(plan, s);
@@ -227,8 +226,8 @@ template <class Blocks, class Launch> void for_tables(const SeriesCall &call, co
             if (!call.small) {
                 t.sums = w[i].sums; t.x = (_Float16 *)w[i].x[0]; t.o = (_Float16 *)w[i].o; t.b = (_Float16 *)w[i].b; t.direction = (const float *)w[i].x[direction];
             }
-            t.numel = (int64_t)l.numel; t.per = (int64_t)l.per; t.rows = (int)s.rows; t.cols = (int)s.cols; t.ld = l.ld; t.ld_o = l.ld_o; t.parts = l.parts;
-            t.S = l.S; t.scale = (float)s.scale; t.blocks = l.blocks;
+            t.numel = (int64_t)l.numel; t.per = (int64_t)l.per; t.rows = (int)s.rows; t.cols = (int)s.cols; t.ld = l.ld; t.ld_o = l.ld_o;
+            t.scale = (float)s.scale; t.blocks = l.blocks;
             A.first[A.n++] = (unsigned)blocks;
             blocks += more;
             i++;
@@ -240,10 +239,9 @@ template <class Blocks, class Launch> void for_tables(const SeriesCall &call, co
 inline int64_t series_squares(const SeriesPlan &l) { return (int64_t)((l.side + 63) / 64) * ((l.ld + 63) / 64); }
 
 template <class P, class G, bool MOVE> void run_small(ckksmi_ctx *c, const SeriesCall &call, const ckksmi_series &s, const PassArgs &A, hipStream_t st) {
-    const SmallSeries S{s.steps, (float)s.a, (float)s.b, (float)s.c};
+    const SmallSeries S{s.steps, (float)s.a, (float)s.b, (float)s.c, call.of_b};
     for_tables(call, {}, A, 0, [](const SeriesPlan &) { return (int64_t)1; }, [&](const PassArgs &a, unsigned blocks) {
-        if (call.plan[0].parts > 1) KL(c, CKKSMI_K_SERIES, blocks, (series_small_kernel<P, G, MOVE, 2>), dim3(blocks), dim3(TS_SMALL_THREADS), st, a, S);
-        else KL(c, CKKSMI_K_SERIES, blocks, (series_small_kernel<P, G, MOVE, 1>), dim3(blocks), dim3(TS_SMALL_THREADS), st, a, S);
+        KL(c, CKKSMI_K_SERIES, blocks, (series_small_kernel<P, G, MOVE>), dim3(blocks), dim3(TS_SMALL_THREADS), st, a, S);
     });
 }
 template <class P, bool MOVE> void run_series(ckksmi_ctx *c, const SeriesCall &call, const ckksmi_series &s, const PassArgs &A, void *ws, hipStream_t st) {
@@ -285,7 +283,7 @@ template <class P, bool MOVE> void run_series(ckksmi_ctx *c, const SeriesCall &c
             const int n = (int)std::min<size_t>(TS_PROBLEMS, w.size() - i);
             SeriesProblem p[TS_PROBLEMS];
             auto all = [&](int epi) {
-                for (int j = 0; j < n; j++) p[j] = series_problem(call.plan[i + j], w[i + j], s, epi, k & 1, k + 1 == s.steps);
+                for (int j = 0; j < n; j++) p[j] = series_problem(call.plan[i + j], w[i + j], s, call.of_b, epi, k & 1, k + 1 == s.steps);
             };
             all(EPI_GRAM);
             launch_series<EPI_GRAM>(c, p, n, part, st);
@@ -300,11 +298,6 @@ template <class P, bool MOVE> void run_series(ckksmi_ctx *c, const SeriesCall &c
 }
 
 int check_sizes(int64_t rows, int64_t cols) { return rows < 0 || cols < 0 || rows > kMaxSide || cols > kMaxSide ? CKKSMI_EINVAL : CKKSMI_OK; }
-
-// Directions that end in bf16 are formed from upper parts alone: 6e-4 of the direction's size off, where bf16 rounds by 4e-3
-inline int parts_of_direction(int dtype) { return dtype == CKKSMI_BF16 ? 1 : 2; }
-// ... and so are those that move 16-bit parameters: a step is a small part of them, 6e-4 of it less than their last place (4e-3, 5e-4 of them)
-inline int parts_of_step(int p_dtype) { return p_dtype == CKKSMI_F32 ? 2 : 1; }
 
 int directions_call(const ckksmi_series *s, const ckksmi_direction *t, int n, int dtype, ckksmi_series &series, std::vector<SeriesTensor> &out) {
     if (!s || n < 0 || (!t && n) || !dtype_ok(dtype)) return CKKSMI_EINVAL;
@@ -354,7 +347,7 @@ extern "C" int ckksmi_orthogonalise_workspace_bytes(const ckksmi_ctx *c, const c
         ckksmi_series series;
         std::vector<SeriesTensor> tensors;
         const int rc = directions_call(s, t, n, dtype, series, tensors);
-        if (!rc) *bytes = SeriesCall(tensors, parts_of_direction(dtype), series).need;
+        if (!rc) *bytes = SeriesCall(tensors, series).need;
         return rc;
     });
 }
@@ -366,7 +359,7 @@ extern "C" int ckksmi_orthogonalise(ckksmi_ctx *c, const ckksmi_series *s, const
         std::vector<SeriesTensor> tensors;
         const int rc = directions_call(s, t, n, dtype, series, tensors);
         if (rc) return rc;
-        const SeriesCall call(tensors, parts_of_direction(dtype), series);
+        const SeriesCall call(tensors, series);
         if (call.t.empty()) return CKKSMI_OK;
         for (const SeriesTensor &x : call.t)
             if (!x.p || !x.g || !aligned(x.p, element_bytes(dtype)) || !aligned(x.g, element_bytes(dtype))) return CKKSMI_EINVAL;
@@ -396,7 +389,7 @@ extern "C" int ckksmi_muon_workspace_bytes(const ckksmi_ctx *c, const ckksmi_muo
         std::vector<SeriesTensor> tensors;
         bool copies;
         const int rc = muon_call(opt, t, n, o, tensors, copies);
-        if (!rc) *bytes = SeriesCall(tensors, parts_of_step(o.p_dtype), o.series).need;
+        if (!rc) *bytes = SeriesCall(tensors, o.series).need;
         return rc;
     });
 }
@@ -409,7 +402,7 @@ extern "C" int ckksmi_muon_step(ckksmi_ctx *c, const ckksmi_muon *opt, const ckk
         bool copies;
         const int rc = muon_call(opt, t, n, o, tensors, copies);
         if (rc) return rc;
-        const SeriesCall call(tensors, parts_of_step(o.p_dtype), o.series);
+        const SeriesCall call(tensors, o.series);
         if (call.t.empty()) return CKKSMI_OK;
         const size_t ps = element_bytes(o.p_dtype), gs = element_bytes(o.grad_dtype);
         for (const SeriesTensor &x : call.t)

@@ -1,21 +1,22 @@
 // Directions of matrices by a polynomial of their singular values: X <- a X + (b A + c A^2) X, A = X X^T, some steps from X = u / |u|.
 //
-// A tensor is held as m x n with m <= n (transposed where it has more rows than columns): X in two f16 parts, H + L = S x with S a power of
-// two near sqrt(m n), so that elements of the usual size 1 / sqrt(m n) are near one: their two parts have 22 bits, and S times the
-// largest singular value stays inside f16.  A = D + O and the polynomial B = b A + c A^2 are held as their diagonals in f32 and the
-// rest in f16 (256 times the value), because the diagonals are the large part and what is rounded there changes whole rows:
+// A tensor is held as m x n with m <= n (transposed where it has more rows than columns): X in two f16 parts, H + L = 2^14 x, 22 bits of elements near
+// |X|, which is near one.  A = D + O and the polynomial B = b A + c A^2 are held as their diagonals in f32 and the rest in
+// two f16 parts likewise (2^13 times the value, and as B allows), because the diagonals are the large part and what is rounded there
+// changes whole rows:
 //     A^2 outside the diagonal = (d_i + d_j) O_ij + (O O)_ij,     row i of the new X = (a + B_ii) X_i + (rest of B) X.
-// The products take f16 on the matrix cores (train_gemm.h's tiles).  PARTS == 1: the upper parts alone, O and B's rest in one part; X itself keeps
-// both through the sum, so rounding errors do not grow from step to step: 4e-4 - 9e-4 of the direction's size for gradients of any
-// spectrum (X in one part: up to 4e-2 on matrices of low rank).  PARTS == 2: H H + H L + L H of two parts each, 22 bits: 1e-7 - 7e-6,
-// less than sums in f32 add.  Symmetric products form the tiles that reach the diagonal from below and store their results twice.
+// The products take f16 on the matrix cores (train_gemm.h's tiles): H H + H L + L H; L L is left out, 2^-22 of the
+// result at most.  One part alone in any of the products is not enough, not even for bf16 results: what it
+// rounds off adds up over the steps to 4e-3 of the direction for matrices of low rank and to 4e-2 for exact rank one.
+// Symmetric products form the tiles that reach the diagonal from below and store their results twice.
 // Bound by the matrix cores for large matrices and by launches (three a step) for small ones.  One 4096 x 4096, bf16: a step's products 106
 // (X X^T), 127 (square), 129 us (1.06 PFLOP/s); twelve of 1024 x 4096, f32, three products each: 214, 79, 316 us (0.98 PFLOP/s); two of
 // 256 x 3136: 11, 13, 13 us and 6 of a join.  Passes over the elements: 4096 x 4096 13, 24, 18 us
 #pragma once
 #include "train_gemm.h"
 
-#define TS_SCALE 256.0f  // of O and of B's rest
+#define TS_X 16384.0f       // of X: its singular values are below 2
+#define TS_O 8192.0f        // of O, whose elements are below 4
 
 struct SeriesProblem {
     const char *a[3], *b[3];
@@ -26,14 +27,13 @@ struct SeriesProblem {
     // epilogues
     _Float16 *o;           // GRAM: O; SQUARE: B's rest; APPLY: the new X
     const _Float16 *in;    // SQUARE: O; APPLY: X
-    size_t o_apart, in_apart;  // elements from the first part to the second
+    size_t apart;          // elements from the first part of o and of in to the second
     size_t ldo;            // elements, of o and in
     const float *diag;     // SQUARE: d; APPLY: a + B_ii
     float *diag_out;       // GRAM: d; SQUARE: a + B_ii
     float *last;           // APPLY: null, or the direction in f32 instead of o
-    float scale;           // GRAM: TS_SCALE / S^2; APPLY, last: 1 / S
-    int parts;             // of o (GRAM, SQUARE)
     float ca, cb, cc;      // a, b, c
+    float of_b;            // scale of B's rest: the largest power of two that keeps it inside f16
 };
 
 #define TS_PROBLEMS 16
@@ -49,14 +49,12 @@ __device__ __forceinline__ void split16(float x, _Float16 &h, _Float16 &l) {
     h = (_Float16)x;
     l = (_Float16)(x - (float)h);
 }
-__device__ __forceinline__ void load_parts(const _Float16 *p, size_t apart, int parts, float (&x)[8]) {
+__device__ __forceinline__ void load_two(const _Float16 *p, size_t apart, float (&x)[8]) {
+    float l[8];
     load_oct(p, x);
-    if (parts > 1) {
-        float l[8];
-        load_oct(p + apart, l);
+    load_oct(p + apart, l);
 #pragma unroll
-        for (int e = 0; e < 8; e++) x[e] += l[e];
-    }
+    for (int e = 0; e < 8; e++) x[e] += l[e];
 }
 __device__ __forceinline__ void store_two(_Float16 *p, size_t apart, const float (&x)[8]) {
     float l[8];
@@ -69,10 +67,7 @@ __device__ __forceinline__ void store_two(_Float16 *p, size_t apart, const float
 // 8 columns of row m from n <= m on of a symmetric matrix without its diagonal: stored there and as a column
 __device__ __forceinline__ void store_symmetric(const SeriesProblem &P, size_t m, int n, const float (&x)[8]) {
     _Float16 *row = P.o + m * P.ldo + n;
-    if (n + 8 <= (int)m) {
-        if (P.parts > 1) store_two(row, P.o_apart, x);
-        else store_oct(row, x);
-    }
+    if (n + 8 <= (int)m) store_two(row, P.apart, x);
 #pragma unroll
     for (int e = 0; e < 8; e++) {
         if (n + e > (int)m) continue;
@@ -80,10 +75,10 @@ __device__ __forceinline__ void store_symmetric(const SeriesProblem &P, size_t m
         split16(n + e < (int)m ? x[e] : 0.0f, h, l);
         _Float16 *column = P.o + (size_t)(n + e) * P.ldo + m;
         *column = h;
-        if (P.parts > 1) column[P.o_apart] = l;
+        column[P.apart] = l;
         if (n + 8 > (int)m) {
             row[e] = h;
-            if (P.parts > 1) row[P.o_apart + e] = l;
+            row[P.apart + e] = l;
         }
     }
 }
@@ -92,8 +87,8 @@ template <> struct SeriesEpilogue<EPI_GRAM> {
     static __device__ __forceinline__ void eight(const SeriesProblem &P, size_t m, int n, float (&v)[8]) {
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            v[e] *= P.scale;
-            if (n + e == (int)m) P.diag_out[m] = v[e] * (1.0f / TS_SCALE);
+            v[e] *= TS_O / (TS_X * TS_X);
+            if (n + e == (int)m) P.diag_out[m] = v[e] * (1.0f / TS_O);
         }
         store_symmetric(P, m, n, v);
     }
@@ -101,14 +96,14 @@ template <> struct SeriesEpilogue<EPI_GRAM> {
 template <> struct SeriesEpilogue<EPI_SQUARE> {
     static __device__ __forceinline__ void eight(const SeriesProblem &P, size_t m, int n, float (&v)[8]) {
         float o[8];
-        load_parts(P.in + m * P.ldo + n, P.in_apart, P.parts, o);
+        load_two(P.in + m * P.ldo + n, P.apart, o);
         const float d = P.diag[m];
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             if (n + e > (int)m) continue;
-            const float square = v[e] * (1.0f / TS_SCALE);
-            if (n + e == (int)m) P.diag_out[m] = P.ca + P.cb * d + P.cc * (d * d + square * (1.0f / TS_SCALE));
-            v[e] = P.cb * o[e] + P.cc * ((d + P.diag[n + e]) * o[e] + square);
+            const float square = v[e] * (1.0f / TS_O);
+            if (n + e == (int)m) P.diag_out[m] = P.ca + P.cb * d + P.cc * (d * d + square * (1.0f / TS_O));
+            v[e] = (P.cb * o[e] + P.cc * ((d + P.diag[n + e]) * o[e] + square)) * (P.of_b / TS_O);
         }
         store_symmetric(P, m, n, v);
     }
@@ -117,16 +112,16 @@ template <> struct SeriesEpilogue<EPI_APPLY> {
     static __device__ __forceinline__ void eight(const SeriesProblem &P, size_t m, int n, float (&v)[8]) {
         float x[8];
         const size_t at = m * P.ldo + n;
-        load_parts(P.in + at, P.in_apart, 2, x);
-        const float d = P.diag[m];
+        load_two(P.in + at, P.apart, x);
+        const float d = P.diag[m], by = 1.0f / P.of_b;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-            x[e] = d * x[e] + v[e] * (1.0f / TS_SCALE);
-            if (P.last) x[e] *= P.scale;
+            x[e] = d * x[e] + v[e] * by;
+            if (P.last) x[e] *= 1.0f / TS_X;
             if (n + e >= P.N) x[e] = 0.0f;  // what pads a row stays zeros
         }
         if (P.last) store_oct(P.last + at, x);
-        else store_two(P.o + at, P.o_apart, x);
+        else store_two(P.o + at, P.apart, x);
     }
 };
 
@@ -163,11 +158,11 @@ struct PassTensor {
     char *copy;
     double *sums;          // of squares, one a workgroup of the first pass
     _Float16 *x;           // two parts of [side][ld]
-    _Float16 *o, *b;       // [parts][side][ld_o]: their padding is set to zeros
+    _Float16 *o, *b;       // two parts of [side][ld_o]: their padding is set to zeros
     const float *direction;  // [side][ld]
     int64_t numel, per;    // per: elements of a workgroup of the first pass
-    int rows, cols, ld, ld_o, parts;
-    float S, scale;        // scale: lr times the tensor's
+    int rows, cols, ld, ld_o;
+    float scale;           // lr times the tensor's
     int blocks;            // workgroups of the first pass
 };
 #define TS_TENSORS 24
@@ -205,9 +200,9 @@ struct Unit {
     }
     __device__ __forceinline__ float of(float u) const { return ldexpf(u, exponent) * rest; }
 };
-__device__ __forceinline__ double series_inverse(const PassArgs &A, const PassTensor &t, double squares) {
+__device__ __forceinline__ double series_inverse(const PassArgs &A, double squares) {
     const double size = sqrt(squares) + A.eps;
-    return size < 1e-300 ? 0.0 : (double)t.S / size;  // (f32 numbers that are not all zeros are larger)
+    return size < 1e-300 ? 0.0 : (double)TS_X / size;  // (f32 numbers that are not all zeros are larger)
 }
 // 64-bit sum over the workgroup
 template <int THREADS> __device__ __forceinline__ double block_sum(double x, double (&sums)[THREADS]) {
@@ -312,7 +307,7 @@ template <class G> __global__ void __launch_bounds__(256) series_begin_kernel(Pa
     }
     double sum = 0.0;
     for (int b = threadIdx.x; b < t.blocks; b += 256) sum += t.sums[b];
-    const Unit unit(series_inverse(A, t, block_sum<256>(sum, sums)));
+    const Unit unit(series_inverse(A, block_sum<256>(sum, sums)));
 #pragma unroll
     for (int k = 0; k < 4; k++)
 #pragma unroll
@@ -336,7 +331,7 @@ template <class G> __global__ void __launch_bounds__(256) series_begin_kernel(Pa
     }
     // the tensor's first tiles of a row clear what pads the symmetric matrices' rows
     if (l0 == 0 && t.ld_o > q.side)
-        for (int k = threadIdx.x; k < 64 * t.parts; k += 256) {
+        for (int k = threadIdx.x; k < 64 * 2; k += 256) {
             const int row = s0 + k % 64;
             if (row >= q.side) continue;
             for (int col = q.side; col < t.ld_o; col++) {
@@ -399,13 +394,13 @@ template <class P, bool MOVE> __global__ void __launch_bounds__(256) series_end_
 // launches: 132)
 #define TS_SMALL_LDS 151552
 #define TS_SMALL_THREADS 1024
-struct SmallSeries { int steps; float ca, cb, cc; };
+struct SmallSeries { int steps; float ca, cb, cc, of_b; };
 __host__ __device__ __forceinline__ int small_ld(int n) { return (n + 31) / 32 * 32 + 8; }
-inline size_t small_lds(int side, int length, int parts) {
+inline size_t small_lds(int side, int length) {
     const size_t M = (side + 15) / 16 * 16, rows = (side + 31) / 32 * 32;
-    return 4 * (rows * small_ld(length) + parts * M * small_ld((int)M));
+    return 4 * (rows * small_ld(length) + 2 * M * small_ld((int)M));
 }
-template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bounds__(TS_SMALL_THREADS) series_small_kernel(PassArgs A, SmallSeries S) {
+template <class P, class G, bool MOVE> __global__ void __launch_bounds__(TS_SMALL_THREADS) series_small_kernel(PassArgs A, SmallSeries S) {
     if (A.skip && *A.skip) return;
     const PassTensor &t = A.t[blockIdx.x];
     __shared__ __attribute__((aligned(1024))) char lds[TS_SMALL_LDS];
@@ -415,10 +410,10 @@ template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bound
     const bool tall = t.rows > t.cols;
     const int side = tall ? t.cols : t.rows, length = tall ? t.rows : t.cols, tiles = (side + 15) / 16, M = 16 * tiles, ld = small_ld(length), ld_o = small_ld(M);
     const int x_apart = (M + 31) / 32 * 32 * ld, o_apart = M * ld_o;
-    _Float16 *const X = (_Float16 *)lds, *const O = X + 2 * x_apart, *const B = O + PARTS * o_apart;  // parts one behind the other
+    _Float16 *const X = (_Float16 *)lds, *const O = X + 2 * x_apart, *const B = O + 2 * o_apart;  // parts one behind the other
     const int lane = threadIdx.x & 63, wave = TG_UNIFORM((int)(threadIdx.x >> 6)), i = lane & 15, q = lane >> 4;
     constexpr int WAVES = TS_SMALL_THREADS / 64;
-    for (int k = threadIdx.x; k < 2 * (x_apart + PARTS * o_apart) / 8; k += TS_SMALL_THREADS) ((u32x4 *)lds)[k] = u32x4{0, 0, 0, 0};
+    for (int k = threadIdx.x; k < 2 * (x_apart + 2 * o_apart) / 8; k += TS_SMALL_THREADS) ((u32x4 *)lds)[k] = u32x4{0, 0, 0, 0};
     __syncthreads();
     // u, held as its word's halves where X's parts will be; momentum and size.  Eight elements of a thread are requested together
     const G *g = (const G *)t.g;
@@ -451,7 +446,7 @@ template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bound
             ((uint16_t *)X)[x_apart + at] = (uint16_t)word;
         }
     }
-    const Unit unit(series_inverse(A, t, block_sum<TS_SMALL_THREADS>(sum, sums)));
+    const Unit unit(series_inverse(A, block_sum<TS_SMALL_THREADS>(sum, sums)));
     for (int k = threadIdx.x; k < numel; k += TS_SMALL_THREADS) {
         const int at = place(k);
         const float u = __uint_as_float((unsigned)((uint16_t *)X)[at] << 16 | ((uint16_t *)X)[x_apart + at]);
@@ -468,18 +463,22 @@ template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bound
         __builtin_memcpy(&f, h, 16);
         return f;
     };
+    // sums of H H and of H L + L H
+    auto with_low = [](f32x4 acc, f32x4 low) {
+#pragma unroll
+        for (int k = 0; k < 4; k++) acc[k] += low[k];
+        return acc;
+    };
     // 16 x 16 results of a symmetric product of rows along k: lane l has row l % 16, columns 4 (l / 16) .. + 3
     auto symmetric_tile = [&](const _Float16 *p, int apart, int stride, int row, int col, int K) {
-        f32x4 acc = {0, 0, 0, 0};
+        f32x4 acc = {0, 0, 0, 0}, low = {0, 0, 0, 0};
         for (int k = 0; k < K; k += 32) {
             const u32x4 a = fragment(p, col, stride, k), b = fragment(p, row, stride, k);
             acc = mma<_Float16>(a, b, acc);
-            if constexpr (PARTS > 1) {
-                acc = mma<_Float16>(a, fragment(p + apart, row, stride, k), acc);
-                acc = mma<_Float16>(fragment(p + apart, col, stride, k), b, acc);
-            }
+            low = mma<_Float16>(a, fragment(p + apart, row, stride, k), low);
+            low = mma<_Float16>(fragment(p + apart, col, stride, k), b, low);
         }
-        return acc;
+        return with_low(acc, low);
     };
     // four neighbouring columns of a row of a symmetric matrix, and as a column; those that reach the diagonal one by one
     auto put = [&](_Float16 *p, int row, int col, const float (&x)[4]) {
@@ -489,15 +488,15 @@ template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bound
             split16(x[k], h[k], l[k]);
             if (col + k >= row) continue;
             p[(col + k) * ld_o + row] = h[k];
-            if (PARTS > 1) p[o_apart + (col + k) * ld_o + row] = l[k];
+            p[o_apart + (col + k) * ld_o + row] = l[k];
             if (col + 3 >= row) {
                 p[row * ld_o + col + k] = h[k];
-                if (PARTS > 1) p[o_apart + row * ld_o + col + k] = l[k];
+                p[o_apart + row * ld_o + col + k] = l[k];
             }
         }
         if (col + 3 < row) {
             __builtin_memcpy(__builtin_assume_aligned(p + row * ld_o + col, 8), h, 8);
-            if (PARTS > 1) __builtin_memcpy(__builtin_assume_aligned(p + o_apart + row * ld_o + col, 8), l, 8);
+            __builtin_memcpy(__builtin_assume_aligned(p + o_apart + row * ld_o + col, 8), l, 8);
         }
     };
     auto four = [&](const _Float16 *p, int apart, float (&x)[4]) {
@@ -505,10 +504,10 @@ template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bound
         __builtin_memcpy(h, __builtin_assume_aligned(p, 8), 8);
         __builtin_memcpy(l, __builtin_assume_aligned(p + apart, 8), 8);
 #pragma unroll
-        for (int k = 0; k < 4; k++) x[k] = apart ? (float)h[k] + (float)l[k] : (float)h[k];
+        for (int k = 0; k < 4; k++) x[k] = (float)h[k] + (float)l[k];
     };
-    const float gram = TS_SCALE / (t.S * t.S);
     const int pairs = tiles * (tiles + 1) / 2, columns = (length + 15) / 16;
+    const float by = 1.0f / S.of_b;
     for (int s = 0; s < S.steps; s++) {
         __syncthreads();
         for (int p = wave; p < pairs; p += WAVES) {
@@ -519,8 +518,8 @@ template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bound
             float x[4];
 #pragma unroll
             for (int k = 0; k < 4; k++) {
-                x[k] = v[k] * gram;
-                if (n + k == m) d[m] = x[k] * (1.0f / TS_SCALE);
+                x[k] = v[k] * (TS_O / (TS_X * TS_X));
+                if (n + k == m) d[m] = x[k] * (1.0f / TS_O);
             }
             put(O, m, n, x);
         }
@@ -532,12 +531,12 @@ template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bound
             const int m = 16 * row + i, n = 16 * col + 4 * q;
             const float dm = d[m];
             float o[4];
-            four(O + m * ld_o + n, PARTS > 1 ? o_apart : 0, o);
+            four(O + m * ld_o + n, o_apart, o);
 #pragma unroll
             for (int k = 0; k < 4; k++) {
-                const float square = v[k] * (1.0f / TS_SCALE);
-                if (n + k == m) e[m] = S.ca + S.cb * dm + S.cc * (dm * dm + square * (1.0f / TS_SCALE));
-                o[k] = S.cb * o[k] + S.cc * ((dm + d[n + k]) * o[k] + square);
+                const float square = v[k] * (1.0f / TS_O);
+                if (n + k == m) e[m] = S.ca + S.cb * dm + S.cc * (dm * dm + square * (1.0f / TS_O));
+                o[k] = (S.cb * o[k] + S.cc * ((dm + d[n + k]) * o[k] + square)) * (S.of_b / TS_O);
             }
             put(B, m, n, o);
         }
@@ -548,23 +547,23 @@ template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bound
             for (int k = 0; k < 2; k++)
                 if (32 * k < M) {
                     x[k][0] = column(X, 16 * c, 32 * k);
-                    if (PARTS > 1) x[k][1] = column(X + x_apart, 16 * c, 32 * k);
+                    x[k][1] = column(X + x_apart, 16 * c, 32 * k);
                 }
             f32x4 acc[4];
 #pragma unroll
             for (int r = 0; r < 4; r++) {
-                acc[r] = f32x4{0, 0, 0, 0};
+                f32x4 low = {0, 0, 0, 0};
+                acc[r] = low;
                 if (r >= tiles) continue;
 #pragma unroll
                 for (int k = 0; k < 2; k++)
                     if (32 * k < M) {
                         const u32x4 b = fragment(B, 16 * r, ld_o, 32 * k);
                         acc[r] = mma<_Float16>(x[k][0], b, acc[r]);
-                        if constexpr (PARTS > 1) {
-                            acc[r] = mma<_Float16>(x[k][1], b, acc[r]);
-                            acc[r] = mma<_Float16>(x[k][0], fragment(B + o_apart, 16 * r, ld_o, 32 * k), acc[r]);
-                        }
+                        low = mma<_Float16>(x[k][1], b, low);
+                        low = mma<_Float16>(x[k][0], fragment(B + o_apart, 16 * r, ld_o, 32 * k), low);
                     }
+                acc[r] = with_low(acc[r], low);
             }
 #pragma unroll
             for (int r = 0; r < 4; r++) {
@@ -576,14 +575,14 @@ template <class P, class G, bool MOVE, int PARTS> __global__ void __launch_bound
                 four(at, x_apart, old);
                 _Float16 h[4], l[4];
 #pragma unroll
-                for (int k = 0; k < 4; k++) split16(em * old[k] + acc[r][k] * (1.0f / TS_SCALE), h[k], l[k]);
+                for (int k = 0; k < 4; k++) split16(em * old[k] + acc[r][k] * by, h[k], l[k]);
                 __builtin_memcpy(__builtin_assume_aligned(at, 8), h, 8);
                 __builtin_memcpy(__builtin_assume_aligned(at + x_apart, 8), l, 8);
             }
         }
     }
     __syncthreads();
-    const float size = 1.0f / t.S;
+    const float size = 1.0f / TS_X;
     for (int first = threadIdx.x; first < numel; first += 8 * TS_SMALL_THREADS) {
         float p[8];
         if (MOVE)
