@@ -148,9 +148,10 @@ int ckksmi_adamw_read_states(ckksmi_ctx *ctx, const ckksmi_adamw_tensor *tensors
  *     X = u / (|u| + eps)   (|u|: root of the sum of squares),   then `steps` times   X <- a X + (b A + c A^2) X,  A = X X^T
  * (on u^T where rows > cols): the odd polynomial a s + b s^3 + c s^5 applied to u's singular values s, which the steps drive towards one.
  * The polynomials must keep singular values from [0, 1] below 2, and |b| s^2 + |c| s^4 below 100, at every step (CKKSMI_EINVAL).  u = 0 has direction 0.
- * Rounding errors of X grow by up to a^steps in directions that u is weak in, as they would in any arithmetic.  X is held in two f16 parts
- * (22 bits), the diagonals of A and of the polynomial in f32; every product is three products of the parts, whatever type the
- * direction ends in.  Any finite u; an infinity or NaN makes the direction NaN (and 0).
+ * Rounding errors of X grow by up to a^steps in directions that u is weak in, as they would in any arithmetic.  X is held in two f16 parts:
+ * an element to 2^-22 of itself or to 2^-50 (|X| is near one), whichever is more, so rows or columns that are weaker than 1e-6 of an element of usual
+ * size have fewer bits than f32 would give them.  The diagonals of A and of the polynomial are held in f32; every product is three
+ * products of the parts, whatever type the direction ends in.  Any finite u; an infinity or NaN makes the direction NaN (and 0).
  * Sizes 0 .. 2^16 each (a matrix without elements is left out); numbers of any type are contiguous.  A tensor's results depend on its own
  * numbers and on the sizes in the call alone. */
 typedef struct {

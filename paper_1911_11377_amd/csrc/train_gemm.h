@@ -364,6 +364,11 @@ struct TileWalk {
         step = s0 + group;
         enter();
     }
+    // own steps before the last source's (EPI_GRAM and on: what they add up is taken times 1 / TS_LOW when that begins)
+    __device__ __forceinline__ int before_last(int group) const {
+        const int left = per_src * (P->nsrc - 1) - s0 - group;
+        return left > 0 ? (left + EVERY - 1) / EVERY : 0;
+    }
     __device__ __forceinline__ void enter() {
         while (step >= per_src && src + 1 < P->nsrc) {
             step -= per_src;
@@ -398,6 +403,15 @@ struct TileWalk {
 };
 
 template <int EPI> struct SeriesEpilogue;  // (train_series.h)
+#define TS_LOW 2048.0f                     // its second parts are held this much larger
+template <int FM, int N> __device__ __forceinline__ void scale_low(f32x4 (&acc)[FM][N]) {
+#pragma unroll
+    for (int i = 0; i < FM; i++)
+#pragma unroll
+        for (int j = 0; j < N; j++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) acc[i][j][k] *= 1.0f / TS_LOW;
+}
 
 // A wave's results to memory, 8 neighbouring columns at a time
 template <class T, int EPI, int FM, int PAIRS, int WN, class Args>
@@ -542,7 +556,9 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) gemm_kernel(Arg
     read_first(0);
     int other = STAGE;  // from the stage at hand to the other one
     LdsAddress stage = lds;
+    const int low = EPI >= EPI_GRAM ? w.before_last(0) : 0;
     for (int t = 0; t < n; t++) {
+        if (EPI >= EPI_GRAM && t == low) scale_low(acc);
         read_second(0);
         multiply(0, 0, 0, 0, 0);
         read_first(1);
@@ -559,6 +575,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) gemm_kernel(Arg
         other = -other;
     }
     wait_loads<0>();
+    if (EPI >= EPI_GRAM && low >= n) scale_low(acc);
     write_tile<T, EPI, FM, PAIRS, WN>(G, *w.P, w.m0 + wm, w.n0, wn, lane, acc);
 }
 
@@ -603,17 +620,21 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN) * KG) gemm_small_ke
         }
     };
     const int rounds = (w.s1 - w.s0 + KG - 1) / KG, own = (w.s1 - w.s0 - group + KG - 1) / KG;  // of the workgroup, of this group
+    const int low = EPI >= EPI_GRAM ? w.before_last(group) : 0;
     if (own > 0) w.issue_all(lds_address(stage0));
     for (int r = 0; r < rounds; r += 2) {
         tile_barrier();
         if (r + 1 < own) w.issue_all(lds_address(stage1));
+        if (EPI >= EPI_GRAM && r == low) scale_low(acc);
         if (r < own) multiply(stage0);
         if (r + 1 < rounds) {
             tile_barrier();
             if (r + 2 < own) w.issue_all(lds_address(stage0));
+            if (EPI >= EPI_GRAM && r + 1 == low) scale_low(acc);
             if (r + 1 < own) multiply(stage1);
         }
     }
+    if (EPI >= EPI_GRAM && low >= rounds) scale_low(acc);
     if constexpr (KG > 1) {
         static_assert((KG - 1) * BM * BN * 4 <= KG * 2 * STAGE, "the other groups' sums fit the stages");
         f32x4 *sums = (f32x4 *)stages;

@@ -1,12 +1,14 @@
 // Directions of matrices by a polynomial of their singular values: X <- a X + (b A + c A^2) X, A = X X^T, some steps from X = u / |u|.
 //
-// A tensor is held as m x n with m <= n (transposed where it has more rows than columns): X in two f16 parts, H + L = 2^14 x, 22 bits of elements near
-// |X|, which is near one.  A = D + O and the polynomial B = b A + c A^2 are held as their diagonals in f32 and the rest in
-// two f16 parts likewise (2^13 times the value, and as B allows), because the diagonals are the large part and what is rounded there
-// changes whole rows:
+// A tensor is held as m x n with m <= n (transposed where it has more rows than columns): X in two f16 parts, H + 2^-11 L = 2^14 x.  The second
+// part is held 2^11 times larger, so that it has all of f16's bits wherever the first one has: 22 bits of an element down to 2^-28 (|X| is near
+// one), and below that to 2^-50.  (Both parts in one scale end at 2^-25 of the largest element: rows 1e-6 of the
+// others' size would be 3e-3 off, and all of the direction 2e-2 after twelve steps.)  A = D + O and the polynomial B = b A + c A^2 are held
+// as their diagonals in f32 and the rest in two f16 parts likewise (2^13 times the value, and TS_B times), because the diagonals are the large
+// part and what is rounded there changes whole rows:
 //     A^2 outside the diagonal = (d_i + d_j) O_ij + (O O)_ij,     row i of the new X = (a + B_ii) X_i + (rest of B) X.
-// The products take f16 on the matrix cores (train_gemm.h's tiles): H H + H L + L H; L L is left out, 2^-22 of the
-// result at most.  One part alone in any of the products is not enough, not even for bf16 results: what it
+// The products take f16 on the matrix cores (train_gemm.h's tiles): first H L + L H, whose sum is then taken times 2^-11, on top of it H H; L L is left
+// out, 2^-22 of the result at most.  One part alone in any of the products is not enough, not even for bf16 results: what it
 // rounds off adds up over the steps to 4e-3 of the direction for matrices of low rank and to 4e-2 for exact rank one.
 // Symmetric products form the tiles that reach the diagonal from below and store their results twice.
 // Bound by the matrix cores for large matrices and by launches (three a step) for small ones.  One 4096 x 4096, bf16: a step's products 106
@@ -47,19 +49,19 @@ static_assert(sizeof(SeriesArgs) <= 4096, "kernel arguments");
 
 __device__ __forceinline__ void split16(float x, _Float16 &h, _Float16 &l) {
     h = (_Float16)x;
-    l = (_Float16)(x - (float)h);
+    l = (_Float16)((x - (float)h) * TS_LOW);
 }
 __device__ __forceinline__ void load_two(const _Float16 *p, size_t apart, float (&x)[8]) {
     float l[8];
     load_oct(p, x);
     load_oct(p + apart, l);
 #pragma unroll
-    for (int e = 0; e < 8; e++) x[e] += l[e];
+    for (int e = 0; e < 8; e++) x[e] += l[e] * (1.0f / TS_LOW);
 }
 __device__ __forceinline__ void store_two(_Float16 *p, size_t apart, const float (&x)[8]) {
     float l[8];
 #pragma unroll
-    for (int e = 0; e < 8; e++) l[e] = x[e] - (float)(_Float16)x[e];
+    for (int e = 0; e < 8; e++) l[e] = (x[e] - (float)(_Float16)x[e]) * TS_LOW;
     store_oct(p, x);
     store_oct(p + apart, l);
 }
@@ -466,7 +468,7 @@ template <class P, class G, bool MOVE> __global__ void __launch_bounds__(TS_SMAL
     // sums of H H and of H L + L H
     auto with_low = [](f32x4 acc, f32x4 low) {
 #pragma unroll
-        for (int k = 0; k < 4; k++) acc[k] += low[k];
+        for (int k = 0; k < 4; k++) acc[k] += low[k] * (1.0f / TS_LOW);
         return acc;
     };
     // 16 x 16 results of a symmetric product of rows along k: lane l has row l % 16, columns 4 (l / 16) .. + 3
@@ -504,7 +506,7 @@ template <class P, class G, bool MOVE> __global__ void __launch_bounds__(TS_SMAL
         __builtin_memcpy(h, __builtin_assume_aligned(p, 8), 8);
         __builtin_memcpy(l, __builtin_assume_aligned(p + apart, 8), 8);
 #pragma unroll
-        for (int k = 0; k < 4; k++) x[k] = (float)h[k] + (float)l[k];
+        for (int k = 0; k < 4; k++) x[k] = (float)h[k] + (float)l[k] * (1.0f / TS_LOW);
     };
     const int pairs = tiles * (tiles + 1) / 2, columns = (length + 15) / 16;
     const float by = 1.0f / S.of_b;
@@ -593,7 +595,7 @@ template <class P, class G, bool MOVE> __global__ void __launch_bounds__(TS_SMAL
             const int k = first + j * TS_SMALL_THREADS;
             if (k >= numel) continue;
             const int at = place(k);
-            const float v = ((float)X[at] + (float)X[x_apart + at]) * size, moved = MOVE ? p[j] * A.decay - v * t.scale : v;
+            const float v = ((float)X[at] + (float)X[x_apart + at] * (1.0f / TS_LOW)) * size, moved = MOVE ? p[j] * A.decay - v * t.scale : v;
             ((P *)t.p)[k] = (P)moved;
             if (MOVE && t.copy) {
                 if (A.copy_f16) ((_Float16 *)t.copy)[k] = (_Float16)moved;

@@ -1,10 +1,10 @@
 """How near orthogonalised directions come to 64 bits, judged by what arithmetic in 32 bits loses and by nothing that the kernels do: matrices of any
-spectrum, of low and exact rank, of equal elements; on the CPU stand-in and on the GPU.
+spectrum, of low and exact rank, of equal elements, with rows and columns of very different sizes; on the CPU stand-in and on the GPU.
 
 `loss` evaluates the steps in 64 bits with every value moved that an f32 evaluation would round: by up to 2^-24 of itself, each element by itself or all
 of a matrix alike (matrices of equal elements round alike).  The kernels' operands are f16 pairs of 22 bits, off by 2^-22, four times as much, and
 each product has two of them and leaves out the product of the second parts, another 2^-22: 3 * 4 = 12 times that loss is allowed.  What is below f16's numbers adds an absolute
-error: 2^-25 of a unit in X (of 2^-14), A outside its diagonal (2^-13) and the polynomial (2^-12 for the usual
+error: 2^-25 of a second part's unit, held 2^11 times larger, in X (units of 2^-14), A outside its diagonal (2^-13) and the polynomial (2^-12 for the usual
 coefficients; |b| + 4 |c| times A's); a later step raises it by at most |a| (the largest slope of the polynomials here).  The last rounding is
 monotone, so an element lies between the rounded ends of what is allowed."""
 import ctypes as C
@@ -45,7 +45,7 @@ def allowed(u, steps):
     off = torch.stack([(loss(u, steps, s, s % 2 == 1) - want).abs() for s in range(8)]).amax(0)
     off = torch.minimum(off.amax(1, keepdim=True), off.amax(0, keepdim=True))
     a, b, c = (abs(k) for k in sr.COEFFICIENTS)
-    floor = 2.0**-25 * (2.0**-14 + min(u.shape) ** 0.5 * (2.0**-12 + (b + 4 * c) * 2.0**-13))
+    floor = 2.0**-36 * (2.0**-14 + min(u.shape) ** 0.5 * (2.0**-12 + (b + 4 * c) * 2.0**-13))
     return want, 12 * off + floor * sum(a**k for k in range(1, steps + 1)) * 2
 
 
@@ -65,10 +65,23 @@ def outer(m, n, rank, seed, whole=False, sign=False):
     return torch.sign(p) @ torch.sign(q) if sign else p @ q
 
 
+def graded(m, n, rows=True, cols=False):
+    """rows (columns) of sizes 1, 1e-4, 1e-6, 1e-8 in turn"""
+    x = sr.matrix(m, n, 11).double()
+    if rows:
+        x = x * (10.0 ** torch.tensor([0.0, -4.0, -6.0, -8.0], dtype=F64))[torch.arange(m) % 4][:, None]
+    if cols:
+        x = x * (10.0 ** torch.tensor([0.0, -4.0, -6.0, -8.0], dtype=F64))[torch.arange(n) % 4]
+    return x
+
+
 def matrices(m, n):
+    one = graded(m, n)
+    one[1:] = one[1:].sign() * 1e-6
     return {
         "normal": sr.matrix(m, n, 1),
         "strong": sr.matrix(m, n, 2, "strong"),
+        "falling": sr.matrix(m, n, 3, "falling"),
         "rank 3 and noise": sr.matrix(m, n, 4, "rank3"),
         "rank 1 and noise": outer(m, n, 1, 5) + 1e-4 * sr.matrix(m, n, 6).double(),
         "rank 1": outer(m, n, 1, 7, whole=True),
@@ -76,6 +89,10 @@ def matrices(m, n):
         "rank 4": outer(m, n, 4, 9),
         "ones": torch.ones(m, n),
         "identity": torch.eye(m, n),
+        "graded rows": graded(m, n),
+        "graded columns": graded(m, n, False, True),
+        "both graded": graded(m, n, True, True),
+        "one strong row": one,
     }
 
 
@@ -129,7 +146,7 @@ def test_against_the_loss_of_32_bits(ctx, kind, size, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("kind", ["normal", "rank 1", "ones"])
+@pytest.mark.parametrize("kind", ["normal", "rank 1", "ones", "graded rows"])
 def test_tiles_of_every_size(ctx, kind, dtype):
     """sixteen of 256 x 1100: 128 x 128 tiles and larger; one of 1100 x 1030: 32 x 128 and 128 x 128, some with their k axes in parts"""
     us = [matrices(256, 1100)[kind].to(dtype).to("cuda:0")] * 16
