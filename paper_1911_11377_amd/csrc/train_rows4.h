@@ -32,6 +32,7 @@ struct Rows4Args {
 #define TG_KEEP() (void)0
 static inline unsigned upper_halves(float low, float high) { return __float_as_uint(low) >> 16 | (__float_as_uint(high) & 0xffff0000u); }
 static inline float within(float x, float most) { return fminf(fmaxf(x, -most), most); }
+static inline float quieted(float x) { return x == x ? x : __uint_as_float(__float_as_uint(x) | 0x400000u); }
 #else
 // what the wave wrote to LDS is there for all of its lanes (a wave's LDS instructions keep their order)
 __device__ __forceinline__ void wave_fence() {
@@ -42,6 +43,7 @@ __device__ __forceinline__ void wave_fence() {
 #define TG_KEEP() asm volatile("" ::: "memory")  // loads before it stay before it (the compiler would move those of a later round to their use)
 __device__ __forceinline__ unsigned upper_halves(float low, float high) { return __builtin_amdgcn_perm(__float_as_uint(high), __float_as_uint(low), 0x07060302u); }
 __device__ __forceinline__ float within(float x, float most) { return __builtin_amdgcn_fmed3f(x, -most, most); }  // (of NaN: a number)
+__device__ __forceinline__ float quieted(float x) { return __builtin_canonicalizef(x); }  // (a NaN gets its quiet bit: one in the upper half of its word)
 // the lowest 4 bits of c as a number from -8 to 7, in sixteenths
 __device__ __forceinline__ float code_to_float(unsigned c) { return __builtin_amdgcn_cvt_off_f32_i4((int)c); }
 // word s of the lane in row q of 16 lanes <-> word q of the lane in row s
@@ -82,12 +84,13 @@ template <class T> __device__ __forceinline__ u32x4 codes8(unsigned w) {
     }
     return o;
 }
-// f32 values as three bf16 parts, each what is left cut to 8 bits: together all 24.  An infinity is in its first part (what is left of it,
-// NaN, becomes a number that its product does not notice)
+// f32 values as three bf16 parts, each what is left cut to 8 bits: together all 24 (to bf16's smallest number, 2^-133).  An infinity is in its first part
+// (what is left of it, NaN, becomes a number that its product does not notice), and so is a NaN: cut as it is, one whose payload
+// lies in the lower half of its word would be an infinity
 __device__ __forceinline__ void cut3(const float (&x)[8], u32x4 (&part)[3]) {
 #pragma unroll
     for (int e = 0; e < 4; e++) {
-        float r[2] = {x[2 * e], x[2 * e + 1]};
+        float r[2] = {quieted(x[2 * e]), quieted(x[2 * e + 1])};
 #pragma unroll
         for (int p = 0; p < 3; p++) {
             part[p][e] = upper_halves(r[0], r[1]);
