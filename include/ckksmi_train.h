@@ -193,7 +193,8 @@ int ckksmi_muon_step(ckksmi_ctx *ctx, const ckksmi_muon *opt, const ckksmi_muon_
  * [d_out][round_up(d_in, 32) / 2] bytes, two's complement, the even k of a pair in the lower half of its byte (what lies behind d_in may
  * be anything), 16-byte aligned; scales: [d_out][ceil(d_in / group)] of dtype.  group: 32, 64, .. 1024; d_in, d_out, ld 1 .. 2^20.
  * Products are formed from the codes' exact values and x (f32 x as three bf16 parts, 24 bits), summed in 32 bits over a group, and the
- * groups' sums times their scales in 32 bits; the order depends on the sizes alone.  Any number of rows, but every 64 read the codes again. */
+ * groups' sums times their scales in 32 bits; the order depends on the sizes alone.  A group's sum of code * x has to stay below 2^132 (16 times
+ * f32's largest number) and an answer, with its sums on the way, within its type; f32 x smaller than 2^-110 has fewer than 24 bits (to 2^-133).  Any number of rows, but every 64 read the codes again. */
 typedef struct {
     int dtype;          /* of x, y and the scales */
     int group;

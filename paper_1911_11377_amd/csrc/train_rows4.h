@@ -5,7 +5,9 @@
 // lanes of a row read 32 codes each and exchange words, so that lane l holds what a step of the matrix cores takes of it: 8 codes of row l % 16
 // from k0 + 32 s + 8 (l / 16) on for step s.  Codes become bf16 or f16 exactly (in sixteenths: that is what the
 // conversion gives), a group's sum stays in f32 and is scaled there: a scaled weight rounded to 16 bits would cost three decimal
-// places of four.  x: 16-bit as it is, f32 in three bf16 parts, cut as it is read; h between the block's products in two or three bf16 parts.
+// places of four.  Sums stay in sixteenths to the end: 16 of a group's sum, or of its scale, may be beyond f32 where the answer is not.
+// (Near f32's smallest numbers a group's product is rounded to 2^-146 of the answer so; products of single elements would be to 2^-150, 32 of them.)
+// x: 16-bit as it is, f32 in three bf16 parts, cut as it is read; h between the block's products in two or three bf16 parts.
 // The waves' sums meet in LDS and are added in their order.
 // Bound by the codes' bytes (one row, 8192 -> 16384: 20 - 22.5 us, 3.1 - 3.4 TB/s), for small matrices by the latency of one trip to memory (1024 -> 4096,
 // two of them: 7.4 us), and for 64 f32 rows by cutting x, which every workgroup does (4096 -> 4096: 24 - 27 us)
@@ -211,7 +213,7 @@ __global__ void __launch_bounds__(64 * WAVES) rows4_kernel(Rows4Args R) {
 #pragma unroll
                     for (int t = 0; t < MT; t++)
 #pragma unroll
-                        for (int r = 0; r < 4; r++) acc[a][t][r] = fmaf(scale[r], 16.0f * sum[a][t][r], acc[a][t][r]);  // (16 scale may be beyond f32)
+                        for (int r = 0; r < 4; r++) acc[a][t][r] = fmaf(scale[r], sum[a][t][r], acc[a][t][r]);
                 }
         }
     };
@@ -296,7 +298,7 @@ __global__ void __launch_bounds__(64 * WAVES) rows4_kernel(Rows4Args R) {
 #pragma unroll 3
             for (int k = 1; k < WAVES; k++) s += sums_of(k, a, t, (2 * half + e) * 16 + r);
 #pragma unroll
-            for (int j = 0; j < 4; j++) v[a][4 * e + j] = s[j];
+            for (int j = 0; j < 4; j++) v[a][4 * e + j] = 16.0f * s[j];
         }
     if constexpr (GATE) {
         float h[8];

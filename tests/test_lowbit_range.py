@@ -1,10 +1,12 @@
-"""Products with 4-bit matrices at the ends of their types' ranges: NaN of any payload; on the CPU stand-in and
+"""Products with 4-bit matrices at the ends of their types' ranges: NaN of any payload, finite answers of numbers near the largest; on the CPU stand-in and
 on the GPU."""
+import math
+
 import pytest
 import torch
 
 import train_emu_support as emu
-from lowbit_reference import F32
+from lowbit_reference import BF16, F32
 from paper_1911_11377_amd import ckksmi, lowbit
 
 
@@ -51,3 +53,27 @@ def test_every_nan_makes_its_row_nan(where, word, rows):
         block.forward(x, into, into, matrix4(block.out, 1, 1.0, device), z, ws)
         for r in (y, z):
             assert bool(torch.isnan(r[1]).all()) and bool(torch.isfinite(r[torch.arange(rows) != 1]).all())
+
+
+# x, code, scale: what 16 times a sum, or 16 times a scale, does not hold; the answer is finite
+ENDS = [(6e37, 7, 0.01), (3.3e38, 1, 0.5), (-3.3e38, -8, 1e-3), (1e-3, 7, 2e38), (4e-39, -8, 3e38), (1e-30, 3, 1e30), (5e36, 7, 9.0)]
+
+
+@pytest.mark.parametrize("x,code,scale", ENDS)
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_finite_answers_of_large_numbers(where, x, code, scale, dtype, group):
+    """one number that is not 0 in a row: its product with the code is exact in three parts, which two sums put together; one product with the scale, one
+    rounding at the end.  bfloat16 parts end at 2^-133: the last of f32 x is off by less than that"""
+    ctx, device = where
+    for rows, d_in, at in ((1, 1, 0), (3, 200, 150), (40, 300, 2)):
+        v = torch.zeros(rows, d_in, dtype=dtype)
+        v[0, at] = x
+        plan = lowbit.Product4(ctx, d_in, 5, dtype, group)
+        w = matrix4(plan, code, scale, device)
+        y = torch.full((rows, 5), math.nan, dtype=dtype, device=device)
+        plan.forward(v.to(device), *w, y)
+        want = float(v[0, at]) * code * float(w[1][0, 0])
+        off = 3 * 2.0**-24 * abs(want) + (2.0**-133 * abs(code * scale) if dtype == F32 else 2.0**-8 * abs(want))
+        assert bool(((y[0].double() - want).abs() <= off).all()), (y[0], want)
+        assert bool((y[1:] == 0).all())
