@@ -305,12 +305,15 @@ __global__ void __launch_bounds__(64 * WAVES) rows4_kernel(Rows4Args R) {
 #pragma unroll
         for (int e = 0; e < 8; e++) h[e] = n + e < R.N ? act_value(R.epi.act, v[0][e]) * v[1][e] : 0.0f;
         for (int p = 0; p < R.h_parts; p++) {
-            store_oct((__bf16 *)R.h + p * R.h_apart + (size_t)m * R.ldh + n, h);
+            // (a part is at most bf16's largest number, 3.3895e38: rounded, a finite h beyond it would be an infinity)
+            float part[8];
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const float part = (float)(__bf16)h[e];
-                h[e] = fabsf(part) <= 3.4e38f ? h[e] - part : 0.0f;  // what is not finite is in its first part alone
+                const bool finite = fabsf(h[e]) <= 3.4028235e38f;
+                part[e] = finite ? (float)(__bf16)within(h[e], 3.3895314e38f) : h[e];
+                h[e] = finite ? h[e] - part[e] : 0.0f;  // what is not finite is in its first part alone
             }
+            store_oct((__bf16 *)R.h + p * R.h_apart + (size_t)m * R.ldh + n, part);
         }
     } else
         epilogue8<O, EPI_STORE>(R.epi, m, n, v[0], v[0]);

@@ -77,3 +77,23 @@ def test_finite_answers_of_large_numbers(where, x, code, scale, dtype, group):
         off = 3 * 2.0**-24 * abs(want) + (2.0**-133 * abs(code * scale) if dtype == F32 else 2.0**-8 * abs(want))
         assert bool(((y[0].double() - want).abs() <= off).all()), (y[0], want)
         assert bool((y[1:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_h_beyond_the_largest_16_bit_number(where, dtype, sign):
+    """h = 181 * 181 * 2^113 = (1 - 2^-12.2) 2^128, in f32's range, is rounded beyond bfloat16's largest number, (1 - 2^-8) 2^128"""
+    ctx, device = where
+    plan = lowbit.GatedFF4(ctx, 1, 1, 3, dtype, "linear", 32)
+    x, y = torch.ones(2, 1, dtype=dtype, device=device), torch.zeros(2, 3, dtype=dtype, device=device)
+    gate, up, down = matrix4(plan.into, sign, 181 * 2.0**112, device), matrix4(plan.into, 1, 362.0, device), matrix4(plan.out, 1, 2.0**-10, device)
+    h = 181 * 181 * 2.0**113
+    assert torch.tensor(h).isfinite() and not torch.tensor(h).to(BF16).isfinite()
+    plan.forward(x, gate, up, down, y, room(plan.workspace_bytes(2), device))
+    # two parts have 16 bits of h (three: 24), and the answer's rounding
+    off = (2.0**-16 if dtype == BF16 else 2.0**-22) + 2.0**-24 + (2.0**-8 if dtype == BF16 else 0)
+    assert bool(((y.double() - sign * h * 2.0**-10).abs() <= off * h * 2.0**-10).all()), (y, h * 2.0**-10)
+    # an infinity stays one
+    gate[1].fill_(3e38)
+    plan.forward(x, gate, up, down, y, room(plan.workspace_bytes(2), device))
+    assert bool((y == sign * math.inf).all())
