@@ -33,7 +33,8 @@ class GatedHead:
     [d_out][d_hidden], updated in place; dtype: the type the products run in (bfloat16 and float16: copies of the weights,
     renewed by each step); state_bits: 8 or 32.  optimizer: "adamw", or "muon" (steps along orthogonalised momentum, which is held in 32
     bits).  empty(shape, dtype) allocates zeros on the device.  The constructor waits for what it enqueues: answers and steps may
-    use any stream."""
+    use any stream.  Steps have to be ordered after each other, and answers after each other: each kind has buffers of its own and shares them with
+    nothing else, so an answer may be made within `loss` or beside a step; the weights that it reads move at the step's end."""
 
     def __init__(self, ctx, rows, weights, act, dtype, empty, state_bits=8, optimizer="adamw"):
         import torch
@@ -61,13 +62,14 @@ class GatedHead:
             units = [[empty((-(-w.numel() // ckksmi.STATE_BLOCK),), torch.float32) for w in weights] for _ in range(2)] if state_bits == 8 else (None, None)
             self.opt = training.AdamW(ctx, weights, self.grads, m, v, *units, copies=copies)
         self.ws = empty((max(16, self.ff.workspace_bytes(rows, backward=True)),), torch.uint8)
+        self.answer_ws = empty((max(16, self.ff.workspace_bytes(rows)),), torch.uint8)
         self.saved = empty((max(16, self.ff.saved_bytes(rows)),), torch.uint8)
         self.y, self.dy = [empty((rows, weights[2].shape[0]), dtype) for _ in range(2)]
         if weights[0].is_cuda:
             torch.cuda.current_stream(weights[0].device).synchronize()
 
     def answer(self, x, y, stream=None):
-        self.ff.forward(x, *self.used, y, self.ws, stream=stream)
+        self.ff.forward(x, *self.used, y, self.answer_ws, stream=stream)
 
     def step(self, x, loss, lr, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.0, stream=None):
         """One step on rows x.  loss(y, dy) writes the loss's gradient by the answers y into dy; what it returns is returned.  All of the step is
@@ -92,7 +94,7 @@ class GatedHead:
 class ResidualHead:
     """A gated block between norms, answers of the features' width: r = residual_scale x + block_scale gate * N_post(block(N_pre(x))), with a learned
     gate for every channel.  `block` is the GatedHead inside (its weights, its optimizer); `vectors` are the norms' weights and the gate
-    (float32, from ones; AdamW with 32-bit states).  Arguments as for GatedHead."""
+    (float32, from ones; AdamW with 32-bit states).  Arguments, and which calls may run beside each other, as for GatedHead."""
 
     def __init__(self, ctx, rows, weights, act, dtype, empty, norm="rms", residual_scale=1.0, block_scale=1.0, eps=1e-5, optimizer="muon", state_bits=32):
         import torch
@@ -109,7 +111,7 @@ class ResidualHead:
         self.grads = {k: empty((d,), torch.float32) for k in names}
         states = [[empty((d,), torch.float32) for _ in names] for _ in range(2)]
         self.opt = training.AdamW(ctx, [self.vectors[k] for k in names], [self.grads[k] for k in names], *states)
-        self.n, self.f, self.df, self.dn, self.r, self.dr = [empty((rows, d), dtype) for _ in range(6)]
+        self.n, self.f, self.df, self.dn, self.r, self.dr, self.answer_n, self.answer_f = [empty((rows, d), dtype) for _ in range(8)]
         self.saved = [empty((max(16, p.saved_bytes(rows)),), torch.uint8) for p in (self.before, self.after)]
         self.ws = empty((max(16, self.before.workspace_bytes(rows), self.after.workspace_bytes(rows)),), torch.uint8)
         if weights[0].is_cuda:
@@ -128,10 +130,10 @@ class ResidualHead:
         self.after.forward(x, f, r, None, **self._of("post"), stream=stream)
 
     def answer(self, x, r, stream=None):
-        rows = x.shape[0]
-        self.normed(x, self.n[:rows], stream)
-        self.block.answer(self.n[:rows], self.f[:rows], stream)
-        self.joined(x, self.f[:rows], r, stream)
+        n, f = (t[:x.shape[0]] for t in (self.answer_n, self.answer_f))
+        self.normed(x, n, stream)
+        self.block.answer(n, f, stream)
+        self.joined(x, f, r, stream)
 
     def step(self, x, loss, lr, vector_lr=1e-3, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.0, stream=None):
         """one step on rows x, like GatedHead.step; vector_lr: of the norms' weights and the gate"""
@@ -151,7 +153,8 @@ class ResidualHead:
 
 class LowBitHead:
     """A trained head's answers in the clear from its matrices in 4 bits, up to `rows` rows a call.  weights: device tensors as for GatedHead (read once,
-    here); empty(shape, dtype) allocates on the device.  The constructor waits for what it enqueues."""
+    here); empty(shape, dtype) allocates on the device.  The constructor waits for what it enqueues: answers may use any stream, but have to be
+    ordered after each other, since they share a workspace; one that may run beside others takes its own, of workspace_bytes(rows)."""
 
     def __init__(self, ctx, rows, weights, act, dtype, empty, group=128):
         import torch
@@ -163,12 +166,15 @@ class LowBitHead:
             pair = empty(plan.codes_shape, torch.uint8), empty(plan.scales_shape, dtype)
             plan.pack(w, *pair)
             self.matrices.append(pair)
-        self.ws = empty((max(16, self.ff.workspace_bytes(rows)),), torch.uint8)
+        self.ws = empty((self.workspace_bytes(rows),), torch.uint8)
         if weights[0].is_cuda:
             torch.cuda.current_stream(weights[0].device).synchronize()
 
-    def answer(self, x, y, stream=None):
-        self.ff.forward(x, *self.matrices, y, self.ws, stream=stream)
+    def workspace_bytes(self, rows):
+        return max(16, self.ff.workspace_bytes(rows))
+
+    def answer(self, x, y, stream=None, ws=None):
+        self.ff.forward(x, *self.matrices, y, self.ws if ws is None else ws, stream=stream)
 
 
 @dataclass
