@@ -71,7 +71,8 @@ extern "C" {
 #define CKKSMI_K_SERIES_PASS 48   /* momentum, normalisation, parameters (units: workgroups) */
 #define CKKSMI_K_ROWS4 49         /* products of few rows with a 4-bit matrix (units: operations) */
 #define CKKSMI_K_PACK4 50         /* matrices to 4 bits and back (units: elements) */
-#define CKKSMI_K_COUNT 51
+#define CKKSMI_K_SERIES_SMALL 51  /* whole directions, one matrix a workgroup (units: operations of their products) */
+#define CKKSMI_K_COUNT 52
 int ckksmi_profile_enable(ckksmi_ctx *ctx, int on);
 int ckksmi_profile_read(ckksmi_ctx *ctx, int kernel_class, double *total_ms, long long *launches, double *units);
 /* name of the kernel that class runs as in this context (the transforms have size-specific kernels; a fused kernel's variants for

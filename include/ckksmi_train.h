@@ -153,7 +153,7 @@ int ckksmi_adamw_read_states(ckksmi_ctx *ctx, const ckksmi_adamw_tensor *tensors
  * size have fewer bits than f32 would give them.  The diagonals of A and of the polynomial are held in f32; every product is three
  * products of the parts, whatever type the direction ends in.  Any finite u; an infinity or NaN makes the direction NaN (and 0).
  * Sizes 0 .. 2^16 each (a matrix without elements is left out); numbers of any type are contiguous.  A tensor's results depend on its own
- * numbers and on the sizes in the call alone. */
+ * numbers and on the sizes in the call, in their order, alone. */
 typedef struct {
     double a, b, c;     /* 3.4445, -4.7750, 2.0315 reach [0.7, 1.2] from most singular values in five steps */
     double eps;         /* >= 0 */

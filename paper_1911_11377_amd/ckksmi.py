@@ -168,7 +168,7 @@ SIGNATURES = {
 _RESTYPES = {"ckksmi_ctx_destroy": None, "ckksmi_strerror": C.c_char_p, "ckksmi_kernel_class_name": C.c_char_p}
 TRAINING = ("ckksmi_gated_ff_", "ckksmi_adamw_", "ckksmi_residual_norm_", "ckksmi_orthogonalise", "ckksmi_muon_", "ckksmi_pack4", "ckksmi_unpack4", "ckksmi_product4",
             "ckksmi_gated_ff4_")  # entry points of include/ckksmi_train.h
-K_COUNT = 51
+K_COUNT = 52
 
 _LIBS = {}
 

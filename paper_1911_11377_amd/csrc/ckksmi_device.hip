@@ -1903,7 +1903,7 @@ extern "C" const char *ckksmi_kernel_class_name(const ckksmi_ctx *c, int kernel_
                                                 "axpy_limb_kernel", "modup_cols_kernel", "inner_product_hoisted_tile_kernel", "automorphism_bcast_kernel",
                                                 "encoding kernels", "encryption kernels", "modup_cols_kernel", "conv_mac_mfma_resident_kernel", "conv_mac_mfma_strip_kernel", "conv_final_kernel", "inner_wg_kernel",
                                                 "tensor_wg_kernel", "ntt_wg_inv_gal_kernel", "tail_sources_kernel", "mac_wsum_kernel", "gemm_kernel", "gemm_join_kernel", "pad_rows_kernel", "adamw_kernel", "adamw_read_kernel", "rows_kernel",
-                                                "norm_forward_kernel", "norm_backward_kernel", "norm_join_kernel", "gemm_kernel", "series_join_kernel", "series_begin_kernel", "rows4_kernel", "pack4_kernel"};
+                                                "norm_forward_kernel", "norm_backward_kernel", "norm_join_kernel", "gemm_kernel", "series_join_kernel", "series_begin_kernel", "rows4_kernel", "pack4_kernel", "series_small_kernel"};
     if (kernel_class < 0 || kernel_class >= CKKSMI_K_COUNT) return "";
     if (c && kernel_class == CKKSMI_K_INNER_HOISTED && !hoisted_tile_ok(c, c->beta_top)) return "inner_product_hoisted_kernel";
     if (c && c->logN >= 12 && c->logN <= 16) {

@@ -241,7 +241,12 @@ inline int64_t series_squares(const SeriesPlan &l) { return (int64_t)((l.side + 
 template <class P, class G, bool MOVE> void run_small(ckksmi_ctx *c, const SeriesCall &call, const ckksmi_series &s, const PassArgs &A, hipStream_t st) {
     const SmallSeries S{s.steps, (float)s.a, (float)s.b, (float)s.c, call.of_b};
     for_tables(call, {}, A, 0, [](const SeriesPlan &) { return (int64_t)1; }, [&](const PassArgs &a, unsigned blocks) {
-        KL(c, CKKSMI_K_SERIES, blocks, (series_small_kernel<P, G, MOVE>), dim3(blocks), dim3(TS_SMALL_THREADS), st, a, S);
+        double flops = 0;  // three products of each kind, half of the symmetric ones
+        for (int i = 0; i < a.n; i++) {
+            const double m = std::min(a.t[i].rows, a.t[i].cols), n = std::max(a.t[i].rows, a.t[i].cols);
+            flops += 3.0 * s.steps * (m * m * n + m * m * m + 2.0 * m * m * n);
+        }
+        KL(c, CKKSMI_K_SERIES_SMALL, flops, (series_small_kernel<P, G, MOVE>), dim3(blocks), dim3(TS_SMALL_THREADS), st, a, S);
     });
 }
 template <class P, bool MOVE> void run_series(ckksmi_ctx *c, const SeriesCall &call, const ckksmi_series &s, const PassArgs &A, void *ws, hipStream_t st) {

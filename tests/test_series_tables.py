@@ -92,3 +92,19 @@ def test_every_matrix_of_a_call_on_the_stand_in(small):
         c._L.emu_series_small(2**63)
     assert c.errors() == 0
     c.close()
+
+
+@pytest.mark.gpu
+def test_operations_that_the_profile_counts(ctx):
+    """three products of each kind a step, half of the symmetric ones: the same count in tiles and in one workgroup, under the kernel that ran"""
+    for (m, n), name in (((60, 90), "series_small_kernel"), ((256, 512), "gemm_kernel")):
+        u = sr.matrix(m, n, 1).to("cuda:0")
+        plan = training.Orthogonalise(ctx, [u], [torch.empty_like(u)])
+        ws = torch.empty(max(16, plan.workspace_bytes()), dtype=torch.uint8, device="cuda:0")
+        ctx.profile_enable(True)
+        plan.run(ws, steps=4)
+        torch.cuda.synchronize()
+        ran = ctx.profile_read()
+        ctx.profile_enable(False)
+        assert ran[name][1] == (1 if m == 60 else 12) and ran[name][2] == 4 * 3.0 * (m * m * n + m**3 + 2 * m * m * n), ran
+        assert ("gemm_kernel" in ran) == (m == 256)
