@@ -86,14 +86,15 @@ long long series_tiles(const SeriesProblem &p, const SeriesShape &t, bool triang
 }
 inline int series_steps(const SeriesProblem &p) { return (p.K + 63) / 64 * p.nsrc; }
 
-// Tile and parts of the k axis of a launch.  Measured, us of a whole direction (bf16: one product of each kind, f32: three):
+// Tile and parts of the k axis of a launch.  Measured, us of a whole direction (three products of each kind):
 //   enough 128 x 128 tiles for three quarters of the compute units: those or 256 x 256, by rounds of the compute units, which hold one of 256 or two of 128
-//       (a round of the smaller takes 0.56 of the larger's; X X^T and its square for one 4096 x 4096, 136 tiles of 256 or 528 of 128: 1757, 1923;
-//       X X^T of twelve 1024 x 4096, 120 or 432: 3810, 3290)
-//   enough 32 x 128 tiles: those, the k axis whole (X X^T of 2048 x 2048, bf16, 544: 527, 136 of 128 566, in 3 parts 608)
-//   few tiles and a long k axis: 128 x 128 in parts (X X^T of 1024 x 4096, f32: 8 parts 599, 4 632, 32 x 128 whole 667, in 4 parts 612)
+//       (a round of the smaller takes 0.72 of the larger's; all in tiles of 256, 128: one 4096 x 4096 4340, 5290; 8192 x 8192, 528 tiles of 256 or 2080
+//       of 128 for the symmetric products, 32400, 39300, and with 128 there alone 36000; 6144 x 6144 15730, 16190; twelve of 1024 x 4096,
+//       whose X X^T has 120 or 432: 3800, 3530, and with 256 for X's product alone 3270)
+//   enough 32 x 128 tiles: those, the k axis whole (2048 x 2048, 544: 1080, 136 of 128 1200)
+//   few tiles and a long k axis: 128 x 128 in parts (X X^T of 1024 x 4096: 8 parts 599, 4 632, 32 x 128 whole 667, in 4 parts 612)
 //   else 32 x 128, with four groups of waves for a tile's k axis (launch_series); in parts where that leaves half of the compute units idle
-//       (the square and X X^T of 1024 x 1024, f32: 32 x 128 whole 377, two parts 428, 128 x 128 in 4 421; X X^T of two 256 x 3136: 8 parts 212, 4 231, whole 336)
+//       (the square and X X^T of 1024 x 1024: 32 x 128 whole 377, two parts 428, 128 x 128 in 4 421; X X^T of two 256 x 3136: 8 parts 212, 4 231, whole 336)
 SeriesLaunch series_choose(const SeriesProblem *p, int n, bool triangle) {
     long long tiles[3] = {0, 0, 0};
     int steps = 0;
@@ -104,7 +105,7 @@ SeriesLaunch series_choose(const SeriesProblem *p, int n, bool triangle) {
     const long long units = 4 * TG_ENOUGH_TILES / 3;  // compute units
     auto rounds = [](long long tiles, long long held) { return (double)((tiles + held - 1) / held); };
     auto parts = [&](int t) { return (int)std::max(1LL, std::min(std::min(256 / tiles[t], (long long)steps / 16), 32LL)); };
-    if (tiles[1] >= TG_ENOUGH_TILES) return SeriesLaunch{TS_TILE(rounds(tiles[0], units) <= 0.56 * rounds(tiles[1], 2 * units) ? 0 : 1), 1};
+    if (tiles[1] >= TG_ENOUGH_TILES) return SeriesLaunch{TS_TILE(rounds(tiles[0], units) <= 0.72 * rounds(tiles[1], 2 * units) ? 0 : 1), 1};
     if (tiles[2] >= 256) return SeriesLaunch{2, 1};
     if (steps >= 128 && tiles[1] >= 24) return SeriesLaunch{1, parts(1)};
     return SeriesLaunch{2, parts(2)};
