@@ -123,6 +123,14 @@ template <int LANES> struct RowSums {
     }
 };
 
+// A layer norm's mean is a sum in 32 bits, some last places off: of a row of equal numbers, 1e4 say, what is left of them would be normed to 0.3 and more.
+// The sum of what is left says how far it is off, and with it comes the sum of squares: q of the mean before, t that sum
+__device__ __forceinline__ void right_mean(const NormArgs &A, float t, float &mean, float &q) {
+    const float by = t * A.inv_d;
+    mean += by;
+    q = fmaxf(fmaf(-t, by, q), 0.0f);  // (a row that is not finite has a mean that is not)
+}
+
 // mean and s of a row's values that the group holds (elements beyond the row are zeros)
 template <bool LAYER, int LANES, int V>
 __device__ __forceinline__ void row_stats(const NormArgs &A, int kind, int t, const float (&v)[V][8], RowSums<LANES> &sums, float &mean, float &s) {
@@ -135,15 +143,20 @@ __device__ __forceinline__ void row_stats(const NormArgs &A, int kind, int t, co
         sums(mean);
         mean *= A.inv_d;
     }
-    float q = 0.0f;
+    float q = 0.0f, left = 0.0f;
 #pragma unroll
     for (int j = 0; j < V; j++)
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             const float c = LAYER ? (8 * (t + LANES * j) + e < A.d ? v[j][e] - mean : 0.0f) : v[j][e];
             q = fmaf(c, c, q);
+            if (LAYER) left += c;
         }
-    sums(q);
+    if (LAYER && kind == CKKSMI_NORM_LAYER) {
+        sums(q, left);
+        right_mean(A, left, mean, q);
+    } else
+        sums(q);
     s = 1.0f / sqrtf(q * A.inv_d + A.eps);
 }
 
@@ -427,7 +440,7 @@ template <class T> __global__ void __launch_bounds__(NORM_LONG) norm_forward_lon
         // mean and s of what value(oct, v) gives (zeros beyond the row)
         auto stats = [&](int kind, auto value, float &mean, float &s) {
             mean = 0.0f;
-            float v[8], q = 0.0f;
+            float v[8], q = 0.0f, left = 0.0f;
             if (kind == CKKSMI_NORM_LAYER) {
                 for (int o = threadIdx.x; o < octs; o += NORM_LONG) {
                     value(8 * o, v);
@@ -443,9 +456,11 @@ template <class T> __global__ void __launch_bounds__(NORM_LONG) norm_forward_lon
                 for (int e = 0; e < 8; e++) {
                     const float c = 8 * o + e < A.d ? v[e] - mean : 0.0f;
                     q = fmaf(c, c, q);
+                    left += c;
                 }
             }
-            sums(q);
+            sums(q, left);
+            if (kind == CKKSMI_NORM_LAYER) right_mean(A, left, mean, q);
             s = 1.0f / sqrtf(q * A.inv_d + A.eps);
         };
         auto load = [&](const T *p, int at, float (&v)[8]) {
