@@ -30,7 +30,9 @@ inline int rule_of(int64_t d, int rules) {
 inline int threads_of(int lanes) { return lanes > 64 ? lanes : 256; }
 inline int groups_of(int lanes) { return threads_of(lanes) / lanes; }
 
-// Workgroups of a backward pass, each going through its rows: as many as the compute units hold at once, so that all have the same number of rows
+// Workgroups of a backward pass, each going through its rows: as many as the compute units hold at once, so that all have the same number of rows.
+// Registers say how many: up to 168 a thread let three waves share a SIMD (768 workgroups of 256 threads).  rms norms have 145 - 168, 16-bit layer norms
+// with an element's gate 164 - 168; without one, where the weights and a channel's gate are kept besides, 172 - 180: two (512)
 // (16384 rows of 2048, rms, both passes: 768 172 us, 1024 209, 512 201; layer norms with a gate's columns 512 222, 768 260, an element's gate
 // 768 211, 512 231)
 int64_t backward_blocks(const ckksmi_residual_norm &c) {

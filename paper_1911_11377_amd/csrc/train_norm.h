@@ -1,7 +1,9 @@
 // Norms before and after a block with its gate and residual sum: r = a x + b gate N1(f), n = N2(r), and their backward pass.
 //
-// A row's norm needs all of the row before its first result: a group of threads holds a row in registers, 8 neighbouring elements a thread,
-// so every operand is read once, and the columns' weights once per group.  With h = (v - mean) s, s = 1 / sqrt(mean (v - mean)^2 + eps),
+// A row's norm needs all of the row before its first result: a group of threads holds a row in registers, 8 neighbouring elements a thread (16
+// for forward rows beyond 8192), so every operand is read once, and the columns' weights once per group.  Layer norms of the widest rows
+// do not fit the 128 registers of a thread of 1024 and keep some in memory: 19 - 29 forward beyond 8192, 153 - 201 backward beyond 4096 (with the
+// columns' sums and weights), where both passes take 293 us for 4096 bf16 rows of 8192, of rms norms 180.  With h = (v - mean) s, s = 1 / sqrt(mean (v - mean)^2 + eps),
 // the gradient of N(v) = h w + b by v is, for g = dy w,
 //     dv = (g - mean(g) - h mean(g h)) s          (rms: without the first mean)
 // The forward pass saves each row's two means and two s; the backward pass forms h of both norms again from x and f and needs two rounds of sums
@@ -10,9 +12,11 @@
 // workgroups' sums go to memory once, and a second kernel adds them in their order: gradients of w1, b1, w2, b2 are P g, Q g, R, T, and of a
 // channel's gate g it is P w1 + Q b1.
 // A norm that is not there has mean 0, s 1, w 1 and b 0; a block that is not there f = 0, a = 1, b = 0: the same results without a case.
-// Longer rows than registers hold are read once for each sum; their column sums take a pass of their own.
+// Longer rows than registers hold (forward beyond 16384, backward beyond 8192) are read once for each sum; their column sums take a pass of their
+// own: 2048 bf16 rows of 16384, rms, both passes, 364 us (1.85 TB/s of what they need); 1024 rows of 65536, forward, 234 us (2.3).
 // Bound by memory: 4096 f32 rows of 4096, forward, 48 - 57 us, 4.6 TB/s and more (a large copy: 4.7); 16384 bf16 rows of 2048 60 us forward (4.5), 109
-// backward (3.7: six operands, and 512 or 768 workgroups whose last rows end at different times); one row 3.7 us, a launch
+// backward (3.7: six operands, and 512 or 768 workgroups whose last rows end at different times); with layer norms both 225; one row 3.7 us, a
+// launch
 #pragma once
 #include "train_types.h"
 

@@ -10,7 +10,9 @@
 // x: 16-bit as it is, f32 in three bf16 parts, cut as it is read; h between the block's products in two or three bf16 parts.
 // The waves' sums meet in LDS and are added in their order.
 // Bound by the codes' bytes (one row, 8192 -> 16384: 20 - 22.5 us, 3.1 - 3.4 TB/s), for small matrices by the latency of one trip to memory (1024 -> 4096,
-// two of them: 7.4 us), and for 64 f32 rows by cutting x, which every workgroup does (4096 -> 4096: 24 - 27 us)
+// two of them: 7.4 us), and for many rows by x, which every workgroup of 16 columns reads and, in f32, cuts again (64 rows, 4096 -> 4096: 14.6 us in bf16,
+// 26 - 29 in f32; workgroups of more columns would share it).  h in three parts for more than 32 rows takes two registers more than
+// there are, with groups of 32 thirty-two (64 f32 rows of 1024 -> 4096 -> 1024: 40 us, with groups of 32 47)
 #pragma once
 #include "train_rows.h"
 

@@ -4,16 +4,17 @@
 // part is held 2^11 times larger, so that it has all of f16's bits wherever the first one has: 22 bits of an element down to 2^-28 (|X| is near
 // one), and below that to 2^-50.  (Both parts in one scale end at 2^-25 of the largest element: rows 1e-6 of the
 // others' size would be 3e-3 off, and all of the direction 2e-2 after twelve steps.)  A = D + O and the polynomial B = b A + c A^2 are held
-// as their diagonals in f32 and the rest in two f16 parts likewise (2^13 times the value, and TS_B times), because the diagonals are the large
-// part and what is rounded there changes whole rows:
+// as their diagonals in f32 and the rest in two f16 parts likewise (2^13 times the value, and as far as B allows), because the diagonals are the
+// large part and what is rounded there changes whole rows:
 //     A^2 outside the diagonal = (d_i + d_j) O_ij + (O O)_ij,     row i of the new X = (a + B_ii) X_i + (rest of B) X.
 // The products take f16 on the matrix cores (train_gemm.h's tiles): first H L + L H, whose sum is then taken times 2^-11, on top of it H H; L L is left
 // out, 2^-22 of the result at most.  One part alone in any of the products is not enough, not even for bf16 results: what it
 // rounds off adds up over the steps to 4e-3 of the direction for matrices of low rank and to 4e-2 for exact rank one.
 // Symmetric products form the tiles that reach the diagonal from below and store their results twice.
-// Bound by the matrix cores for large matrices and by launches (three a step) for small ones.  One 4096 x 4096, bf16: a step's products 106
-// (X X^T), 127 (square), 129 us (1.06 PFLOP/s); twelve of 1024 x 4096, f32, three products each: 214, 79, 316 us (0.98 PFLOP/s); two of
-// 256 x 3136: 11, 13, 13 us and 6 of a join.  Passes over the elements: 4096 x 4096 13, 24, 18 us
+// Bound by the matrix cores for large matrices and by launches (three a step) for small ones.  One 4096 x 4096: a step's products 268
+// (X X^T), 287 (square), 333 us (1.24 PFLOP/s in X's product, a large library product's rate; the symmetric ones leave half of the
+// compute units idle); twelve of 1024 x 4096 215, 76, 324 us (0.95 PFLOP/s); two of 256 x 3136 11, 13, 13 us and 6 of a join.  Passes over the
+// elements: 4096 x 4096, bf16, 15, 24, 18 us
 #pragma once
 #include "train_gemm.h"
 
@@ -392,7 +393,7 @@ template <class P, bool MOVE> __global__ void __launch_bounds__(256) series_end_
 // The same steps on 16 x 16 results a wave.  Rows and k indices (to a multiple of 32) that there are not are zeros in LDS and stay zeros; a row's
 // elements begin 16 bytes further round the banks than the row's before.  The new X takes the old one's place: a wave takes 16 columns,
 // and reads all of them before it writes.
-// Bound by latency: three barriers a step, with a few LDS reads and products between them.  64 x 100, f32, five steps: 31 us (in tiles, eighteen
+// Bound by latency: three barriers a step, with a few LDS reads and products between them.  64 x 100, five steps: 32 us (in tiles, eighteen
 // launches: 132)
 #define TS_SMALL_LDS 151552
 #define TS_SMALL_THREADS 1024
