@@ -34,7 +34,7 @@ class GatedHead:
     renewed by each step); state_bits: 8 or 32.  optimizer: "adamw", or "muon" (steps along orthogonalised momentum, which is held in 32
     bits).  empty(shape, dtype) allocates zeros on the device.  The constructor waits for what it enqueues: answers and steps may
     use any stream.  Steps have to be ordered after each other, and answers after each other: each kind has buffers of its own and shares them with
-    nothing else, so an answer may be made within `loss` or beside a step; the weights that it reads move at the step's end."""
+    nothing else, so an answer on up to `rows` rows may be made within `loss` or beside a step; the weights that it reads move at the step's end."""
 
     def __init__(self, ctx, rows, weights, act, dtype, empty, state_bits=8, optimizer="adamw"):
         import torch
@@ -43,7 +43,7 @@ class GatedHead:
             raise ValueError("expected 'adamw' or 'muon', got %r" % (optimizer,))
 
         d_hidden, d_in = weights[0].shape
-        self.weights, self.steps = weights, 0
+        self.weights, self.rows, self.steps = weights, rows, 0
         self.ff = training.GatedFF(ctx, d_in, d_hidden, weights[2].shape[0], dtype, act)
         copies = None
         if dtype != torch.float32:
@@ -69,7 +69,8 @@ class GatedHead:
             torch.cuda.current_stream(weights[0].device).synchronize()
 
     def answer(self, x, y, stream=None):
-        self.ff.forward(x, *self.used, y, self.answer_ws, stream=stream)
+        # (more rows than a step's are answered in the steps' workspace, as far as that goes)
+        self.ff.forward(x, *self.used, y, self.answer_ws if x.shape[0] <= self.rows else self.ws, stream=stream)
 
     def step(self, x, loss, lr, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.0, stream=None):
         """One step on rows x.  loss(y, dy) writes the loss's gradient by the answers y into dy; what it returns is returned.  All of the step is

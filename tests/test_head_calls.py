@@ -73,3 +73,18 @@ def test_4_bit_answers_with_workspaces_of_their_own(where):
         torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert all(bool((ws != 255).any()) for ws in spaces)
+
+
+def test_answers_of_more_rows_than_a_step_has(where):
+    """as far as the steps' workspace goes"""
+    ctx, device = where
+    d, more = 15, 27
+    w = weights(d, 21, device)
+    h = head.GatedHead(ctx, 24, w, "square", BF16, empty_on(device))
+    wide = head.GatedHead(ctx, more, weights(d, 21, device), "square", BF16, empty_on(device))
+    assert h.answer_ws.numel() < h.ff.workspace_bytes(more) <= h.ws.numel()
+    x = some(3, more, d).to(BF16).to(device)
+    y, want = torch.zeros(more, d, dtype=BF16, device=device), torch.ones(more, d, dtype=BF16, device=device)
+    h.answer(x, y)
+    wide.answer(x, want)
+    assert torch.equal(y, want)
